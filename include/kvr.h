@@ -85,7 +85,12 @@ enum {
   KVR_DEV_PENDING_FULL = 8u, /* completion ring of a worker is full        */
   KVR_DEV_NODES_FULL = 16u,  /* node table of a worker is full             */
   KVR_DEV_ARENA_FULL = 32u,  /* token/child arena of a worker is full      */
-  KVR_DEV_INTERNAL = 64u     /* an internal consistency check failed       */
+  KVR_DEV_INTERNAL = 64u,    /* an internal consistency check failed       */
+  /* serving operators (below) */
+  KVR_DEV_PAGES_FULL = 128u, /* the ring holds fewer pages than are needed, or
+                                more would be given back than it can hold   */
+  KVR_DEV_ROW_FULL = 256u,   /* a row of a page table is too short          */
+  KVR_DEV_BAD_PAGE = 512u    /* a page number or slot outside the cache     */
 };
 
 typedef struct kvr_config {
@@ -292,6 +297,153 @@ uint64_t kvr_queries_done(const kvr_ctx* ctx);
 
 /* Free the host context.  Does not free or touch the caller's workspace. */
 void kvr_destroy(kvr_ctx* ctx);
+
+/* ------------------------------------------------------------------------
+ * Serving operators: what a worker that answers the routed queries does on
+ * its GPU with the tokens of its prefix-sharing cache (Sec. 3.2, "Cache
+ * Matching": the requests of a group share the longest prefix that the cache
+ * holds).  The keys and values of cached tokens stand in pages of 2^k tokens.
+ * A group's prefix has pages of its own, held once; each request has pages
+ * for its own tokens behind that prefix, so both may end anywhere in a page.
+ *
+ * The operators need no context: the caller owns every buffer, they run on
+ * the hip_stream given (NULL = the default stream) of the current device,
+ * allocate nothing, copy nothing to the host and do not synchronise, so they
+ * may be captured into a graph.  Every struct begins with struct_size =
+ * sizeof(the struct).  Strides count elements; the elements of a head are
+ * neighbours, and every head of every token starts on a 16-byte boundary.
+ * What only the device can see (lengths, page numbers) is checked there, as
+ * stated at each operator, and or-ed into a status word (KVR_DEV_*).
+ * ------------------------------------------------------------------------ */
+
+enum { KVR_BF16 = 0, KVR_FP16 = 1, KVR_FP8 = 2 }; /* element types; KVR_FP8: OCP e4m3 */
+
+/* Pages for rows that gain or lose tokens.  Row r (a request's own tokens, or
+ * a group's prefix) holds d_held[r] tokens in the first ceil(held / page_size)
+ * pages of d_table's row r, and is to hold d_held[r] + d_delta[r]: tokens are
+ * added at its end, or dropped from it (a request that ends drops all).
+ * Free pages stand in a ring of ring_size page numbers, at positions
+ * head .. tail - 1 modulo ring_size, d_state = {head, tail, status bits}.
+ * In the order of the rows, gained pages are taken at the head and dropped
+ * ones put back at the tail (in the order of the row's pages); a page put
+ * back can be taken from the next call on.
+ * Outputs: d_held_out[r] (may be d_held), d_state_out (may be d_state),
+ * d_row_start[r] = new tokens of the rows before r ([rows + 1]); and for new
+ * token t, counted over the rows, d_slots[t] = page * page_size + place in
+ * the page and d_positions[t] = d_base[r] + its place in the row (d_base NULL
+ * = 0; the length of the request's prefix).  num_tokens is the length of the
+ * last two, at least the number of new tokens; slots and positions behind
+ * them are -1.
+ * A batch that is not valid is rejected as a whole: the outputs are those of
+ * no change (all slots -1) and d_state_out's status bits gain
+ * KVR_DEV_BAD_LENGTH (a negative length, more new tokens than num_tokens),
+ * KVR_DEV_ROW_FULL (more than width * page_size tokens in a row) or
+ * KVR_DEV_PAGES_FULL. */
+typedef struct kvr_tables {
+  uint32_t struct_size;
+  int32_t rows;       /* 1..2^20                                            */
+  int32_t width;      /* pages of a table row, rows * width < 2^31          */
+  int32_t page_size;  /* a power of two, 1..1024                            */
+  int32_t ring_size;  /* pages of the pool; * page_size < 2^31              */
+  int32_t num_tokens; /* >= 0                                               */
+  int64_t table_stride;
+  const int32_t *d_held, *d_delta, *d_base;
+  int32_t *d_table, *d_ring;
+  const int64_t* d_state;
+  int32_t* d_held_out;
+  int64_t* d_state_out;
+  int32_t *d_row_start, *d_slots, *d_positions;
+} kvr_tables;
+
+/* Bytes of d_workspace that kvr_block_tables needs.  Pure host function. */
+kvr_status kvr_block_tables_workspace(const kvr_tables* t, size_t* bytes);
+
+kvr_status kvr_block_tables(const kvr_tables* t, void* d_workspace, size_t bytes, void* hip_stream);
+
+/* A layer's paged keys and values: element e of head h of the token in slot
+ * s stands at (s / page_size) * k_page + (s % page_size) * k_slot +
+ * h * k_head + e of d_k, and so for d_v.  With KVR_FP8 the values stand for
+ * d_k_scale[h] (d_v_scale[h]) times themselves (NULL = 1; > 0). */
+typedef struct kvr_cache {
+  uint32_t struct_size;
+  int32_t dtype;     /* KVR_BF16, KVR_FP16, KVR_FP8                         */
+  int32_t num_pages; /* num_pages * page_size < 2^31                        */
+  int32_t page_size; /* a power of two, 1..1024                             */
+  int32_t kv_heads;  /* 1..1024                                             */
+  int32_t dim;       /* 64, 128 or 256                                      */
+  void *d_k, *d_v;
+  int64_t k_page, k_slot, k_head;
+  int64_t v_page, v_slot, v_head;
+  const float *d_k_scale, *d_v_scale;
+} kvr_cache;
+
+/* Stores the keys and values of num_tokens tokens into the slots d_slots[t];
+ * a negative slot is skipped.  dtype is KVR_BF16 or KVR_FP16; the cache holds
+ * the same type (copied) or KVR_FP8: x * (1 / scale) in 32 bits, clamped to
+ * +-448 and rounded to nearest even, NaN stays NaN.  Slots are distinct.  A
+ * slot behind the cache is skipped and sets KVR_DEV_BAD_PAGE in d_status
+ * (optional). */
+typedef struct kvr_store {
+  uint32_t struct_size;
+  int32_t dtype;
+  int32_t num_tokens; /* >= 0; num_tokens * kv_heads * dim / 8 < 2^31       */
+  int32_t pad;
+  const void *d_k, *d_v;
+  int64_t k_token, k_head, v_token, v_head;
+  const int32_t* d_slots;
+  uint32_t* d_status;
+} kvr_store;
+
+kvr_status kvr_cache_store(const kvr_cache* c, const kvr_store* s, void* hip_stream);
+
+/* Attention of new tokens over a shared prefix and their request's own tokens.
+ * Request r has the new tokens d_row_start[r] .. d_row_start[r + 1] - 1 of
+ * d_q (d_row_start NULL: one each, num_tokens = num_requests); d_length[r] is
+ * the number of its own tokens, the new ones, which are the last, included.
+ * Its requests are ordered by group: group j's are d_group_start[j] ..
+ * d_group_start[j + 1] - 1 ([num_groups + 1], 0 first and num_requests last),
+ * and d_prefix_length[j] tokens of prefix precede the own tokens of each, in
+ * the pages of row j of d_prefix_table.  num_groups = 0: no prefixes.  Any
+ * length may be 0.  For a new token t of request r and a query head i
+ *   out[t][i] = sum_k softmax_k(scale * q[t][i] . K_k[h]) V_k[h],
+ *   h = i / (heads / kv_heads),
+ * over the prefix and the own tokens up to t itself; lse[t][i] (optional,
+ * [num_tokens][heads]) is the natural logarithm of the softmax's sum.
+ * Whatever stands in the cache behind a length or in a later token (an
+ * infinity or NaN among them) has no influence on a row; a row that sees no
+ * key gets 0 and lse -inf.  Tokens behind d_row_start's last are not written.
+ * A prefix is read once for a whole group where its requests have few new
+ * tokens each, and the partial results are joined.  The order of the sums
+ * depends on the lengths, not on the run: the same call gives the same bits.
+ * Lengths that are not valid (negative or decreasing, longer than the
+ * table's row, fewer own than new tokens) set KVR_DEV_BAD_LENGTH in d_status
+ * (optional) and every result is NaN; a page number that is not one of the
+ * cache sets KVR_DEV_BAD_PAGE and the rows that see it are NaN. */
+typedef struct kvr_attention {
+  uint32_t struct_size;
+  int32_t dtype;        /* of d_q and d_out: KVR_BF16 or KVR_FP16; the cache's
+                           type or, with a KVR_FP8 cache, either            */
+  int32_t num_tokens;   /* >= 0; num_tokens * heads < 2^31                  */
+  int32_t num_requests; /* 1..2^20                                          */
+  int32_t num_groups;   /* 0..2^20                                          */
+  int32_t heads;        /* a multiple of kv_heads                           */
+  int32_t width, prefix_width; /* pages of a row of the tables              */
+  float scale;          /* finite, > 0                                      */
+  int32_t pad;
+  const void* d_q;
+  void* d_out;
+  float* d_lse;
+  int64_t q_token, q_head, out_token, out_head;
+  const int32_t *d_row_start, *d_length, *d_table, *d_group_start, *d_prefix_table, *d_prefix_length;
+  int64_t table_stride, prefix_stride;
+  uint32_t* d_status;
+} kvr_attention;
+
+/* Bytes of d_workspace that kvr_shared_attention needs.  Pure host function. */
+kvr_status kvr_attention_workspace(const kvr_cache* c, const kvr_attention* a, size_t* bytes);
+
+kvr_status kvr_shared_attention(const kvr_cache* c, const kvr_attention* a, void* d_workspace, size_t bytes,
+                                void* hip_stream);
 
 /* Message for the last failure on this thread ("" if none). */
 const char* kvr_last_error(void);

@@ -29,7 +29,9 @@ PHASE_NAMES = ["route", "stage_wait", "mark", "load", "evict", "finish", "match"
                "e_match"]
 
 EXPORTED = ["kvr_config_default", "kvr_workspace_size", "kvr_init_replicas", "kvr_route_batch",
-            "kvr_stats", "kvr_stats_noalloc", "kvr_check", "kvr_queries_done", "kvr_destroy", "kvr_last_error"]
+            "kvr_stats", "kvr_stats_noalloc", "kvr_check", "kvr_queries_done", "kvr_destroy", "kvr_last_error",
+            "kvr_block_tables_workspace", "kvr_block_tables", "kvr_cache_store", "kvr_attention_workspace",
+            "kvr_shared_attention"]
 
 
 class KvrConfig(ctypes.Structure):
@@ -139,6 +141,14 @@ def load_library() -> ctypes.CDLL:
     lib.kvr_queries_done.argtypes = [vp]
     lib.kvr_destroy.restype = None
     lib.kvr_destroy.argtypes = [vp]
+    size_p = ctypes.POINTER(ctypes.c_size_t)
+    for name, args in (("kvr_block_tables_workspace", [vp, size_p]),
+                       ("kvr_block_tables", [vp, vp, ctypes.c_size_t, vp]),
+                       ("kvr_cache_store", [vp, vp, vp]),
+                       ("kvr_attention_workspace", [vp, vp, size_p]),
+                       ("kvr_shared_attention", [vp, vp, vp, ctypes.c_size_t, vp])):
+        getattr(lib, name).restype = ctypes.c_int
+        getattr(lib, name).argtypes = args
     lib.kvr_last_error.restype = ctypes.c_char_p
     lib.kvr_last_error.argtypes = []
     _lib = lib
@@ -255,4 +265,47 @@ def kvr_destroy(ctx: int) -> None:
         load_library().kvr_destroy(ctypes.c_void_p(ctx))
 
 
+# Serving operators: the arguments are the packed structs of include/kvr.h
+# (bytearrays); the functions on tensors that pack them are in serve.py.
+
+def _struct(args: bytearray):
+    return ctypes.byref((ctypes.c_char * len(args)).from_buffer(args))
+
+
+def kvr_block_tables_workspace(tables: bytearray) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load_library().kvr_block_tables_workspace(_struct(tables), ctypes.byref(n)), "kvr_block_tables_workspace")
+    return n.value
+
+
+def kvr_block_tables(tables: bytearray, d_workspace: int, nbytes: int, stream: int = 0) -> None:
+    _check(load_library().kvr_block_tables(_struct(tables), d_workspace, nbytes, stream), "kvr_block_tables")
+
+
+def kvr_cache_store(cache: bytearray, store: bytearray, stream: int = 0) -> None:
+    _check(load_library().kvr_cache_store(_struct(cache), _struct(store), stream), "kvr_cache_store")
+
+
+def kvr_attention_workspace(cache: bytearray, attention: bytearray) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load_library().kvr_attention_workspace(_struct(cache), _struct(attention), ctypes.byref(n)),
+           "kvr_attention_workspace")
+    return n.value
+
+
+def kvr_shared_attention(cache: bytearray, attention: bytearray, d_workspace: int, nbytes: int,
+                         stream: int = 0) -> None:
+    _check(load_library().kvr_shared_attention(_struct(cache), _struct(attention), d_workspace, nbytes, stream),
+           "kvr_shared_attention")
+
+
 from .sim import Simulator  # noqa: E402,F401
+
+
+def __getattr__(name: str):
+    # the functions on torch tensors: torch is imported when one is first used
+    if name in ("BlockTables", "block_tables", "page_ring", "cache_store", "shared_attention", "check_status"):
+        from . import serve
+        globals()[name] = getattr(serve, name)
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

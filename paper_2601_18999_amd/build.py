@@ -8,15 +8,18 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkvr.so")
-SOURCES = ["kvr_device.hip", "kvr_api.cpp"]
+SOURCES = ["kvr_device.hip", "kvr_api.cpp", "kvr_serve.hip", "kvr_serve_api.cpp", "kvr_attend_64.hip",
+           "kvr_attend_128.hip", "kvr_attend_256.hip"]
 ARCH = os.environ.get("KVR_OFFLOAD_ARCH", "gfx950")
 
 FLAGS = [
-    "-O3", "-std=c++17", "-fPIC", "-shared",
+    "-O3", "-std=c++17", "-fPIC",
     # no fused multiply-add: results must equal the IEEE left-to-right definition
     "-ffp-contract=off",
     # keep packed fp32 instructions out of the device code
@@ -35,18 +38,24 @@ def hipcc() -> str:
 
 
 def build(verbose: bool = False) -> str:
-    """Compile every source into libkvr.so (always recompiles)."""
+    """Compile every source (side by side) and link libkvr.so (always recompiles)."""
     tmp = LIB + ".tmp"
-    cmd = [hipcc(), f"--offload-arch={ARCH}", *FLAGS, "-o", tmp,
-           *[os.path.join(CSRC, s) for s in SOURCES]]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    err = "\n".join(l for l in res.stderr.splitlines() if "packed-fp32-ops" not in l)
-    if res.returncode != 0:
-        raise RuntimeError(f"hipcc failed ({res.returncode}):\n{err}")
-    if verbose and err.strip():
-        print(err, file=sys.stderr)
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        res = subprocess.run(cmd, capture_output=True, text=True)
+        err = "\n".join(l for l in res.stderr.splitlines() if "packed-fp32-ops" not in l)
+        if res.returncode != 0:
+            raise RuntimeError(f"hipcc failed ({res.returncode}):\n{err}")
+        if verbose and err.strip():
+            print(err, file=sys.stderr)
+
+    with tempfile.TemporaryDirectory() as tdir, ThreadPoolExecutor(max_workers=len(SOURCES)) as pool:
+        objects = [os.path.join(tdir, os.path.splitext(s)[0] + ".o") for s in SOURCES]
+        list(pool.map(run, [[hipcc(), f"--offload-arch={ARCH}", *FLAGS, "-c", "-o", o, os.path.join(CSRC, s)]
+                            for s, o in zip(SOURCES, objects)]))
+        run([hipcc(), f"--offload-arch={ARCH}", "-fPIC", "-shared", "-o", tmp, *objects])
     os.replace(tmp, LIB)
     return LIB
 

@@ -14,6 +14,7 @@
 #include <string>
 
 #include "kvr_layout.h"
+#include "kvr_serve.h"
 
 namespace kvr {
 hipError_t launch_init(char* ws, const Layout& L, double rls_p0, hipStream_t st);
@@ -141,6 +142,17 @@ std::string describe_bits(uint32_t bits) {
 }
 
 }  // namespace
+
+namespace kvr {
+kvr_status set_error(kvr_status st, const char* msg) noexcept {
+  try {
+    g_err = msg;
+  } catch (...) {
+    g_err.clear();
+  }
+  return st;
+}
+}  // namespace kvr
 
 extern "C" {
 

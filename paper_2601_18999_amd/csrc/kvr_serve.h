@@ -1,0 +1,145 @@
+// kvr_serve.h - arguments of the serving kernels (page tables, cache store,
+// shared-prefix attention): what the host side fills in and the device side
+// reads.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+#include "../../include/kvr.h"
+
+namespace kvr {
+
+// Compute units of a gfx950 device and the attention workgroups that one of
+// them holds: the width that the attention work is split for.
+constexpr int kComputeUnits = 256;
+constexpr int kAttendSlots = 2 * kComputeUnits;
+constexpr int kTileRows = 128;  // most query rows of an attention workgroup
+constexpr int kStepKeys = 64;   // keys of one step: what the plan counts in
+
+// n / d for n < 2^31 by a multiplication, exact (d >= 1, d < 2^31).
+struct Divisor {
+  uint32_t d, mul, shift;
+};
+
+inline Divisor make_divisor(uint32_t d) {
+  // smallest s with 2^s >= d; mul = ceil(2^(31+s) / d) < 2^32 keeps
+  // n * mul / 2^(31+s) within 1/d of n / d for n < 2^31
+  uint32_t s = 0;
+  while ((1ull << s) < d) ++s;
+  Divisor v;
+  v.d = d;
+  v.shift = s;
+  v.mul = (uint32_t)(((1ull << (31 + s)) + d - 1) / d);
+  return v;
+}
+
+__host__ __device__ inline uint32_t divide(uint32_t n, const Divisor& v) {
+  return (uint32_t)(((uint64_t)n * v.mul) >> (31 + v.shift));
+}
+
+// ---- page tables ----
+struct TablesHdr {
+  int64_t head, tail;  // the ring before the call
+  int32_t gain, give;  // pages taken and given back
+  int32_t tokens;      // new tokens
+  int32_t rejected;
+};
+
+struct TablesArgs {
+  const int32_t *held, *delta, *base;
+  int32_t *table, *ring;
+  const int64_t* state;
+  int32_t* held_out;
+  int64_t* state_out;
+  int32_t *row_start, *slots, *positions;
+  TablesHdr* hdr;
+  int32_t *gain_at, *give_at;  // [rows + 1] pages taken / given back before a row
+  int64_t table_stride;
+  int32_t rows, width, page_shift, ring_size, num_tokens;
+};
+
+// ---- cache store ----
+struct StoreArgs {
+  const char *k, *v;
+  char *kc, *vc;
+  const float *ks, *vs;
+  const int32_t* slots;
+  uint32_t* status;
+  int64_t k_tok, k_head, v_tok, v_head;                       // bytes
+  int64_t kc_page, kc_slot, kc_head, vc_page, vc_slot, vc_head;  // bytes
+  Divisor chunks;  // 16-byte source chunks of a token: kv_heads * dim / 8
+  int32_t tokens, dim_shift, page_shift, slots_limit;
+  int32_t fp8, fp16;
+};
+
+// ---- attention ----
+// One unit: up to 128 consecutive query rows (row = token * share + head in
+// its key head's share) of one request, or of one group against its shared
+// prefix.  One item: a range of a unit's key steps, one workgroup per key
+// head.  Items of a unit are consecutive, and so are their partial results.
+struct Unit {
+  int32_t row0, rows;
+  int32_t acc, splits;           // first partial row (-1: written directly), items
+  int32_t group_unit, group_row; // first unit of its group's prefix (-1: none) and that unit's row0
+  int32_t own;                   // 1: a request's unit (0: a group's)
+  int32_t pad;
+};
+
+struct Item {
+  int32_t row0, rows;
+  int32_t step0, step1;    // key steps: the prefix's first, then the own tokens'
+  int32_t prefix_steps;    // steps of the prefix among them
+  int32_t prefix, prefix_len;
+  int32_t request, own_end; // own keys that some row of the unit sees
+  int32_t limit;           // a row of token t sees own keys below t + limit
+  int32_t acc;             // first partial row, -1: final
+  int32_t pad;
+};
+
+struct PlanHdr {
+  int32_t units, items, rejected, pad;
+};
+
+struct AttendArgs {
+  const char* q;
+  char* out;
+  float* lse;
+  const char *kc, *vc;
+  const float *ks, *vs;
+  int64_t q_tok, q_head, o_tok, o_head;                          // bytes
+  int64_t kc_page, kc_slot, kc_head, vc_page, vc_slot, vc_head;  // bytes
+  const int32_t *row_start, *length, *table, *group_start, *prefix_table, *prefix_length;
+  int64_t table_stride, prefix_stride;
+  uint32_t* status;
+  PlanHdr* hdr;
+  int32_t* bounds;  // [groups + requests + 1] first unit of a group / request
+  int32_t* group_of;  // [requests]
+  int32_t* waves;     // [groups] row waves of its requests, then: 1 = shared
+  Unit* units;
+  Item* items;
+  float2* ml;  // [partial row][kv head] running maximum (log2 units) and sum
+  float* acc;  // [partial row][kv head][dim]
+  Divisor share;
+  float scale_log2;
+  int32_t tokens, requests, groups, heads, kv_heads, dim;
+  int32_t page_shift, num_pages, width, prefix_width;
+  int32_t unit_cap, item_cap, split_slots;
+};
+
+hipError_t launch_tables(const TablesArgs& a, hipStream_t st);
+hipError_t launch_store(const StoreArgs& a, hipStream_t st);
+hipError_t launch_attend_plan(const AttendArgs& a, hipStream_t st);
+hipError_t launch_attend_join(const AttendArgs& a, bool fp16, hipStream_t st);
+// fp16: queries and results are 16-bit IEEE, else bfloat16; fp8: the cache
+// holds 8-bit e4m3, else the queries' type
+hipError_t launch_attend_64(const AttendArgs& a, bool fp16, bool fp8, hipStream_t st);
+hipError_t launch_attend_128(const AttendArgs& a, bool fp16, bool fp8, hipStream_t st);
+hipError_t launch_attend_256(const AttendArgs& a, bool fp16, bool fp8, hipStream_t st);
+
+// Sets the message that kvr_last_error returns on this thread.
+kvr_status set_error(kvr_status st, const char* msg) noexcept;
+
+}  // namespace kvr

@@ -1,0 +1,525 @@
+// kvr_serve.hip - kernels of the serving operators but the attention itself:
+// page tables and slot maps, the store of new keys and values, and the plan
+// and the join of the attention.
+#include "kvr_serve.h"
+
+namespace kvr {
+namespace {
+
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// Sum over the lanes before this one, and (by reference) over all lanes.
+template <class V>
+__device__ __forceinline__ V wave_before(V x, V& all) {
+  const int lane = threadIdx.x & 63;
+  V s = x;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const V y = __shfl_up(s, d);
+    if (lane >= d) s += y;
+  }
+  all = __shfl(s, 63);
+  return s - x;
+}
+
+// The same over a workgroup of up to 16 waves; `part` is 17 values of LDS.
+// Every thread of the workgroup calls it.
+template <class V>
+__device__ __forceinline__ V group_before(V x, V& all, V* part) {
+  const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  V w, s = wave_before(x, w);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) part[wave] = w;
+  __syncthreads();
+  V sum = 0;
+  for (int i = 0; i < waves; ++i) {
+    if (i == wave) s += sum;
+    sum += part[i];
+  }
+  all = sum;
+  return s;
+}
+
+// Largest i of [0, n) with start[i] <= x, for start ascending and start[0] <= x.
+template <class P>
+__device__ __forceinline__ int last_at_most(P start, int n, int x) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (start[mid] <= x)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  return lo;
+}
+
+// ---------------------------------------------------------------- page tables
+
+constexpr int kScanThreads = 1024;
+
+struct RowChange {
+  int64_t tokens, pages;  // new tokens; pages taken (low word) and given back (high word)
+  uint32_t bits;
+};
+
+__device__ __forceinline__ RowChange row_change(const TablesArgs& a, int held, int delta) {
+  RowChange c = {0, 0, 0};
+  const int64_t total = (int64_t)held + delta, page = 1ll << a.page_shift;
+  if (held < 0 || total < 0) {
+    c.bits = KVR_DEV_BAD_LENGTH;
+  } else if (held > ((int64_t)a.width << a.page_shift) || total > ((int64_t)a.width << a.page_shift)) {
+    c.bits = KVR_DEV_ROW_FULL;
+  } else {
+    const int64_t before = (held + page - 1) >> a.page_shift, after = (total + page - 1) >> a.page_shift;
+    c.tokens = delta > 0 ? delta : 0;
+    c.pages = after > before ? after - before : (before - after) << 32;
+  }
+  return c;
+}
+
+// One workgroup: sums over the rows, the checks, and everything that is one
+// value a row.  A thread takes neighbouring rows.
+__global__ void __launch_bounds__(kScanThreads) tables_scan_kernel(TablesArgs a) {
+  __shared__ int64_t part[17];
+  const int per = (a.rows + kScanThreads - 1) / kScanThreads;
+  const int r0 = min(a.rows, (int)threadIdx.x * per), r1 = min(a.rows, r0 + per);
+  const int64_t head = a.state[0], tail = a.state[1], old_bits = a.state[2];
+  int64_t tokens = 0, pages = 0;
+  uint32_t bits = 0;
+  for (int r = r0; r < r1; ++r) {
+    const RowChange c = row_change(a, a.held[r], a.delta[r]);
+    tokens += c.tokens;
+    pages += c.pages;
+    bits |= c.bits;
+  }
+  int64_t all_tokens, all_pages;
+  tokens = group_before(tokens, all_tokens, part);
+  pages = group_before(pages, all_pages, part);
+  const int64_t gain = all_pages & 0xffffffffll, give = all_pages >> 32;
+  bits = (__syncthreads_or(bits & KVR_DEV_BAD_LENGTH) ? KVR_DEV_BAD_LENGTH : 0u) |
+         (__syncthreads_or(bits & KVR_DEV_ROW_FULL) ? KVR_DEV_ROW_FULL : 0u);
+  if (all_tokens > a.num_tokens) bits |= KVR_DEV_BAD_LENGTH;
+  if (head < 0 || tail < head || tail - head > a.ring_size || gain > tail - head) bits |= KVR_DEV_PAGES_FULL;
+  // more pages free than there are
+  if (tail - head + give > a.ring_size) bits |= KVR_DEV_PAGES_FULL;
+  for (int r = r0; r < r1; ++r) {
+    const int held = a.held[r], delta = a.delta[r];
+    const RowChange c = row_change(a, held, delta);
+    a.row_start[r] = bits ? 0 : (int)tokens;
+    a.gain_at[r] = (int)(pages & 0xffffffffll);
+    a.give_at[r] = (int)(pages >> 32);
+    a.held_out[r] = bits ? held : held + delta;
+    tokens += c.tokens;
+    pages += c.pages;
+  }
+  if (threadIdx.x == 0) {
+    a.row_start[a.rows] = bits ? 0 : (int)all_tokens;
+    a.gain_at[a.rows] = (int)gain;
+    a.give_at[a.rows] = (int)give;
+    TablesHdr h;
+    h.head = head;
+    h.tail = tail;
+    h.gain = (int)gain;
+    h.give = (int)give;
+    h.tokens = (int)all_tokens;
+    h.rejected = bits != 0;
+    *a.hdr = h;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    a.state_out[0] = bits ? head : head + gain;
+    a.state_out[1] = bits ? tail : tail + give;
+    a.state_out[2] = old_bits | bits;
+  }
+}
+
+constexpr int kFillThreads = 256, kFillTokens = 4;  // tokens of a thread
+
+// Slots and positions of the new tokens, the pages they gain, and the pages
+// that are given back.  A token's row is found in row_start; the first token
+// of a gained page writes its table entry (a gained page always has one).
+__global__ void __launch_bounds__(kFillThreads) tables_fill_kernel(TablesArgs a) {
+  const TablesHdr h = *a.hdr;
+  const int mask = (1 << a.page_shift) - 1;
+  const int t0 = blockIdx.x * kFillThreads * kFillTokens;
+#pragma unroll
+  for (int i = 0; i < kFillTokens; ++i) {
+    const int t = t0 + i * kFillThreads + threadIdx.x;
+    if (t >= a.num_tokens) break;
+    int slot = -1, position = -1;
+    if (!h.rejected && t < h.tokens) {
+      const int r = last_at_most(a.row_start, a.rows, t);
+      const int held = a.held_out[r] - a.delta[r];
+      const int at = held + t - a.row_start[r];
+      const int col = at >> a.page_shift, before = (int)(((int64_t)held + mask) >> a.page_shift);
+      int32_t* entry = a.table + r * a.table_stride + col;
+      int page;
+      if (col < before) {
+        page = *entry;
+      } else {
+        page = a.ring[(h.head + a.gain_at[r] + col - before) % a.ring_size];
+        if ((at & mask) == 0) *entry = page;
+      }
+      slot = (page << a.page_shift) | (at & mask);
+      position = (a.base ? a.base[r] : 0) + at;
+    }
+    a.slots[t] = slot;
+    a.positions[t] = position;
+  }
+  if (h.rejected) return;
+  for (int g = blockIdx.x * kFillThreads + threadIdx.x; g < h.give; g += gridDim.x * kFillThreads) {
+    const int r = last_at_most(a.give_at, a.rows, g);
+    const int after = (int)(((int64_t)a.held_out[r] + mask) >> a.page_shift);
+    a.ring[(h.tail + g) % a.ring_size] = a.table[r * a.table_stride + after + g - a.give_at[r]];
+  }
+}
+
+// ---------------------------------------------------------------- cache store
+
+__device__ __forceinline__ int to_fp8(float a, float b, float c, float d) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+
+// fminf and fmaxf drop a NaN: it stays one
+__device__ __forceinline__ float clamp_fp8(float x) { return x != x ? x : fminf(fmaxf(x, -448.0f), 448.0f); }
+
+__device__ __forceinline__ void widen8(i32x4 x, int fp16, float* f) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if (fp16) {
+      f[2 * j] = (float)__builtin_bit_cast(_Float16, (short)(x[j] & 0xffff));
+      f[2 * j + 1] = (float)__builtin_bit_cast(_Float16, (short)((uint32_t)x[j] >> 16));
+    } else {
+      f[2 * j] = __uint_as_float((uint32_t)x[j] << 16);
+      f[2 * j + 1] = __uint_as_float((uint32_t)x[j] & 0xffff0000u);
+    }
+  }
+}
+
+// 8 elements of K and of V a thread.
+template <bool FP8>
+__global__ void __launch_bounds__(256) store_kernel(StoreArgs a) {
+  const uint32_t n = blockIdx.x * 256u + threadIdx.x;
+  const uint32_t t = divide(n, a.chunks);
+  if (t >= (uint32_t)a.tokens) return;
+  const int c = (int)(n - t * a.chunks.d) * 8, head = c >> a.dim_shift, d = c & ((1 << a.dim_shift) - 1);
+  const int slot = a.slots[t];
+  if (slot < 0) return;
+  if (slot >= a.slots_limit) {
+    if (a.status) atomicOr(a.status, (uint32_t)KVR_DEV_BAD_PAGE);
+    return;
+  }
+  const int64_t page = slot >> a.page_shift, at = slot & ((1 << a.page_shift) - 1);
+  const i32x4 k = *(const i32x4*)(a.k + t * a.k_tok + head * a.k_head + d * 2);
+  const i32x4 v = *(const i32x4*)(a.v + t * a.v_tok + head * a.v_head + d * 2);
+  char* kc = a.kc + page * a.kc_page + at * a.kc_slot + head * a.kc_head;
+  char* vc = a.vc + page * a.vc_page + at * a.vc_slot + head * a.vc_head;
+  if constexpr (FP8) {
+    float f[8];
+    const float ks = a.ks ? 1.0f / a.ks[head] : 1.0f, vs = a.vs ? 1.0f / a.vs[head] : 1.0f;
+    widen8(k, a.fp16, f);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = clamp_fp8(f[j] * ks);
+    *(i32x2*)(kc + d) = i32x2{to_fp8(f[0], f[1], f[2], f[3]), to_fp8(f[4], f[5], f[6], f[7])};
+    widen8(v, a.fp16, f);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = clamp_fp8(f[j] * vs);
+    *(i32x2*)(vc + d) = i32x2{to_fp8(f[0], f[1], f[2], f[3]), to_fp8(f[4], f[5], f[6], f[7])};
+  } else {
+    *(i32x4*)(kc + d * 2) = k;
+    *(i32x4*)(vc + d * 2) = v;
+  }
+}
+
+// ---------------------------------------------------------------- attention: the plan
+
+constexpr int kPlanThreads = 1024;
+constexpr int kMinSplitCost = 8;  // least cost of an item that a unit is split into
+
+// Waves along the rows that `rows` rows take in tiles of kTileRows.
+__device__ __forceinline__ int row_waves(int rows) {
+  const int rest = rows % kTileRows;
+  return rows / kTileRows * 4 + (rest == 0 ? 0 : rest <= 32 ? 1 : rest <= 64 ? 2 : 4);
+}
+
+__device__ __forceinline__ int steps_of(int keys) { return (keys + kStepKeys - 1) / kStepKeys; }
+
+struct UnitWork {
+  Item it;
+  int steps, cost;
+  int group;  // the group whose shared partial results the unit's rows have, or -1
+};
+
+// Unit u of segment s (a group, or groups + a request).
+__device__ UnitWork unit_work(const AttendArgs& a, int s, int tile) {
+  UnitWork w;
+  const int g = (int)a.share.d;
+  w.group = -1;
+  w.it.pad = 0;
+  w.it.acc = -1;
+  w.it.step0 = 0;
+  if (s < a.groups) {
+    const int b0 = a.group_start[s], b1 = a.group_start[s + 1];
+    const int t0 = a.row_start ? a.row_start[b0] : b0, t1 = a.row_start ? a.row_start[b1] : b1;
+    w.it.row0 = t0 * g + tile * kTileRows;
+    w.it.rows = min(kTileRows, t1 * g - w.it.row0);
+    w.it.prefix = s;
+    w.it.prefix_len = a.prefix_length[s];
+    w.it.prefix_steps = steps_of(w.it.prefix_len);
+    w.it.request = 0;
+    w.it.own_end = 0;
+    w.it.limit = 0;
+    w.steps = w.it.prefix_steps;
+  } else {
+    const int b = s - a.groups;
+    const int t0 = a.row_start ? a.row_start[b] : b, t1 = a.row_start ? a.row_start[b + 1] : b + 1;
+    w.it.row0 = t0 * g + tile * kTileRows;
+    w.it.rows = min(kTileRows, t1 * g - w.it.row0);
+    w.it.request = b;
+    w.it.limit = a.length[b] - (t1 - t0) - t0 + 1;
+    const int last = (int)divide((uint32_t)(w.it.row0 + w.it.rows - 1), a.share);
+    w.it.own_end = last + w.it.limit;
+    w.it.prefix = 0;
+    w.it.prefix_len = 0;
+    w.it.prefix_steps = 0;
+    if (a.groups) {
+      const int j = a.group_of[b];
+      if (a.waves[j] == 1) {
+        w.group = j;
+      } else {
+        w.it.prefix = j;
+        w.it.prefix_len = a.prefix_length[j];
+        w.it.prefix_steps = steps_of(w.it.prefix_len);
+      }
+    }
+    w.steps = w.it.prefix_steps + steps_of(w.it.own_end);
+  }
+  w.it.step1 = w.steps;
+  w.cost = w.steps * row_waves(w.it.rows);
+  return w;
+}
+
+// One workgroup: checks the lengths, decides which groups take their prefix
+// for all requests at once, and cuts the units into items of about equal cost.
+__global__ void __launch_bounds__(kPlanThreads) plan_kernel(AttendArgs a) {
+  __shared__ int part[17];
+  __shared__ int64_t part64[17];
+  const int g = (int)a.share.d, tid = threadIdx.x;
+  // checks
+  bool bad = false;
+  for (int b = tid; b < a.requests; b += kPlanThreads) {
+    const int t0 = a.row_start ? a.row_start[b] : b, t1 = a.row_start ? a.row_start[b + 1] : b + 1;
+    const int n = a.length[b];
+    bad |= t0 < 0 || t1 < t0 || t1 > a.tokens || n < t1 - t0 || n > ((int64_t)a.width << a.page_shift);
+    if (b == 0) bad |= t0 != 0;
+  }
+  for (int j = tid; j < a.groups; j += kPlanThreads) {
+    const int b0 = a.group_start[j], b1 = a.group_start[j + 1], p = a.prefix_length[j];
+    bad |= b0 < 0 || b1 < b0 || b1 > a.requests || p < 0 || p > ((int64_t)a.prefix_width << a.page_shift);
+    if (j == 0) bad |= b0 != 0;
+    if (j == a.groups - 1) bad |= b1 != a.requests;
+    a.waves[j] = 0;
+  }
+  if (__syncthreads_or(bad)) {
+    if (tid == 0) {
+      a.hdr->units = 0;
+      a.hdr->items = 0;
+      a.hdr->rejected = 1;
+      if (a.status) atomicOr(a.status, (uint32_t)KVR_DEV_BAD_LENGTH);
+    }
+    return;
+  }
+  // waves along the rows that the requests of a group take one by one
+  for (int b = tid; b < a.requests && a.groups; b += kPlanThreads) {
+    const int t0 = a.row_start ? a.row_start[b] : b, t1 = a.row_start ? a.row_start[b + 1] : b + 1;
+    const int j = last_at_most(a.group_start, a.groups, b);
+    a.group_of[b] = j;
+    atomicAdd(&a.waves[j], row_waves((t1 - t0) * g));
+  }
+  __syncthreads();
+  // units: a group's (its prefix, if that is shared), then a request's
+  const int segments = a.groups + a.requests;
+  int units = 0;
+  for (int s0 = 0; s0 < segments; s0 += kPlanThreads) {
+    const int s = s0 + tid;
+    int count = 0;
+    if (s < a.groups) {
+      const int b0 = a.group_start[s], b1 = a.group_start[s + 1];
+      const int t0 = a.row_start ? a.row_start[b0] : b0, t1 = a.row_start ? a.row_start[b1] : b1;
+      const int rows = (t1 - t0) * g;
+      const bool shared = a.prefix_length[s] > 0 && row_waves(rows) * 4 <= a.waves[s] * 3;
+      a.waves[s] = shared ? 1 : 0;
+      count = shared ? (rows + kTileRows - 1) / kTileRows : 0;
+    } else if (s < segments) {
+      const int b = s - a.groups;
+      const int t0 = a.row_start ? a.row_start[b] : b, t1 = a.row_start ? a.row_start[b + 1] : b + 1;
+      count = ((t1 - t0) * g + kTileRows - 1) / kTileRows;
+    }
+    int all;
+    const int before = group_before(count, all, part);
+    if (s < segments) a.bounds[s] = units + before;
+    units += all;
+  }
+  if (tid == 0) a.bounds[segments] = units;
+  __syncthreads();
+  int64_t total = 0;
+  for (int u = tid; u < units; u += kPlanThreads) {
+    const int s = last_at_most(a.bounds, segments, u);
+    total += unit_work(a, s, u - a.bounds[s]).cost;
+  }
+  group_before(total, total, part64);
+  const int64_t fair = (total + a.split_slots - 1) / a.split_slots;
+  const int chunk = (int)(fair < kMinSplitCost ? kMinSplitCost : fair > 0x7fffffff ? 0x7fffffff : fair);
+  int items = 0, rows_acc = 0;
+  for (int u0 = 0; u0 < units; u0 += kPlanThreads) {
+    const int u = u0 + tid;
+    UnitWork w;
+    int splits = 0, per = 1, partial = 0;
+    if (u < units) {
+      const int s = last_at_most(a.bounds, segments, u);
+      w = unit_work(a, s, u - a.bounds[s]);
+      splits = max(1, (w.cost + chunk - 1) / chunk);
+      per = max(1, (w.steps + splits - 1) / splits);
+      splits = max(1, (w.steps + per - 1) / per);
+      partial = s < a.groups || w.group >= 0 || splits > 1 ? splits * w.it.rows : 0;
+    }
+    int all_items, all_rows;
+    const int i0 = items + group_before(splits, all_items, part);
+    const int acc = rows_acc + group_before(partial, all_rows, part);
+    items += all_items;
+    rows_acc += all_rows;
+    if (u < units) {
+      Unit x;
+      x.row0 = w.it.row0;
+      x.rows = w.it.rows;
+      x.acc = partial ? acc : -1;
+      x.splits = splits;
+      x.group_unit = -1;
+      x.group_row = 0;
+      x.pad = 0;
+      if (w.group >= 0) {
+        const int b0 = a.group_start[w.group];
+        x.group_unit = a.bounds[w.group];
+        x.group_row = (a.row_start ? a.row_start[b0] : b0) * g;
+      }
+      x.own = u >= a.bounds[a.groups];
+      a.units[u] = x;
+      for (int i = 0; i < splits; ++i) {
+        Item it = w.it;
+        it.step0 = min(w.steps, i * per);
+        it.step1 = min(w.steps, (i + 1) * per);
+        it.acc = partial ? acc + i * w.it.rows : -1;
+        a.items[i0 + i] = it;
+      }
+    }
+  }
+  if (tid == 0) {
+    a.hdr->units = units;
+    a.hdr->items = items;
+    a.hdr->rejected = 0;
+  }
+}
+
+// ---------------------------------------------------------------- attention: the join
+
+// Joins the partial results of a request's unit, its own splits' and those of
+// its group's prefix: m = max m_i, l = sum l_i 2^(m_i - m), o likewise.
+template <bool FP16>
+__global__ void __launch_bounds__(256) join_kernel(AttendArgs a) {
+  const int u = blockIdx.x / a.kv_heads, head = blockIdx.x % a.kv_heads;
+  const int quads = a.dim / 4;
+  if (a.hdr->rejected) {  // nothing was computed: every result is NaN
+    const int64_t all = (int64_t)a.tokens * a.heads * quads, step = (int64_t)gridDim.x * 256;
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < all; i += step) {
+      const int64_t th = i / quads;
+      *(i32x2*)(a.out + th / a.heads * a.o_tok + th % a.heads * a.o_head + i % quads * 8) = i32x2{-1, -1};
+      if (a.lse && i % quads == 0) a.lse[th] = __uint_as_float(0x7fc00000u);
+    }
+    return;
+  }
+  if (u >= a.hdr->units) return;
+  const Unit x = a.units[u];
+  if (!x.own || x.acc < 0) return;
+  const float vs = a.vs ? a.vs[head] : 1.0f;
+  for (int i = threadIdx.x; i < x.rows * quads; i += 256) {
+    const int r = i / quads, c = i % quads;
+    float m = -INFINITY, l = 0.0f;
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    auto add = [&](int64_t row) {
+      const int64_t at = row * a.kv_heads + head;
+      const float2 ml = a.ml[at];
+      if (ml.x == -INFINITY && ml.y == 0.0f) return;  // it has seen no key
+      const f32x4 y = *(const f32x4*)(a.acc + at * a.dim + c * 4);
+      const float top = fmaxf(m, ml.x), f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top),
+                  h = ml.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml.x - top);
+      o = o * f + y * h;
+      l = l * f + ml.y * h;
+      m = top;
+    };
+    for (int s = 0; s < x.splits; ++s) add(x.acc + s * x.rows + r);
+    const int row = x.row0 + r;
+    if (x.group_unit >= 0) {
+      const int tile = (row - x.group_row) / kTileRows;
+      const Unit y = a.units[x.group_unit + tile];
+      for (int s = 0; s < y.splits; ++s) add(y.acc + s * y.rows + row - y.row0);
+    }
+    const float f = l > 0.0f || l != l ? vs / l : 0.0f;
+    const uint32_t token = divide((uint32_t)row, a.share);
+    const int h = head * (int)a.share.d + (int)(row - token * a.share.d);
+    char* p = a.out + token * a.o_tok + h * a.o_head + c * 8;
+    if (FP16) {
+      typedef _Float16 x4 __attribute__((ext_vector_type(4)));
+      *(x4*)p = __builtin_convertvector(o * f, x4);
+    } else {
+      typedef __bf16 x4 __attribute__((ext_vector_type(4)));
+      *(x4*)p = __builtin_convertvector(o * f, x4);
+    }
+    if (a.lse && c == 0)
+      a.lse[(int64_t)token * a.heads + h] =
+          l > 0.0f || l != l ? (m + __log2f(l)) * 0.69314718055994530942f : -INFINITY;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_tables(const TablesArgs& a, hipStream_t st) {
+  tables_scan_kernel<<<dim3(1), dim3(kScanThreads), 0, st>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  // blocks for the tokens; with few new tokens there may be many pages to give back
+  const int per = kFillThreads * kFillTokens;
+  int blocks = (a.num_tokens + per - 1) / per;
+  const int least = a.rows / kFillThreads + 1 < 64 ? a.rows / kFillThreads + 1 : 64;
+  if (blocks < least) blocks = least;
+  tables_fill_kernel<<<dim3(blocks), dim3(kFillThreads), 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_store(const StoreArgs& a, hipStream_t st) {
+  const uint32_t blocks = (uint32_t)(((int64_t)a.tokens * a.chunks.d + 255) / 256);
+  if (a.fp8)
+    store_kernel<true><<<dim3(blocks), dim3(256), 0, st>>>(a);
+  else
+    store_kernel<false><<<dim3(blocks), dim3(256), 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_attend_plan(const AttendArgs& a, hipStream_t st) {
+  plan_kernel<<<dim3(1), dim3(kPlanThreads), 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_attend_join(const AttendArgs& a, bool fp16, hipStream_t st) {
+  const dim3 blocks((uint32_t)a.unit_cap * (uint32_t)a.kv_heads);
+  if (fp16)
+    join_kernel<true><<<blocks, dim3(256), 0, st>>>(a);
+  else
+    join_kernel<false><<<blocks, dim3(256), 0, st>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace kvr
