@@ -98,16 +98,27 @@ __device__ __forceinline__ float half_sum(float x) {
 }
 
 // RW: waves along the rows; the other 4 / RW are along the keys.
+//
+// A 16-bit cache goes from memory to LDS without a register in between.  With
+// RW > 1 there are two buffers for a tile: while one is worked on, the other
+// is filled.  With RW = 1 (a wave has its tile for itself, and memory bounds)
+// there is one: K's half is filled again as soon as the scores are computed,
+// V's when it has been multiplied, so loads are in flight all the time and
+// two workgroups fit a compute unit.  An 8-bit cache is widened on the way,
+// through registers, once for all waves that share the tile.
 template <int D, int RW>
 struct Shape {
   static constexpr int kKeyGroups = 4 / RW;
-  static constexpr int kKeys = RW == 1 ? 32 : 64;   // of a tile
+  static constexpr int kKeys = RW == 4 ? 64 : 32;   // of a tile
+  static constexpr int kBuffers = RW == 1 ? 1 : 2;
   static constexpr int kRowBytes = 2 * D;           // of a tile's row in LDS (always 16-bit elements)
   static constexpr int kTileBytes = kKeys * kRowBytes;
-  static constexpr int kTiles = kKeyGroups * 2 * kTileBytes;
+  static constexpr int kTiles = kKeyGroups * kBuffers * 2 * kTileBytes;
   // the join of the key groups at the end: maxima and sums, and results
   static constexpr int kJoin = kKeyGroups == 1 ? 0 : kKeyGroups * RW * 32 * (8 + 4 * D);
-  static constexpr int kBytes = (kTiles > kJoin ? kTiles : kJoin) + 64;  // + flags
+  static constexpr int kMain = kTiles > kJoin ? kTiles : kJoin;
+  static constexpr int kPages = RW == 1 ? 4 * 2 * 256 : 0;  // page numbers of a wave's next two tiles
+  static constexpr int kBytes = kMain + kPages + 64;        // + flags
 };
 
 template <int D>
@@ -118,50 +129,93 @@ constexpr int attend_lds() {
   return n;
 }
 
-// A lane's share of a tile on its way from memory to LDS: NI 16-byte chunks of
-// K and of V, at rows i * (threads / chunks of a row) + thread / chunks.
-template <int D, class T, bool FP8, int RW>
-struct Loader {
+// What a lane reads in the place of a row behind the last key, and of a row
+// whose page number is none.
+__device__ const uint32_t kNoRow[4] = {0, 0, 0, 0};
+__device__ const uint32_t kBadRow[4] = {~0u, ~0u, ~0u, ~0u};  // NaN in every type
+
+// Loads from memory straight to LDS: lane i's 16 (4) bytes to `to` + 16 i
+// (4 i), `to` the same in all lanes.  The compiler does not see these loads:
+// wait_loads<n> waits until at most n of them are in flight.  (M0 may not be
+// read in the cycle after it is written.)
+__device__ __forceinline__ uint32_t lds_offset(const void* p) {
+  return (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(lds_char*)p);
+}
+__device__ __forceinline__ void load16_to_lds(const void* from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
+}
+__device__ __forceinline__ void load4_to_lds(const void* from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(to) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+// every read of LDS by this wave has been answered
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+// a barrier that does not wait for loads in flight
+__device__ __forceinline__ void barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// A lane's share of a tile of a 16-bit cache on its way to LDS: kN times 16
+// bytes of K and of V.  Load i of a wave fills 1,024 neighbouring bytes, so a
+// lane reads the chunk that belongs where it writes.
+template <int D, int RW>
+struct Direct {
+  typedef Shape<D, RW> S;
+  static constexpr int kChunks = D / 8;             // of a row
+  static constexpr int kRows = 64 / kChunks;        // of one load of a wave
+  static constexpr int kN = S::kKeys / (kRows * RW);
+  static_assert(kN * kRows * RW == S::kKeys, "tile shape");
+
+  // rows i * RW * kRows + first of the tile, i < kN
+  static __device__ __forceinline__ int first(int wave, int lane) { return wave * kRows + lane / kChunks; }
+
+  template <bool KEYS>
+  static __device__ __forceinline__ void load(const AttendArgs& a, const char* base, const int (&page)[kN], int key0,
+                                              int end, int wave, int lane, uint32_t to) {
+    const int mask = (1 << a.page_shift) - 1;
+    const int64_t page_bytes = KEYS ? a.kc_page : a.vc_page, slot_bytes = KEYS ? a.kc_slot : a.vc_slot;
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const int row = i * RW * kRows + first(wave, lane), key = key0 + row;
+      const int ch = (lane % kChunks) ^ (KEYS ? swizzle_k<D>(row) : swizzle_v<D>(row));
+      const char* p = base + page[i] * page_bytes + (key & mask) * slot_bytes + ch * 16;
+      if (key >= end) p = (const char*)kNoRow;
+      else if ((uint32_t)page[i] >= (uint32_t)a.num_pages) p = (const char*)kBadRow;
+      load16_to_lds(p, to + (i * RW + wave) * 1024);
+    }
+  }
+};
+
+// A lane's share of a tile of an 8-bit cache: kN 16-byte chunks of K and of V
+// in registers, at rows i * (threads / chunks of a row) + thread / chunks.
+template <int D, class T, int RW>
+struct Widened {
   typedef Shape<D, RW> S;
   static constexpr int kThreads = 64 * RW;
-  static constexpr int kChunks = FP8 ? D / 16 : D / 8;  // of a row in the cache
+  static constexpr int kChunks = D / 16;  // of a row in the cache
   static constexpr int kRows = kThreads / kChunks;
   static constexpr int kN = S::kKeys / kRows;
   static_assert(kThreads % kChunks == 0 && S::kKeys % kRows == 0, "tile shape");
 
   i32x4 k[kN], v[kN];
-  int page[kN];  // of the tile that is fetched next; -1: behind the last key
 
-  // The tile's page numbers: keys key0.. of a table's row, `end` keys in all.
-  __device__ __forceinline__ void pages(const AttendArgs& a, const int32_t* table, int key0, int end, int thread) {
-#pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      const int key = key0 + i * kRows + thread / kChunks;
-      page[i] = key < end ? table[key >> a.page_shift] : -1;
-    }
-  }
-
-  __device__ __forceinline__ void fetch(const AttendArgs& a, const char* kc, const char* vc, int key0, int end,
-                                        int thread) {
+  __device__ __forceinline__ void fetch(const AttendArgs& a, const char* kc, const char* vc, const int (&page)[kN],
+                                        int key0, int end, int thread) {
     const int mask = (1 << a.page_shift) - 1;
-    const int64_t at = (int64_t)(thread % kChunks) * 16;
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       const int key = key0 + i * kRows + thread / kChunks;
-      const i32x4 zero = {0, 0, 0, 0};
-      k[i] = zero;
-      v[i] = zero;
-      if (key < end) {
-        if ((uint32_t)page[i] < (uint32_t)a.num_pages) {
-          k[i] = *(const i32x4*)(kc + page[i] * a.kc_page + (key & mask) * a.kc_slot + at);
-          v[i] = *(const i32x4*)(vc + page[i] * a.vc_page + (key & mask) * a.vc_slot + at);
-        } else {  // no such page: the result is NaN
-          const i32x4 nan = {-1, -1, -1, -1};
-          k[i] = nan;
-          v[i] = nan;
-          if (a.status) atomicOr(a.status, (uint32_t)KVR_DEV_BAD_PAGE);
-        }
-      }
+      const char* pk = kc + page[i] * a.kc_page + (key & mask) * a.kc_slot + thread % kChunks * 16;
+      const char* pv = vc + page[i] * a.vc_page + (key & mask) * a.vc_slot + thread % kChunks * 16;
+      if (key >= end)
+        pk = pv = (const char*)kNoRow;
+      else if ((uint32_t)page[i] >= (uint32_t)a.num_pages)
+        pk = pv = (const char*)kBadRow;
+      k[i] = *(const i32x4*)pk;
+      v[i] = *(const i32x4*)pv;
     }
   }
 
@@ -170,41 +224,20 @@ struct Loader {
     hi = i32x4{T::from_fp8_lo(x[2]), T::from_fp8_hi(x[2]), T::from_fp8_lo(x[3]), T::from_fp8_hi(x[3])};
   }
 
-  // whether one of the 8 16-bit values is infinite or NaN
-  static __device__ __forceinline__ bool odd(i32x4 x) {
-    bool b = false;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      b |= (x[j] & T::kExponent) == T::kExponent;
-      b |= ((x[j] >> 16) & T::kExponent) == T::kExponent;
-    }
-    return b;
-  }
-
-  // Writes the tile to LDS; with `look`, whether V has an infinity or NaN here.
-  __device__ __forceinline__ bool store(char* kt, char* vt, int thread, bool look) {
-    bool bad = false;
+  __device__ __forceinline__ void store(char* kt, char* vt, int thread) {
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       const int row = i * kRows + thread / kChunks, ch = thread % kChunks;
       char* kr = kt + row * S::kRowBytes;
       char* vr = vt + row * S::kRowBytes;
-      if constexpr (FP8) {
-        i32x4 lo, hi;
-        widen(k[i], lo, hi);
-        *(i32x4*)(kr + (((2 * ch) ^ swizzle_k<D>(row)) << 4)) = lo;
-        *(i32x4*)(kr + (((2 * ch + 1) ^ swizzle_k<D>(row)) << 4)) = hi;
-        widen(v[i], lo, hi);
-        *(i32x4*)(vr + (((2 * ch) ^ swizzle_v<D>(row)) << 4)) = lo;
-        *(i32x4*)(vr + (((2 * ch + 1) ^ swizzle_v<D>(row)) << 4)) = hi;
-        if (look) bad |= odd(lo) | odd(hi);
-      } else {
-        *(i32x4*)(kr + ((ch ^ swizzle_k<D>(row)) << 4)) = k[i];
-        *(i32x4*)(vr + ((ch ^ swizzle_v<D>(row)) << 4)) = v[i];
-        if (look) bad |= odd(v[i]);
-      }
+      i32x4 lo, hi;
+      widen(k[i], lo, hi);
+      *(i32x4*)(kr + (((2 * ch) ^ swizzle_k<D>(row)) << 4)) = lo;
+      *(i32x4*)(kr + (((2 * ch + 1) ^ swizzle_k<D>(row)) << 4)) = hi;
+      widen(v[i], lo, hi);
+      *(i32x4*)(vr + (((2 * ch) ^ swizzle_v<D>(row)) << 4)) = lo;
+      *(i32x4*)(vr + (((2 * ch + 1) ^ swizzle_v<D>(row)) << 4)) = hi;
     }
-    return bad;
   }
 };
 
@@ -214,86 +247,16 @@ __device__ __forceinline__ s16x4 round4(float a, float b, float c, float d) {
   return __builtin_bit_cast(s16x4, __builtin_convertvector(x, typename T::x4));
 }
 
-template <int D, class T, bool FP8, int RW>
-__device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it, int head, char* lds) {
-  typedef Shape<D, RW> S;
-  constexpr int KG = S::kKeyGroups, KT = S::kKeys, KB = KT / 32, DB = D / 32;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int rw = wave % RW, kg = wave / RW, thread = tid % (64 * RW);
-  const int n = lane & 31, hh = lane >> 5;
-  char* kt = lds + kg * 2 * S::kTileBytes;
-  char* vt = kt + S::kTileBytes;
-  int* flags = (int*)(lds + (S::kTiles > S::kJoin ? S::kTiles : S::kJoin));
-
-  // the lane's row: its token, head and query
-  const int r = rw * 32 + n;
-  const bool live = r < it.rows;
-  const uint32_t row = (uint32_t)(it.row0 + (live ? r : 0));
-  const uint32_t token = divide(row, a.share);
-  const int qhead = head * (int)a.share.d + (int)(row - token * a.share.d);
+// A wave's 32 rows: queries, running maximum (log2 units) and sum, results.
+template <int D, class T>
+struct Rows {
   s16x8 q[D / 16];
-  {
-    const char* p = a.q + token * a.q_tok + qhead * a.q_head + hh * 16;
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) q[i] = *(const s16x8*)(p + i * 32);
-  }
-  const int limit = (int)token + it.limit;                             // own keys that this row sees
-  const int limit0 = (int)divide((uint32_t)it.row0, a.share) + it.limit;  // ... and the first row
+  f32x16 o[D / 32];
+  float m, l;
 
-  const char* kc = a.kc + head * a.kc_head;
-  const char* vc = a.vc + head * a.vc_head;
-  const int32_t* own_table = a.table + it.request * a.table_stride;
-  const int32_t* prefix_table = it.prefix_steps ? a.prefix_table + it.prefix * a.prefix_stride : nullptr;
-
-  f32x16 o[DB];
-#pragma unroll
-  for (int b = 0; b < DB; ++b)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) o[b][i] = 0.0f;
-  float m = -INFINITY, l = 0.0f;
-
-  const int tiles = (it.step1 - it.step0) * (kStepKeys / KT);
-  const int rounds = (tiles + KG - 1) / KG;
-  Loader<D, T, FP8, RW> ld;
-  // tile t of the item: its first key, the end of its keys, and the table they come from
-  auto place = [&](int t, int& key0, int& end, const int32_t*& table) {
-    const int step = it.step0 + t / (kStepKeys / KT), part = t % (kStepKeys / KT);
-    const bool shared = step < it.prefix_steps;
-    key0 = (shared ? step : step - it.prefix_steps) * kStepKeys + part * KT;
-    end = t >= tiles ? 0 : shared ? it.prefix_len : it.own_end;
-    table = shared ? prefix_table : own_table;
-    return shared;
-  };
-  int key0 = 0, end = 0, key1 = 0, end1 = 0;
-  const int32_t* table;
-  bool shared = place(kg, key0, end, table);
-  ld.pages(a, table, key0, end, thread);
-  ld.fetch(a, kc, vc, key0, end, thread);
-  bool shared1 = place(KG + kg, key1, end1, table);
-  ld.pages(a, table, key1, end1, thread);
-  if (tid < 2 * KG) flags[tid] = 0;
-
-  for (int round = 0; round < rounds; ++round) {
-    // a row of this tile may stand before some of its own keys
-    const bool edge = !shared && key0 + KT > limit0;
-    __syncthreads();
-    const bool bad = ld.store(kt, vt, thread, edge);
-    if (edge && __any(bad) && lane == 0) flags[(round & 1) * KG + kg] = 1;
-    __syncthreads();
-    const bool odd = edge && flags[(round & 1) * KG + kg];
-    if (tid < KG) flags[((round + 1) & 1) * KG + tid] = 0;
-    const int k0 = key0, e0 = end;
-    const bool sh0 = shared;
-    // the next tile is on its way while this one is worked on
-    key0 = key1;
-    end = end1;
-    shared = shared1;
-    ld.fetch(a, kc, vc, key0, end, thread);
-    shared1 = place((round + 2) * KG + kg, key1, end1, table);
-    ld.pages(a, table, key1, end1, thread);
-    if (k0 >= e0) continue;
-
-    f32x16 s[KB];
+  // Scores of KB * 32 keys in LDS.
+  template <int KB>
+  __device__ __forceinline__ void scores(const char* kt, f32x16 (&s)[KB], int n, int hh) {
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
 #pragma unroll
@@ -301,12 +264,16 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
       const int kr = b * 32 + n;
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) {
-        const s16x8 x = *(const s16x8*)(kt + kr * S::kRowBytes + (((2 * i + hh) ^ swizzle_k<D>(kr)) << 4));
+        const s16x8 x = *(const s16x8*)(kt + kr * 2 * D + (((2 * i + hh) ^ swizzle_k<D>(kr)) << 4));
         s[b] = T::mfma(x, q[i], s[b]);
       }
     }
-    const int seen = (sh0 ? e0 : min(limit, e0)) - k0;  // keys of this tile that the row sees
-    if (edge || k0 + KT > e0) {
+  }
+
+  // Scores to p; keys from `seen` on are hidden where `edge` says that there are such.
+  template <int KB>
+  __device__ __forceinline__ void softmax(f32x16 (&s)[KB], bool edge, int seen, float scale, int hh) {
+    if (edge) {
 #pragma unroll
       for (int b = 0; b < KB; ++b)
 #pragma unroll
@@ -318,7 +285,7 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
     for (int b = 0; b < KB; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-    top = half_max(top) * a.scale_log2;
+    top = half_max(top) * scale;
     if (__any(top > m)) {
       const float next = fmaxf(m, top);
       // before the first key of a row: nothing to scale
@@ -326,7 +293,7 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
       m = next;
       l *= f;
 #pragma unroll
-      for (int b = 0; b < DB; ++b)
+      for (int b = 0; b < D / 32; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[b][i] *= f;
     }
@@ -336,57 +303,24 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
     for (int b = 0; b < KB; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], a.scale_log2, -base));
+        s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], scale, -base));
         l += s[b][i];
       }
+  }
 
-    if (__builtin_expect(odd, 0)) {
-      // V holds an infinity or NaN and some rows do not see all keys: 0 * inf
-      // must not reach them, so the products are taken key by key
-#pragma unroll
-      for (int b = 0; b < KB; ++b)
-#pragma unroll 1
-        for (int i = 0; i < 16; ++i) {
-          float x = s[b][0];  // s[b][i]
-#pragma unroll
-          for (int j = 1; j < 16; ++j) x = i == j ? s[b][j] : x;
-          const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int key = b * 32 + 8 * (i >> 2) + 4 * h + (i & 3);
-            const float p = __uint_as_float(w[h]);
-            const char* vr = vt + key * S::kRowBytes + hh * 8;
-            int sw = swizzle_v<D>(key) << 4;
-            asm("" : "+v"(sw));  // (folded into the unrolled addresses, it keeps the compiler busy without end)
-#pragma unroll
-            for (int c = 0; c < DB; ++c)
-#pragma unroll
-              for (int g = 0; g < 4; ++g) {
-                const int ch = c * 4 + g;  // 8 elements: this half's four
-                const s16x4 x4 = *(const s16x4*)(vr + ((ch << 4) ^ sw));
-                const auto y = __builtin_convertvector(__builtin_bit_cast(typename T::x4, x4), f32x4);
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  if (key < seen) o[c][g * 4 + e] = __builtin_fmaf(p, y[e], o[c][g * 4 + e]);
-              }
-          }
-        }
-      continue;
-    }
-
-    const int sl = lane & 15, dh = (lane >> 4) & 1;
+  // O^T += V^T P^T
+  template <int KB>
+  __device__ __forceinline__ void values(const char* vt, const f32x16 (&s)[KB], int lane) {
+    const int hh = lane >> 5, sl = lane & 15, dh = (lane >> 4) & 1;
 #pragma unroll
     for (int b = 0; b < KB; ++b)
 #pragma unroll
       for (int st = 0; st < 2; ++st) {
-        s16x8 p;
-        {
-          const s16x4 lo = round4<T>(s[b][8 * st], s[b][8 * st + 1], s[b][8 * st + 2], s[b][8 * st + 3]);
-          const s16x4 hi = round4<T>(s[b][8 * st + 4], s[b][8 * st + 5], s[b][8 * st + 6], s[b][8 * st + 7]);
-          p = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        }
+        const s16x4 lo = round4<T>(s[b][8 * st], s[b][8 * st + 1], s[b][8 * st + 2], s[b][8 * st + 3]);
+        const s16x4 hi = round4<T>(s[b][8 * st + 4], s[b][8 * st + 5], s[b][8 * st + 6], s[b][8 * st + 7]);
+        const s16x8 p = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-        for (int c = 0; c < DB; ++c) {
+        for (int c = 0; c < D / 32; ++c) {
           s16x4 x[2];
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
@@ -394,7 +328,7 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
             // lanes a row, and lane i of them gets column i
             const int vr = b * 32 + st * 16 + j * 8 + hh * 4 + sl / 4;
             const int ch = c * 4 + dh * 2 + (sl & 3) / 2;
-            const char* p8 = vt + vr * S::kRowBytes + ((ch ^ swizzle_v<D>(vr)) << 4) + (sl & 1) * 8;
+            const char* p8 = vt + vr * 2 * D + ((ch ^ swizzle_v<D>(vr)) << 4) + (sl & 1) * 8;
             x[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                 (__attribute__((address_space(3))) s16x4*)(lds_char*)p8);
           }
@@ -402,19 +336,300 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
         }
       }
   }
-  l = half_sum(l);
 
+  // The same key by key, for a tile whose V holds an infinity or NaN that some
+  // rows do not see: 0 * inf must not reach them.
+  template <int KB>
+  __device__ __forceinline__ void values_seen(const char* vt, const f32x16 (&s)[KB], int seen, int hh) {
+#pragma unroll
+    for (int b = 0; b < KB; ++b)
+#pragma unroll 1
+      for (int i = 0; i < 16; ++i) {
+        float x = s[b][0];  // s[b][i]
+#pragma unroll
+        for (int j = 1; j < 16; ++j) x = i == j ? s[b][j] : x;
+        const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int key = b * 32 + 8 * (i >> 2) + 4 * h + (i & 3);
+          const float p = __uint_as_float(w[h]);
+          const char* vr = vt + key * 2 * D + hh * 8;
+          int sw = swizzle_v<D>(key) << 4;
+          asm("" : "+v"(sw));  // (folded into the unrolled addresses, it keeps the compiler busy without end)
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              const int ch = c * 4 + g;  // 8 elements: this half's four
+              const s16x4 x4 = *(const s16x4*)(vr + ((ch << 4) ^ sw));
+              const auto y = __builtin_convertvector(__builtin_bit_cast(typename T::x4, x4), f32x4);
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (key < seen) o[c][g * 4 + e] = __builtin_fmaf(p, y[e], o[c][g * 4 + e]);
+            }
+        }
+      }
+  }
+};
+
+// Whether a tile of `bytes` bytes in LDS holds an infinity or NaN, by one wave.
+template <class T, int BYTES>
+__device__ __forceinline__ bool holds_odd(const char* tile, int lane) {
+  bool odd = false;
+#pragma unroll 4
+  for (int i = lane * 16; i < BYTES; i += 1024) {
+    const i32x4 x = *(const i32x4*)(tile + i);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      odd |= (x[j] & T::kExponent) == T::kExponent;
+      odd |= ((x[j] >> 16) & T::kExponent) == T::kExponent;
+    }
+  }
+  return __any(odd);
+}
+
+template <int D, class T, bool FP8, int RW>
+__device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it, int head, float scale, char* lds) {
+  typedef Shape<D, RW> S;
+  constexpr int KG = S::kKeyGroups, KT = S::kKeys, KB = KT / 32, DB = D / 32;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rw = wave % RW, kg = wave / RW, thread = tid % (64 * RW);
+  const int n = lane & 31, hh = lane >> 5;
+
+  // the lane's row: its token, head and query
+  const int r = rw * 32 + n;
+  const bool live = r < it.rows;
+  const uint32_t row = (uint32_t)(it.row0 + (live ? r : 0));
+  const uint32_t token = divide(row, a.share);
+  const int qhead = head * (int)a.share.d + (int)(row - token * a.share.d);
+  Rows<D, T> x;
+  {
+    const char* p = a.q + token * a.q_tok + qhead * a.q_head + hh * 16;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) x.q[i] = *(const s16x8*)(p + i * 32);
+  }
+#pragma unroll
+  for (int b = 0; b < DB; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x.o[b][i] = 0.0f;
+  x.m = -INFINITY;
+  x.l = 0.0f;
+  const int limit = (int)token + it.limit;                                // own keys that this row sees
+  const int limit0 = (int)divide((uint32_t)it.row0, a.share) + it.limit;  // ... and the first row
+
+  const char* kc = a.kc + head * a.kc_head;
+  const char* vc = a.vc + head * a.vc_head;
+  const int32_t* own_table = a.table + it.request * a.table_stride;
+  const int32_t* prefix_table = it.prefix_steps ? a.prefix_table + it.prefix * a.prefix_stride : nullptr;
+  const int tiles = (it.step1 - it.step0) * (kStepKeys / KT);
+
+  // tile t of the item: its first key, the end of its keys, their table, and
+  // whether it is the prefix's
+  struct Place {
+    int key0, end;
+    const int32_t* table;
+    bool shared;
+  };
+  auto place = [&](int t) {
+    const int step = it.step0 + t / (kStepKeys / KT), part = t % (kStepKeys / KT);
+    Place p;
+    p.shared = step < it.prefix_steps;
+    p.key0 = (p.shared ? step : step - it.prefix_steps) * kStepKeys + part * KT;
+    p.end = t >= tiles ? 0 : p.shared ? it.prefix_len : it.own_end;
+    p.table = p.shared ? prefix_table : own_table;
+    return p;
+  };
+  // page numbers of rows row0 + i * step (i < N) of a tile
+  auto pages = [&](const Place& p, int row0, int step, auto& page) {
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(page) / sizeof(int)); ++i) {
+      const int key = p.key0 + row0 + i * step;
+      page[i] = key < p.end ? p.table[key >> a.page_shift] : 0;
+    }
+  };
+  auto check_pages = [&](const Place& p, int row0, int step, const auto& page) {
+    if (!a.status) return;
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(page) / sizeof(int)); ++i)
+      bad |= p.key0 + row0 + i * step < p.end && (uint32_t)page[i] >= (uint32_t)a.num_pages;
+    if (bad) atomicOr(a.status, (uint32_t)KVR_DEV_BAD_PAGE);
+  };
+  // the scores of a tile, p, and their product with V
+  auto seen_of = [&](const Place& p) { return (p.shared ? p.end : min(limit, p.end)) - p.key0; };
+  // a row of this tile may stand before some of its own keys
+  auto edge_of = [&](const Place& p) { return !p.shared && p.key0 + KT > limit0; };
+
+  if constexpr (RW == 1 && !FP8) {
+    typedef Direct<D, 1> L;
+    constexpr int N = L::kN;
+    char* kt = lds + wave * 2 * S::kTileBytes;
+    char* vt = kt + S::kTileBytes;
+    int* ids = (int*)(lds + S::kMain) + wave * 128;
+    const uint32_t k_to = lds_offset(kt), v_to = lds_offset(vt), id_to = lds_offset(ids);
+    const int mine = (tiles - wave + 3) / 4;  // tiles wave, wave + 4, ..
+    auto load_ids = [&](int j) {
+      const Place p = place(wave + 4 * j);
+      const int key = min(p.key0 + n, p.end - 1);
+      load4_to_lds(p.table + (key >> a.page_shift), id_to + (j & 1) * 256);
+    };
+    int page[N];
+    auto read_ids = [&](int j) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) page[i] = ids[(j & 1) * 64 + i * L::kRows + L::first(0, lane)];
+    };
+    if (mine > 0) {
+      Place p = place(wave);
+      load_ids(0);
+      wait_loads<0>();
+      read_ids(0);
+      L::template load<true>(a, kc, page, p.key0, p.end, 0, lane, k_to);
+      if (mine > 1) load_ids(1);
+      L::template load<false>(a, vc, page, p.key0, p.end, 0, lane, v_to);
+      for (int j = 0; j < mine; ++j) {
+        // in flight, oldest first: K of this tile, the next one's page numbers, V of this tile
+        const bool more = j + 1 < mine;
+        const Place p1 = place(wave + 4 * (j + 1));
+        check_pages(p, L::first(0, lane), L::kRows, page);
+        wait_loads<N>();
+        if (more) read_ids(j + 1);
+        f32x16 s[KB];
+        x.scores(kt, s, n, hh);
+        wait_lds();
+        if (more) {
+          L::template load<true>(a, kc, page, p1.key0, p1.end, 0, lane, k_to);
+          if (j + 2 < mine) load_ids(j + 2);
+        }
+        const bool edge = edge_of(p);
+        const int seen = seen_of(p);
+        x.softmax(s, edge || p.key0 + KT > p.end, seen, scale, hh);
+        if (j + 2 < mine)
+          wait_loads<N + 1>();
+        else if (more)
+          wait_loads<N>();
+        else
+          wait_loads<0>();
+        if (edge && holds_odd<T, S::kTileBytes>(vt, lane))
+          x.values_seen(vt, s, seen, hh);
+        else
+          x.values(vt, s, lane);
+        wait_lds();
+        if (more) L::template load<false>(a, vc, page, p1.key0, p1.end, 0, lane, v_to);
+        p = p1;
+      }
+    }
+  } else if constexpr (RW == 1) {
+    typedef Widened<D, T, 1> L;
+    char* kt = lds + wave * 2 * S::kTileBytes;
+    char* vt = kt + S::kTileBytes;
+    const int mine = (tiles - wave + 3) / 4;
+    int page[L::kN];
+    L ld;
+    const int row0 = lane / L::kChunks;
+    Place p = place(wave), p1 = place(wave + 4);
+    pages(p, row0, L::kRows, page);
+    ld.fetch(a, kc, vc, page, p.key0, p.end, lane);
+    check_pages(p, row0, L::kRows, page);
+    pages(p1, row0, L::kRows, page);
+    for (int j = 0; j < mine; ++j) {
+      ld.store(kt, vt, lane);
+      ld.fetch(a, kc, vc, page, p1.key0, p1.end, lane);
+      check_pages(p1, row0, L::kRows, page);
+      const Place p2 = place(wave + 4 * (j + 2));
+      pages(p2, row0, L::kRows, page);
+      f32x16 s[KB];
+      x.scores(kt, s, n, hh);
+      const bool edge = edge_of(p);
+      const int seen = seen_of(p);
+      x.softmax(s, edge || p.key0 + KT > p.end, seen, scale, hh);
+      if (edge && holds_odd<T, S::kTileBytes>(vt, lane))
+        x.values_seen(vt, s, seen, hh);
+      else
+        x.values(vt, s, lane);
+      p = p1;
+      p1 = p2;
+    }
+  } else {
+    // two buffers; one barrier a tile
+    char* group = lds + kg * 4 * S::kTileBytes;
+    const int rounds = (tiles + KG - 1) / KG;
+    Place p = place(kg), p1 = place(KG + kg);
+    auto work = [&](const char* kt, const char* vt) {
+      if (p.key0 >= p.end) return;
+      f32x16 s[KB];
+      x.scores(kt, s, n, hh);
+      const bool edge = edge_of(p);
+      const int seen = seen_of(p);
+      x.softmax(s, edge || p.key0 + KT > p.end, seen, scale, hh);
+      if (edge && holds_odd<T, S::kTileBytes>(vt, lane))
+        x.values_seen(vt, s, seen, hh);
+      else
+        x.values(vt, s, lane);
+    };
+    if constexpr (!FP8) {
+      typedef Direct<D, RW> L;
+      int page[L::kN];
+      const int row0 = L::first(rw, lane), step = RW * L::kRows;
+      const uint32_t to = lds_offset(group);
+      pages(p, row0, step, page);
+      L::template load<true>(a, kc, page, p.key0, p.end, rw, lane, to);
+      L::template load<false>(a, vc, page, p.key0, p.end, rw, lane, to + S::kTileBytes);
+      check_pages(p, row0, step, page);
+      pages(p1, row0, step, page);
+      for (int round = 0; round < rounds; ++round) {
+        wait_loads<0>();
+        barrier();
+        const uint32_t b1 = (round + 1 & 1) * 2 * S::kTileBytes;
+        const char* kt = group + (round & 1) * 2 * S::kTileBytes;
+        const Place p2 = place((round + 2) * KG + kg);
+        if (round + 1 < rounds) {
+          L::template load<true>(a, kc, page, p1.key0, p1.end, rw, lane, to + b1);
+          L::template load<false>(a, vc, page, p1.key0, p1.end, rw, lane, to + b1 + S::kTileBytes);
+          check_pages(p1, row0, step, page);
+          pages(p2, row0, step, page);
+        }
+        work(kt, kt + S::kTileBytes);
+        p = p1;
+        p1 = p2;
+      }
+    } else {
+      typedef Widened<D, T, RW> L;
+      int page[L::kN];
+      L ld;
+      const int row0 = thread / L::kChunks;
+      pages(p, row0, L::kRows, page);
+      ld.fetch(a, kc, vc, page, p.key0, p.end, thread);
+      check_pages(p, row0, L::kRows, page);
+      pages(p1, row0, L::kRows, page);
+      ld.store(group, group + S::kTileBytes, thread);
+      for (int round = 0; round < rounds; ++round) {
+        barrier();
+        char* kt = group + (round & 1) * 2 * S::kTileBytes;
+        char* kt1 = group + (round + 1 & 1) * 2 * S::kTileBytes;
+        const Place p2 = place((round + 2) * KG + kg);
+        ld.fetch(a, kc, vc, page, p1.key0, p1.end, thread);
+        check_pages(p1, row0, L::kRows, page);
+        pages(p2, row0, L::kRows, page);
+        work(kt, kt + S::kTileBytes);
+        ld.store(kt1, kt1 + S::kTileBytes, thread);
+        p = p1;
+        p1 = p2;
+      }
+    }
+  }
+  const float m = x.m, l = half_sum(x.l);
+  auto& o = x.o;
   const float vs = a.vs ? a.vs[head] : 1.0f;
   // four consecutive results of a row: the final ones, or the partial ones
-  auto emit = [&](int rr, int d, f32x4 x, float ll) {
+  auto emit = [&](int rr, int d, f32x4 y, float ll) {
     const uint32_t R = (uint32_t)(it.row0 + rr);
     if (it.acc < 0) {
       const float f = ll > 0.0f || ll != ll ? vs / ll : 0.0f;
       const uint32_t tk = divide(R, a.share);
       const int hd = head * (int)a.share.d + (int)(R - tk * a.share.d);
-      *(s16x4*)(a.out + tk * a.o_tok + hd * a.o_head + d * 2) = round4<T>(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
+      *(s16x4*)(a.out + tk * a.o_tok + hd * a.o_head + d * 2) = round4<T>(y[0] * f, y[1] * f, y[2] * f, y[3] * f);
     } else {
-      *(f32x4*)(a.acc + ((int64_t)(it.acc + rr) * a.kv_heads + head) * D + d) = x;
+      *(f32x4*)(a.acc + ((int64_t)(it.acc + rr) * a.kv_heads + head) * D + d) = y;
     }
   };
   auto emit_ml = [&](int rr, float mm, float ll) {
@@ -469,14 +684,14 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
       float mm = -INFINITY, ll = 0.0f;
 #pragma unroll
       for (int g = 0; g < KG; ++g) mm = fmaxf(mm, jm[g * ROWS + rr]);
-      f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+      f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int g = 0; g < KG; ++g) {
         const float mg = jm[g * ROWS + rr];
         if (mg != -INFINITY) ll += jl[g * ROWS + rr] * __builtin_amdgcn_exp2f(mg - mm);
-        x += *(const f32x4*)(jo + (g * ROWS + rr) * D + (c ^ (rr & 15)) * 4);
+        y += *(const f32x4*)(jo + (g * ROWS + rr) * D + (c ^ (rr & 15)) * 4);
       }
-      emit(rr, c * 4, x, ll);
+      emit(rr, c * 4, y, ll);
       if (c == 0) emit_ml(rr, mm, ll);
     }
   }
@@ -488,14 +703,13 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(AttendArg
   const int item = blockIdx.x / a.kv_heads, head = blockIdx.x % a.kv_heads;
   if (item >= a.hdr->items) return;
   const Item it = a.items[item];
-  AttendArgs b = a;
-  if (FP8 && a.ks) b.scale_log2 *= a.ks[head];
+  const float scale = FP8 && a.ks ? a.scale_log2 * a.ks[head] : a.scale_log2;
   if (it.rows > 64)
-    attend_item<D, T, FP8, 4>(b, it, head, lds);
+    attend_item<D, T, FP8, 4>(a, it, head, scale, lds);
   else if (it.rows > 32)
-    attend_item<D, T, FP8, 2>(b, it, head, lds);
+    attend_item<D, T, FP8, 2>(a, it, head, scale, lds);
   else
-    attend_item<D, T, FP8, 1>(b, it, head, lds);
+    attend_item<D, T, FP8, 1>(a, it, head, scale, lds);
 }
 
 template <int D, class T, bool FP8>
