@@ -311,7 +311,8 @@ void kvr_destroy(kvr_ctx* ctx);
  * allocate nothing, copy nothing to the host and do not synchronise, so they
  * may be captured into a graph.  Every struct begins with struct_size =
  * sizeof(the struct).  Strides count elements; the elements of a head are
- * neighbours, and every head of every token starts on a 16-byte boundary.
+ * neighbours, every head of every token starts on a 16-byte boundary, and a
+ * page or token of the cache is below 2^31 bytes from the next.
  * What only the device can see (lengths, page numbers) is checked there, as
  * stated at each operator, and or-ed into a status word (KVR_DEV_*).
  * ------------------------------------------------------------------------ */

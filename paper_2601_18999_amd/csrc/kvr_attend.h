@@ -19,9 +19,9 @@
 // that the sum over keys does not care about.  V^T comes out of LDS by the
 // transposing reads.
 //
-// Four waves share the rows and the keys: with more than 64 rows each wave
-// has 32 rows and all share a tile of 64 keys; with fewer rows the waves take
-// different tiles of keys and are joined in LDS at the end.
+// With more than 32 rows each of the four waves has 32 rows (or none) and all
+// share a tile of 64 keys; with fewer rows the waves take different tiles of
+// 32 keys and are joined in LDS at the end.
 //
 // Scores, maxima, sums and accumulators are 32-bit.  p is rounded to the
 // queries' type for the second product (the matrix instructions take 16-bit
@@ -41,6 +41,9 @@ typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) char lds_char;
+typedef const __attribute__((address_space(1))) int32_t* global_ints;
+typedef const __attribute__((address_space(1))) char* global_bytes;
+typedef const __attribute__((address_space(1))) i32x4* global_chunk;
 
 struct Bf16 {
   typedef __bf16 x2 __attribute__((ext_vector_type(2)));
@@ -97,6 +100,11 @@ __device__ __forceinline__ float half_sum(float x) {
   return __uint_as_float(s[0]) + __uint_as_float(s[1]);
 }
 
+// The largest of three, or NaN (one instruction; fmaxf's rule for NaN takes two more).
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
+}
+
 // RW: waves along the rows; the other 4 / RW are along the keys.
 //
 // A 16-bit cache goes from memory to LDS without a register in between.  With
@@ -109,7 +117,7 @@ __device__ __forceinline__ float half_sum(float x) {
 template <int D, int RW>
 struct Shape {
   static constexpr int kKeyGroups = 4 / RW;
-  static constexpr int kKeys = RW == 4 ? 64 : 32;   // of a tile
+  static constexpr int kKeys = RW == 4 ? 64 : 32;  // of a tile
   static constexpr int kBuffers = RW == 1 ? 1 : 2;
   static constexpr int kRowBytes = 2 * D;           // of a tile's row in LDS (always 16-bit elements)
   static constexpr int kTileBytes = kKeys * kRowBytes;
@@ -123,10 +131,7 @@ struct Shape {
 
 template <int D>
 constexpr int attend_lds() {
-  int n = Shape<D, 1>::kBytes;
-  if (Shape<D, 2>::kBytes > n) n = Shape<D, 2>::kBytes;
-  if (Shape<D, 4>::kBytes > n) n = Shape<D, 4>::kBytes;
-  return n;
+  return Shape<D, 1>::kBytes > Shape<D, 4>::kBytes ? Shape<D, 1>::kBytes : Shape<D, 4>::kBytes;
 }
 
 // What a lane reads in the place of a row behind the last key, and of a row
@@ -141,10 +146,10 @@ __device__ const uint32_t kBadRow[4] = {~0u, ~0u, ~0u, ~0u};  // NaN in every ty
 __device__ __forceinline__ uint32_t lds_offset(const void* p) {
   return (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(lds_char*)p);
 }
-__device__ __forceinline__ void load16_to_lds(const void* from, uint32_t to) {
+__device__ __forceinline__ void load16_to_lds(global_bytes from, uint32_t to) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
 }
-__device__ __forceinline__ void load4_to_lds(const void* from, uint32_t to) {
+__device__ __forceinline__ void load4_to_lds(global_ints from, uint32_t to) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(to) : "memory");
 }
 template <int N>
@@ -156,6 +161,12 @@ __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)"
 // a barrier that does not wait for loads in flight
 __device__ __forceinline__ void barrier() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// page * page_bytes + slot * slot_bytes behind base (32-bit factors: two multiply-adds)
+__device__ __forceinline__ global_bytes row_address(global_bytes base, int page, int slot, uint32_t page_bytes,
+                                                   uint32_t slot_bytes) {
+  return base + (uint64_t)(uint32_t)page * page_bytes + (uint64_t)(uint32_t)slot * slot_bytes;
 }
 
 // A lane's share of a tile of a 16-bit cache on its way to LDS: kN times 16
@@ -172,20 +183,30 @@ struct Direct {
   // rows i * RW * kRows + first of the tile, i < kN
   static __device__ __forceinline__ int first(int wave, int lane) { return wave * kRows + lane / kChunks; }
 
+  // whole: every row is a key and every page number is one of the cache
   template <bool KEYS>
-  static __device__ __forceinline__ void load(const AttendArgs& a, const char* base, const int (&page)[kN], int key0,
-                                              int end, int wave, int lane, uint32_t to) {
-    const int mask = (1 << a.page_shift) - 1;
-    const int64_t page_bytes = KEYS ? a.kc_page : a.vc_page, slot_bytes = KEYS ? a.kc_slot : a.vc_slot;
+  static __device__ __forceinline__ void load(const AttendArgs& a, global_bytes base, const int (&page)[kN], bool whole,
+                                              int key0, int end, int wave, int lane, uint32_t to) {
+    const uint32_t page_bytes = KEYS ? a.kc_page : a.vc_page, slot_bytes = KEYS ? a.kc_slot : a.vc_slot;
+    global_bytes p[kN];
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const int row = i * RW * kRows + first(wave, lane), key = key0 + row;
+      const int row = i * RW * kRows + first(wave, lane);
       const int ch = (lane % kChunks) ^ (KEYS ? swizzle_k<D>(row) : swizzle_v<D>(row));
-      const char* p = base + page[i] * page_bytes + (key & mask) * slot_bytes + ch * 16;
-      if (key >= end) p = (const char*)kNoRow;
-      else if ((uint32_t)page[i] >= (uint32_t)a.num_pages) p = (const char*)kBadRow;
-      load16_to_lds(p, to + (i * RW + wave) * 1024);
+      p[i] = row_address(base + ch * 16, page[i], (key0 + row) & a.page_mask, page_bytes, slot_bytes);
     }
+    if (!whole) {
+#pragma unroll
+      for (int i = 0; i < kN; ++i) {
+        const int key = key0 + i * RW * kRows + first(wave, lane);
+        if (key >= end)
+          p[i] = (global_bytes)kNoRow;
+        else if ((uint32_t)page[i] >= (uint32_t)a.num_pages)
+          p[i] = (global_bytes)kBadRow;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kN; ++i) load16_to_lds(p[i], to + (i * RW + wave) * 1024);
   }
 };
 
@@ -202,20 +223,29 @@ struct Widened {
 
   i32x4 k[kN], v[kN];
 
-  __device__ __forceinline__ void fetch(const AttendArgs& a, const char* kc, const char* vc, const int (&page)[kN],
-                                        int key0, int end, int thread) {
-    const int mask = (1 << a.page_shift) - 1;
+  __device__ __forceinline__ void fetch(const AttendArgs& a, global_bytes kc, global_bytes vc, const int (&page)[kN],
+                                        bool whole, int key0, int end, int thread) {
+    global_bytes pk[kN], pv[kN];
+    const int at = thread % kChunks * 16;
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const int key = key0 + i * kRows + thread / kChunks;
-      const char* pk = kc + page[i] * a.kc_page + (key & mask) * a.kc_slot + thread % kChunks * 16;
-      const char* pv = vc + page[i] * a.vc_page + (key & mask) * a.vc_slot + thread % kChunks * 16;
-      if (key >= end)
-        pk = pv = (const char*)kNoRow;
-      else if ((uint32_t)page[i] >= (uint32_t)a.num_pages)
-        pk = pv = (const char*)kBadRow;
-      k[i] = *(const i32x4*)pk;
-      v[i] = *(const i32x4*)pv;
+      const int slot = (key0 + i * kRows + thread / kChunks) & a.page_mask;
+      pk[i] = row_address(kc + at, page[i], slot, a.kc_page, a.kc_slot);
+      pv[i] = row_address(vc + at, page[i], slot, a.vc_page, a.vc_slot);
+    }
+    if (!whole) {
+#pragma unroll
+      for (int i = 0; i < kN; ++i) {
+        if (key0 + i * kRows + thread / kChunks >= end)
+          pk[i] = pv[i] = (global_bytes)kNoRow;
+        else if ((uint32_t)page[i] >= (uint32_t)a.num_pages)
+          pk[i] = pv[i] = (global_bytes)kBadRow;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      k[i] = *(global_chunk)pk[i];
+      v[i] = *(global_chunk)pv[i];
     }
   }
 
@@ -247,6 +277,8 @@ __device__ __forceinline__ s16x4 round4(float a, float b, float c, float d) {
   return __builtin_bit_cast(s16x4, __builtin_convertvector(x, typename T::x4));
 }
 
+constexpr float kSlack = 8.0f;  // p < 2^8: far from the largest half, and l from the largest float
+
 // A wave's 32 rows: queries, running maximum (log2 units) and sum, results.
 template <int D, class T>
 struct Rows {
@@ -258,16 +290,17 @@ struct Rows {
   template <int KB>
   __device__ __forceinline__ void scores(const char* kt, f32x16 (&s)[KB], int n, int hh) {
 #pragma unroll
-    for (int b = 0; b < KB; ++b) {
+    for (int b = 0; b < KB; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
-      const int kr = b * 32 + n;
+#pragma unroll
+    for (int b = 0; b < KB; ++b)
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) {
+        const int kr = b * 32 + n;
         const s16x8 x = *(const s16x8*)(kt + kr * 2 * D + (((2 * i + hh) ^ swizzle_k<D>(kr)) << 4));
         s[b] = T::mfma(x, q[i], s[b]);
       }
-    }
   }
 
   // Scores to p; keys from `seen` on are hidden where `edge` says that there are such.
@@ -277,16 +310,20 @@ struct Rows {
 #pragma unroll
       for (int b = 0; b < KB; ++b)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (b * 32 + 8 * (i / 4) + 4 * hh + i % 4 >= seen) s[b][i] = -INFINITY;
+        for (int i = 0; i < 16; ++i) {
+          int last = seen - 4 * hh;
+          asm("" : "+v"(last));  // each compare by itself: related, they take more masks than there are registers
+          if (b * 32 + 8 * (i / 4) + i % 4 >= last) s[b][i] = -INFINITY;
+        }
     }
-    float top = s[0][0];
+    float top = max3(s[0][0], s[0][1], s[0][2]);
 #pragma unroll
-    for (int b = 0; b < KB; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+    for (int i = 3; i < 16 * KB - 1; i += 2) top = max3(top, s[i / 16][i % 16], s[(i + 1) / 16][(i + 1) % 16]);
+    top = max3(top, s[KB - 1][15], s[KB - 1][15]);
     top = half_max(top) * scale;
-    if (__any(top > m)) {
+    // m need not be the maximum, only near it: o and l are scaled when a row's
+    // maximum has grown by more than 2^kSlack, which p then stays below
+    if (__any(top > m + kSlack)) {
       const float next = fmaxf(m, top);
       // before the first key of a row: nothing to scale
       const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - next);
@@ -388,6 +425,8 @@ __device__ __forceinline__ bool holds_odd(const char* tile, int lane) {
   return __any(odd);
 }
 
+typedef const __attribute__((address_space(4))) AttendArgs Args;
+
 template <int D, class T, bool FP8, int RW>
 __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it, int head, float scale, char* lds) {
   typedef Shape<D, RW> S;
@@ -407,6 +446,9 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
     const char* p = a.q + token * a.q_tok + qhead * a.q_head + hh * 16;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) x.q[i] = *(const s16x8*)(p + i * 32);
+    // waited for here: a wait inside the loop would be for the tiles' loads too
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) asm volatile("" : "+v"(x.q[i]));
   }
 #pragma unroll
   for (int b = 0; b < DB; ++b)
@@ -417,17 +459,17 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
   const int limit = (int)token + it.limit;                                // own keys that this row sees
   const int limit0 = (int)divide((uint32_t)it.row0, a.share) + it.limit;  // ... and the first row
 
-  const char* kc = a.kc + head * a.kc_head;
-  const char* vc = a.vc + head * a.vc_head;
-  const int32_t* own_table = a.table + it.request * a.table_stride;
-  const int32_t* prefix_table = it.prefix_steps ? a.prefix_table + it.prefix * a.prefix_stride : nullptr;
+  const global_bytes kc = (global_bytes)(a.kc + head * a.kc_head);
+  const global_bytes vc = (global_bytes)(a.vc + head * a.vc_head);
+  const global_ints own_table = (global_ints)(a.table + it.request * a.table_stride);
+  const global_ints prefix_table = (global_ints)(a.prefix_table + it.prefix * a.prefix_stride);
   const int tiles = (it.step1 - it.step0) * (kStepKeys / KT);
 
   // tile t of the item: its first key, the end of its keys, their table, and
   // whether it is the prefix's
   struct Place {
     int key0, end;
-    const int32_t* table;
+    global_ints table;
     bool shared;
   };
   auto place = [&](int t) {
@@ -436,24 +478,23 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
     p.shared = step < it.prefix_steps;
     p.key0 = (p.shared ? step : step - it.prefix_steps) * kStepKeys + part * KT;
     p.end = t >= tiles ? 0 : p.shared ? it.prefix_len : it.own_end;
-    p.table = p.shared ? prefix_table : own_table;
+    p.table = t >= tiles ? (global_ints)kNoRow : p.shared ? prefix_table : own_table;
     return p;
   };
-  // page numbers of rows row0 + i * step (i < N) of a tile
+  // page numbers of rows row0 + i * step (i < N) of a tile (behind its end: the last key's)
   auto pages = [&](const Place& p, int row0, int step, auto& page) {
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof(page) / sizeof(int)); ++i) {
-      const int key = p.key0 + row0 + i * step;
-      page[i] = key < p.end ? p.table[key >> a.page_shift] : 0;
-    }
-  };
-  auto check_pages = [&](const Place& p, int row0, int step, const auto& page) {
-    if (!a.status) return;
-    bool bad = false;
-#pragma unroll
     for (int i = 0; i < (int)(sizeof(page) / sizeof(int)); ++i)
-      bad |= p.key0 + row0 + i * step < p.end && (uint32_t)page[i] >= (uint32_t)a.num_pages;
-    if (bad) atomicOr(a.status, (uint32_t)KVR_DEV_BAD_PAGE);
+      page[i] = p.table[max(0, min(p.key0 + row0 + i * step, p.end - 1)) >> a.page_shift];
+  };
+  // whether all rows of a tile are keys in pages of the cache; a page outside it is reported
+  auto whole_of = [&](const Place& p, const auto& page) {
+    uint32_t top = (uint32_t)page[0];
+#pragma unroll
+    for (int i = 1; i < (int)(sizeof(page) / sizeof(int)); ++i) top = max(top, (uint32_t)page[i]);
+    const bool bad = top >= (uint32_t)a.num_pages && p.end > 0;
+    if (bad && a.status) atomicOr(a.status, (uint32_t)KVR_DEV_BAD_PAGE);
+    return p.key0 + KT <= p.end && !__any(bad);
   };
   // the scores of a tile, p, and their product with V
   auto seen_of = [&](const Place& p) { return (p.shared ? p.end : min(limit, p.end)) - p.key0; };
@@ -483,21 +524,23 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
       load_ids(0);
       wait_loads<0>();
       read_ids(0);
-      L::template load<true>(a, kc, page, p.key0, p.end, 0, lane, k_to);
+      const bool whole = whole_of(p, page);
+      L::template load<true>(a, kc, page, whole, p.key0, p.end, 0, lane, k_to);
       if (mine > 1) load_ids(1);
-      L::template load<false>(a, vc, page, p.key0, p.end, 0, lane, v_to);
+      L::template load<false>(a, vc, page, whole, p.key0, p.end, 0, lane, v_to);
       for (int j = 0; j < mine; ++j) {
         // in flight, oldest first: K of this tile, the next one's page numbers, V of this tile
         const bool more = j + 1 < mine;
         const Place p1 = place(wave + 4 * (j + 1));
-        check_pages(p, L::first(0, lane), L::kRows, page);
+        bool whole1 = false;
         wait_loads<N>();
-        if (more) read_ids(j + 1);
         f32x16 s[KB];
+        if (more) read_ids(j + 1);
         x.scores(kt, s, n, hh);
         wait_lds();
         if (more) {
-          L::template load<true>(a, kc, page, p1.key0, p1.end, 0, lane, k_to);
+          whole1 = whole_of(p1, page);
+          L::template load<true>(a, kc, page, whole1, p1.key0, p1.end, 0, lane, k_to);
           if (j + 2 < mine) load_ids(j + 2);
         }
         const bool edge = edge_of(p);
@@ -514,7 +557,7 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
         else
           x.values(vt, s, lane);
         wait_lds();
-        if (more) L::template load<false>(a, vc, page, p1.key0, p1.end, 0, lane, v_to);
+        if (more) L::template load<false>(a, vc, page, whole1, p1.key0, p1.end, 0, lane, v_to);
         p = p1;
       }
     }
@@ -528,13 +571,11 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
     const int row0 = lane / L::kChunks;
     Place p = place(wave), p1 = place(wave + 4);
     pages(p, row0, L::kRows, page);
-    ld.fetch(a, kc, vc, page, p.key0, p.end, lane);
-    check_pages(p, row0, L::kRows, page);
+    ld.fetch(a, kc, vc, page, whole_of(p, page), p.key0, p.end, lane);
     pages(p1, row0, L::kRows, page);
     for (int j = 0; j < mine; ++j) {
       ld.store(kt, vt, lane);
-      ld.fetch(a, kc, vc, page, p1.key0, p1.end, lane);
-      check_pages(p1, row0, L::kRows, page);
+      ld.fetch(a, kc, vc, page, whole_of(p1, page), p1.key0, p1.end, lane);
       const Place p2 = place(wave + 4 * (j + 2));
       pages(p2, row0, L::kRows, page);
       f32x16 s[KB];
@@ -572,9 +613,9 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
       const int row0 = L::first(rw, lane), step = RW * L::kRows;
       const uint32_t to = lds_offset(group);
       pages(p, row0, step, page);
-      L::template load<true>(a, kc, page, p.key0, p.end, rw, lane, to);
-      L::template load<false>(a, vc, page, p.key0, p.end, rw, lane, to + S::kTileBytes);
-      check_pages(p, row0, step, page);
+      bool whole = whole_of(p, page);
+      L::template load<true>(a, kc, page, whole, p.key0, p.end, rw, lane, to);
+      L::template load<false>(a, vc, page, whole, p.key0, p.end, rw, lane, to + S::kTileBytes);
       pages(p1, row0, step, page);
       for (int round = 0; round < rounds; ++round) {
         wait_loads<0>();
@@ -583,9 +624,9 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
         const char* kt = group + (round & 1) * 2 * S::kTileBytes;
         const Place p2 = place((round + 2) * KG + kg);
         if (round + 1 < rounds) {
-          L::template load<true>(a, kc, page, p1.key0, p1.end, rw, lane, to + b1);
-          L::template load<false>(a, vc, page, p1.key0, p1.end, rw, lane, to + b1 + S::kTileBytes);
-          check_pages(p1, row0, step, page);
+          whole = whole_of(p1, page);
+          L::template load<true>(a, kc, page, whole, p1.key0, p1.end, rw, lane, to + b1);
+          L::template load<false>(a, vc, page, whole, p1.key0, p1.end, rw, lane, to + b1 + S::kTileBytes);
           pages(p2, row0, step, page);
         }
         work(kt, kt + S::kTileBytes);
@@ -598,8 +639,7 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
       L ld;
       const int row0 = thread / L::kChunks;
       pages(p, row0, L::kRows, page);
-      ld.fetch(a, kc, vc, page, p.key0, p.end, thread);
-      check_pages(p, row0, L::kRows, page);
+      ld.fetch(a, kc, vc, page, whole_of(p, page), p.key0, p.end, thread);
       pages(p1, row0, L::kRows, page);
       ld.store(group, group + S::kTileBytes, thread);
       for (int round = 0; round < rounds; ++round) {
@@ -607,8 +647,7 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
         char* kt = group + (round & 1) * 2 * S::kTileBytes;
         char* kt1 = group + (round + 1 & 1) * 2 * S::kTileBytes;
         const Place p2 = place((round + 2) * KG + kg);
-        ld.fetch(a, kc, vc, page, p1.key0, p1.end, thread);
-        check_pages(p1, row0, L::kRows, page);
+        ld.fetch(a, kc, vc, page, whole_of(p1, page), p1.key0, p1.end, thread);
         pages(p2, row0, L::kRows, page);
         work(kt, kt + S::kTileBytes);
         ld.store(kt1, kt1 + S::kTileBytes, thread);
@@ -619,27 +658,32 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
   }
   const float m = x.m, l = half_sum(x.l);
   auto& o = x.o;
-  const float vs = a.vs ? a.vs[head] : 1.0f;
+  // what only the end needs is read here, not kept in scalar registers
+  const Args* late = (const Args*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(late));
+  const Args& z = *late;
+  const Divisor share = {z.share.d, z.share.mul, z.share.shift};
+  const float vs = z.vs ? z.vs[head] : 1.0f;
   // four consecutive results of a row: the final ones, or the partial ones
   auto emit = [&](int rr, int d, f32x4 y, float ll) {
     const uint32_t R = (uint32_t)(it.row0 + rr);
     if (it.acc < 0) {
       const float f = ll > 0.0f || ll != ll ? vs / ll : 0.0f;
-      const uint32_t tk = divide(R, a.share);
-      const int hd = head * (int)a.share.d + (int)(R - tk * a.share.d);
-      *(s16x4*)(a.out + tk * a.o_tok + hd * a.o_head + d * 2) = round4<T>(y[0] * f, y[1] * f, y[2] * f, y[3] * f);
+      const uint32_t tk = divide(R, share);
+      const int hd = head * (int)share.d + (int)(R - tk * share.d);
+      *(s16x4*)(z.out + tk * z.o_tok + hd * z.o_head + d * 2) = round4<T>(y[0] * f, y[1] * f, y[2] * f, y[3] * f);
     } else {
-      *(f32x4*)(a.acc + ((int64_t)(it.acc + rr) * a.kv_heads + head) * D + d) = y;
+      *(f32x4*)(z.acc + ((int64_t)(it.acc + rr) * z.kv_heads + head) * D + d) = y;
     }
   };
   auto emit_ml = [&](int rr, float mm, float ll) {
     if (it.acc >= 0) {
-      a.ml[(int64_t)(it.acc + rr) * a.kv_heads + head] = make_float2(mm, ll);
-    } else if (a.lse) {
+      z.ml[(int64_t)(it.acc + rr) * z.kv_heads + head] = make_float2(mm, ll);
+    } else if (z.lse) {
       const uint32_t R = (uint32_t)(it.row0 + rr);
-      const uint32_t tk = divide(R, a.share);
-      const int hd = head * (int)a.share.d + (int)(R - tk * a.share.d);
-      a.lse[(int64_t)tk * a.heads + hd] = ll > 0.0f || ll != ll ? (mm + __log2f(ll)) * 0.69314718055994530942f
+      const uint32_t tk = divide(R, share);
+      const int hd = head * (int)share.d + (int)(R - tk * share.d);
+      z.lse[(int64_t)tk * z.heads + hd] = ll > 0.0f || ll != ll ? (mm + __log2f(ll)) * 0.69314718055994530942f
                                                                : -INFINITY;
     }
   };
@@ -704,10 +748,8 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(AttendArg
   if (item >= a.hdr->items) return;
   const Item it = a.items[item];
   const float scale = FP8 && a.ks ? a.scale_log2 * a.ks[head] : a.scale_log2;
-  if (it.rows > 64)
+  if (it.rows > 32)
     attend_item<D, T, FP8, 4>(a, it, head, scale, lds);
-  else if (it.rows > 32)
-    attend_item<D, T, FP8, 2>(a, it, head, scale, lds);
   else
     attend_item<D, T, FP8, 1>(a, it, head, scale, lds);
 }

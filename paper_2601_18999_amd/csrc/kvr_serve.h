@@ -109,8 +109,9 @@ struct AttendArgs {
   float* lse;
   const char *kc, *vc;
   const float *ks, *vs;
-  int64_t q_tok, q_head, o_tok, o_head;                          // bytes
-  int64_t kc_page, kc_slot, kc_head, vc_page, vc_slot, vc_head;  // bytes
+  int64_t q_tok, q_head, o_tok, o_head;  // bytes
+  int64_t kc_head, vc_head;
+  uint32_t kc_page, kc_slot, vc_page, vc_slot;
   const int32_t *row_start, *length, *table, *group_start, *prefix_table, *prefix_length;
   int64_t table_stride, prefix_stride;
   uint32_t* status;
@@ -125,7 +126,7 @@ struct AttendArgs {
   Divisor share;
   float scale_log2;
   int32_t tokens, requests, groups, heads, kv_heads, dim;
-  int32_t page_shift, num_pages, width, prefix_width;
+  int32_t page_shift, page_mask, num_pages, width, prefix_width;
   int32_t unit_cap, item_cap, split_slots;
 };
 

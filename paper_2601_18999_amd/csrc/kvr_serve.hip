@@ -243,7 +243,7 @@ constexpr int kMinSplitCost = 8;  // least cost of an item that a unit is split 
 // Waves along the rows that `rows` rows take in tiles of kTileRows.
 __device__ __forceinline__ int row_waves(int rows) {
   const int rest = rows % kTileRows;
-  return rows / kTileRows * 4 + (rest == 0 ? 0 : rest <= 32 ? 1 : rest <= 64 ? 2 : 4);
+  return rows / kTileRows * 4 + (rest == 0 ? 0 : rest <= 32 ? 1 : 4);
 }
 
 __device__ __forceinline__ int steps_of(int keys) { return (keys + kStepKeys - 1) / kStepKeys; }
@@ -254,8 +254,12 @@ struct UnitWork {
   int group;  // the group whose shared partial results the unit's rows have, or -1
 };
 
-// Unit u of segment s (a group, or groups + a request).
-__device__ UnitWork unit_work(const AttendArgs& a, int s, int tile) {
+// Unit u of segment s (a group, or groups + a request).  A request's last
+// rows, which see the most keys, come first: the workgroups that start last
+// are then the short ones (9,216 new tokens of 32 heads: 924 -> 804 us with
+// the scheduler that build.py names).
+__device__ UnitWork unit_work(const AttendArgs& a, int s, int u) {
+  const int tile = s < a.groups ? u - a.bounds[s] : a.bounds[s + 1] - 1 - u;
   UnitWork w;
   const int g = (int)a.share.d;
   w.group = -1;
@@ -369,7 +373,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(AttendArgs a) {
   int64_t total = 0;
   for (int u = tid; u < units; u += kPlanThreads) {
     const int s = last_at_most(a.bounds, segments, u);
-    total += unit_work(a, s, u - a.bounds[s]).cost;
+    total += unit_work(a, s, u).cost;
   }
   group_before(total, total, part64);
   const int64_t fair = (total + a.split_slots - 1) / a.split_slots;
@@ -381,7 +385,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(AttendArgs a) {
     int splits = 0, per = 1, partial = 0;
     if (u < units) {
       const int s = last_at_most(a.bounds, segments, u);
-      w = unit_work(a, s, u - a.bounds[s]);
+      w = unit_work(a, s, u);
       splits = max(1, (w.cost + chunk - 1) / chunk);
       per = max(1, (w.steps + splits - 1) / splits);
       splits = max(1, (w.steps + per - 1) / per);

@@ -70,6 +70,9 @@ kvr_status check_buffers(const kvr_cache* c) {
   if (!aligned(c->d_k, 16) || !aligned(c->d_v, 16) || !on_chunks(c->k_page, c->k_slot, c->k_head, size) ||
       !on_chunks(c->v_page, c->v_slot, c->v_head, size))
     return invalid("every head of the cache must start on a 16-byte boundary");
+  // the kernels multiply by these in 32 bits
+  for (const int64_t stride : {c->k_page, c->k_slot, c->v_page, c->v_slot})
+    if (stride < 0 || stride * size > kInt) return invalid("strides of pages and slots must be in 0..2^31 - 1 bytes");
   return KVR_OK;
 }
 
@@ -272,11 +275,11 @@ kvr_status kvr_shared_attention(const kvr_cache* c, const kvr_attention* s, void
   a.q_head = s->q_head * 2;
   a.o_tok = s->out_token * 2;
   a.o_head = s->out_head * 2;
-  a.kc_page = c->k_page * size;
-  a.kc_slot = c->k_slot * size;
+  a.kc_page = (uint32_t)(c->k_page * size);
+  a.kc_slot = (uint32_t)(c->k_slot * size);
   a.kc_head = c->k_head * size;
-  a.vc_page = c->v_page * size;
-  a.vc_slot = c->v_slot * size;
+  a.vc_page = (uint32_t)(c->v_page * size);
+  a.vc_slot = (uint32_t)(c->v_slot * size);
   a.vc_head = c->v_head * size;
   a.row_start = s->d_row_start;
   a.length = s->d_length;
@@ -304,6 +307,7 @@ kvr_status kvr_shared_attention(const kvr_cache* c, const kvr_attention* s, void
   a.kv_heads = c->kv_heads;
   a.dim = c->dim;
   a.page_shift = log2_of(c->page_size);
+  a.page_mask = c->page_size - 1;
   a.num_pages = c->num_pages;
   a.width = s->width;
   a.prefix_width = s->prefix_width;
