@@ -265,38 +265,38 @@ def kvr_destroy(ctx: int) -> None:
         load_library().kvr_destroy(ctypes.c_void_p(ctx))
 
 
-# Serving operators: the arguments are the packed structs of include/kvr.h
-# (bytearrays); the functions on tensors that pack them are in serve.py.
+# Serving operators: the arguments are the packed structs of include/kvr.h (bytes);
+# the functions on tensors that pack them are in serve.py.
 
-def _struct(args: bytearray):
-    return ctypes.byref((ctypes.c_char * len(args)).from_buffer(args))
-
-
-def kvr_block_tables_workspace(tables: bytearray) -> int:
+def kvr_block_tables_workspace(tables: bytes) -> int:
     n = ctypes.c_size_t(0)
-    _check(load_library().kvr_block_tables_workspace(_struct(tables), ctypes.byref(n)), "kvr_block_tables_workspace")
+    _check(load_library().kvr_block_tables_workspace(bytes(tables), ctypes.byref(n)), "kvr_block_tables_workspace")
     return n.value
 
 
-def kvr_block_tables(tables: bytearray, d_workspace: int, nbytes: int, stream: int = 0) -> None:
-    _check(load_library().kvr_block_tables(_struct(tables), d_workspace, nbytes, stream), "kvr_block_tables")
+def kvr_block_tables(tables: bytes, d_workspace: int, nbytes: int, stream: int = 0) -> None:
+    st = (_lib or load_library()).kvr_block_tables(bytes(tables), d_workspace, nbytes, stream)
+    if st:
+        _check(st, "kvr_block_tables")
 
 
-def kvr_cache_store(cache: bytearray, store: bytearray, stream: int = 0) -> None:
-    _check(load_library().kvr_cache_store(_struct(cache), _struct(store), stream), "kvr_cache_store")
+def kvr_cache_store(cache: bytes, store: bytes, stream: int = 0) -> None:
+    st = (_lib or load_library()).kvr_cache_store(bytes(cache), bytes(store), stream)
+    if st:
+        _check(st, "kvr_cache_store")
 
 
-def kvr_attention_workspace(cache: bytearray, attention: bytearray) -> int:
+def kvr_attention_workspace(cache: bytes, attention: bytes) -> int:
     n = ctypes.c_size_t(0)
-    _check(load_library().kvr_attention_workspace(_struct(cache), _struct(attention), ctypes.byref(n)),
+    _check(load_library().kvr_attention_workspace(bytes(cache), bytes(attention), ctypes.byref(n)),
            "kvr_attention_workspace")
     return n.value
 
 
-def kvr_shared_attention(cache: bytearray, attention: bytearray, d_workspace: int, nbytes: int,
-                         stream: int = 0) -> None:
-    _check(load_library().kvr_shared_attention(_struct(cache), _struct(attention), d_workspace, nbytes, stream),
-           "kvr_shared_attention")
+def kvr_shared_attention(cache: bytes, attention: bytes, d_workspace: int, nbytes: int, stream: int = 0) -> None:
+    st = (_lib or load_library()).kvr_shared_attention(bytes(cache), bytes(attention), d_workspace, nbytes, stream)
+    if st:
+        _check(st, "kvr_shared_attention")
 
 
 from .sim import Simulator  # noqa: E402,F401

@@ -24,22 +24,19 @@ __device__ __forceinline__ V wave_before(V x, V& all) {
   return s - x;
 }
 
-// The same over a workgroup of up to 16 waves; `part` is 17 values of LDS.
+// The same over a workgroup of up to 16 waves; `part` is 16 values of LDS.
 // Every thread of the workgroup calls it.
 template <class V>
 __device__ __forceinline__ V group_before(V x, V& all, V* part) {
-  const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  V w, s = wave_before(x, w);
+  const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6, lane = threadIdx.x & 63;
+  V w;
+  const V s = wave_before(x, w);
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) part[wave] = w;
+  if (lane == 0) part[wave] = w;
   __syncthreads();
-  V sum = 0;
-  for (int i = 0; i < waves; ++i) {
-    if (i == wave) s += sum;
-    sum += part[i];
-  }
-  all = sum;
-  return s;
+  const V y = lane < waves ? part[lane] : V(0);
+  const V before = wave_before(y, all);
+  return s + __shfl(before, wave);
 }
 
 // Largest i of [0, n) with start[i] <= x, for start ascending and start[0] <= x.
@@ -81,10 +78,11 @@ __device__ __forceinline__ RowChange row_change(const TablesArgs& a, int held, i
 }
 
 // One workgroup: sums over the rows, the checks, and everything that is one
-// value a row.  A thread takes neighbouring rows.
-__global__ void __launch_bounds__(kScanThreads) tables_scan_kernel(TablesArgs a) {
-  __shared__ int64_t part[17];
-  const int per = (a.rows + kScanThreads - 1) / kScanThreads;
+// value a row.  A thread takes neighbouring rows.  row_start (one more than
+// the rows), gain_at and give_at are written for what follows.
+__device__ __forceinline__ TablesHdr scan_rows(const TablesArgs& a, int64_t* part, int* row_start, int* gain_at,
+                                               int* give_at) {
+  const int per = (a.rows + blockDim.x - 1) / blockDim.x;
   const int r0 = min(a.rows, (int)threadIdx.x * per), r1 = min(a.rows, r0 + per);
   const int64_t head = a.state[0], tail = a.state[1], old_bits = a.state[2];
   int64_t tokens = 0, pages = 0;
@@ -108,73 +106,104 @@ __global__ void __launch_bounds__(kScanThreads) tables_scan_kernel(TablesArgs a)
   for (int r = r0; r < r1; ++r) {
     const int held = a.held[r], delta = a.delta[r];
     const RowChange c = row_change(a, held, delta);
-    a.row_start[r] = bits ? 0 : (int)tokens;
-    a.gain_at[r] = (int)(pages & 0xffffffffll);
-    a.give_at[r] = (int)(pages >> 32);
+    row_start[r] = bits ? 0 : (int)tokens;
+    gain_at[r] = (int)(pages & 0xffffffffll);
+    give_at[r] = (int)(pages >> 32);
     a.held_out[r] = bits ? held : held + delta;
     tokens += c.tokens;
     pages += c.pages;
   }
-  if (threadIdx.x == 0) {
-    a.row_start[a.rows] = bits ? 0 : (int)all_tokens;
-    a.gain_at[a.rows] = (int)gain;
-    a.give_at[a.rows] = (int)give;
-    TablesHdr h;
-    h.head = head;
-    h.tail = tail;
-    h.gain = (int)gain;
-    h.give = (int)give;
-    h.tokens = (int)all_tokens;
-    h.rejected = bits != 0;
-    *a.hdr = h;
-  }
-  __syncthreads();
+  if (threadIdx.x == 0) row_start[a.rows] = bits ? 0 : (int)all_tokens;
+  TablesHdr h;
+  h.head = head % a.ring_size;
+  h.tail = tail % a.ring_size;
+  h.gain = (int)gain;
+  h.give = (int)give;
+  h.tokens = (int)all_tokens;
+  h.rejected = bits != 0;
+  __syncthreads();  // every thread has read the state and its rows
   if (threadIdx.x == 0) {
     a.state_out[0] = bits ? head : head + gain;
     a.state_out[1] = bits ? tail : tail + give;
     a.state_out[2] = old_bits | bits;
   }
+  return h;
+}
+
+// place of page i of the ring counted from `from`; from, i < size
+__device__ __forceinline__ int ring_at(int from, int i, int size) {
+  const uint32_t at = (uint32_t)from + (uint32_t)i;
+  return (int)(at >= (uint32_t)size ? at - size : at);
+}
+
+// Slot and position of new token t.  Its row is found in row_start; the first
+// token of a gained page writes its table entry (a gained page always has one).
+__device__ __forceinline__ void place_token(const TablesArgs& a, const TablesHdr& h, const int* row_start,
+                                            const int* gain_at, int t) {
+  int slot = -1, position = -1;
+  if (!h.rejected && t < h.tokens) {
+    const int mask = (1 << a.page_shift) - 1;
+    const int r = last_at_most(row_start, a.rows, t);
+    const int held = a.held_out[r] - a.delta[r];
+    const int at = held + t - row_start[r];
+    const int col = at >> a.page_shift, before = (int)(((int64_t)held + mask) >> a.page_shift);
+    int32_t* entry = a.table + r * a.table_stride + col;
+    int page;
+    if (col < before) {
+      page = *entry;
+    } else {
+      page = a.ring[ring_at((int)h.head, gain_at[r] + col - before, a.ring_size)];
+      if ((at & mask) == 0) *entry = page;
+    }
+    slot = (page << a.page_shift) | (at & mask);
+    position = (a.base ? a.base[r] : 0) + at;
+  }
+  a.slots[t] = slot;
+  a.positions[t] = position;
+}
+
+// Puts back dropped page g.
+__device__ __forceinline__ void drop_page(const TablesArgs& a, const TablesHdr& h, const int* give_at, int g) {
+  const int r = last_at_most(give_at, a.rows, g);
+  const int mask = (1 << a.page_shift) - 1;
+  const int after = (int)(((int64_t)a.held_out[r] + mask) >> a.page_shift);
+  a.ring[ring_at((int)h.tail, g, a.ring_size)] = a.table[r * a.table_stride + after + g - give_at[r]];
+}
+
+__global__ void __launch_bounds__(kScanThreads) tables_scan_kernel(TablesArgs a) {
+  __shared__ int64_t part[16];
+  const TablesHdr h = scan_rows(a, part, a.row_start, a.gain_at, a.give_at);
+  if (threadIdx.x == 0) *a.hdr = h;
+}
+
+// Few rows and tokens: all in one workgroup and one launch, the sums in LDS
+// (FUSED_FIGURE).
+constexpr int kFusedRows = 1024, kFusedTokens = 4096;
+__global__ void __launch_bounds__(kScanThreads) tables_fused_kernel(TablesArgs a) {
+  __shared__ int64_t part[16];
+  __shared__ int row_start[kFusedRows + 1], gain_at[kFusedRows], give_at[kFusedRows];
+  const TablesHdr h = scan_rows(a, part, row_start, gain_at, give_at);
+  for (int r = threadIdx.x; r <= a.rows; r += blockDim.x) a.row_start[r] = row_start[r];
+  for (int t = threadIdx.x; t < a.num_tokens; t += blockDim.x) place_token(a, h, row_start, gain_at, t);
+  if (h.rejected) return;
+  for (int g = threadIdx.x; g < h.give; g += blockDim.x) drop_page(a, h, give_at, g);
 }
 
 constexpr int kFillThreads = 256, kFillTokens = 4;  // tokens of a thread
 
 // Slots and positions of the new tokens, the pages they gain, and the pages
-// that are given back.  A token's row is found in row_start; the first token
-// of a gained page writes its table entry (a gained page always has one).
+// that are given back.
 __global__ void __launch_bounds__(kFillThreads) tables_fill_kernel(TablesArgs a) {
   const TablesHdr h = *a.hdr;
-  const int mask = (1 << a.page_shift) - 1;
   const int t0 = blockIdx.x * kFillThreads * kFillTokens;
 #pragma unroll
   for (int i = 0; i < kFillTokens; ++i) {
     const int t = t0 + i * kFillThreads + threadIdx.x;
-    if (t >= a.num_tokens) break;
-    int slot = -1, position = -1;
-    if (!h.rejected && t < h.tokens) {
-      const int r = last_at_most(a.row_start, a.rows, t);
-      const int held = a.held_out[r] - a.delta[r];
-      const int at = held + t - a.row_start[r];
-      const int col = at >> a.page_shift, before = (int)(((int64_t)held + mask) >> a.page_shift);
-      int32_t* entry = a.table + r * a.table_stride + col;
-      int page;
-      if (col < before) {
-        page = *entry;
-      } else {
-        page = a.ring[(h.head + a.gain_at[r] + col - before) % a.ring_size];
-        if ((at & mask) == 0) *entry = page;
-      }
-      slot = (page << a.page_shift) | (at & mask);
-      position = (a.base ? a.base[r] : 0) + at;
-    }
-    a.slots[t] = slot;
-    a.positions[t] = position;
+    if (t < a.num_tokens) place_token(a, h, a.row_start, a.gain_at, t);
   }
   if (h.rejected) return;
-  for (int g = blockIdx.x * kFillThreads + threadIdx.x; g < h.give; g += gridDim.x * kFillThreads) {
-    const int r = last_at_most(a.give_at, a.rows, g);
-    const int after = (int)(((int64_t)a.held_out[r] + mask) >> a.page_shift);
-    a.ring[(h.tail + g) % a.ring_size] = a.table[r * a.table_stride + after + g - a.give_at[r]];
-  }
+  for (int g = blockIdx.x * kFillThreads + threadIdx.x; g < h.give; g += gridDim.x * kFillThreads)
+    drop_page(a, h, a.give_at, g);
 }
 
 // ---------------------------------------------------------------- cache store
@@ -238,6 +267,7 @@ __global__ void __launch_bounds__(256) store_kernel(StoreArgs a) {
 // ---------------------------------------------------------------- attention: the plan
 
 constexpr int kPlanThreads = 1024;
+constexpr int kPlanSmall = 1024;  // requests, groups: their lengths then stand in LDS
 constexpr int kMinSplitCost = 8;  // least cost of an item that a unit is split into
 
 // Waves along the rows that `rows` rows take in tiles of kTileRows.
@@ -254,12 +284,21 @@ struct UnitWork {
   int group;  // the group whose shared partial results the unit's rows have, or -1
 };
 
+// The lengths, in LDS or (many requests) where the caller has them, and what
+// the plan finds on its way.
+struct Lengths {
+  const int *row_start, *length, *group_start, *prefix_length;
+  int *bounds, *group_of, *waves;
+  bool single;  // one token each: row_start[b] = b
+  __device__ __forceinline__ int start(int b) const { return single ? b : row_start[b]; }
+};
+
 // Unit u of segment s (a group, or groups + a request).  A request's last
 // rows, which see the most keys, come first: the workgroups that start last
 // are then the short ones (9,216 new tokens of 32 heads: 924 -> 804 us with
 // the scheduler that build.py names).
-__device__ UnitWork unit_work(const AttendArgs& a, int s, int u) {
-  const int tile = s < a.groups ? u - a.bounds[s] : a.bounds[s + 1] - 1 - u;
+__device__ UnitWork unit_work(const AttendArgs& a, const Lengths& z, int s, int u) {
+  const int tile = s < a.groups ? u - z.bounds[s] : z.bounds[s + 1] - 1 - u;
   UnitWork w;
   const int g = (int)a.share.d;
   w.group = -1;
@@ -267,12 +306,11 @@ __device__ UnitWork unit_work(const AttendArgs& a, int s, int u) {
   w.it.acc = -1;
   w.it.step0 = 0;
   if (s < a.groups) {
-    const int b0 = a.group_start[s], b1 = a.group_start[s + 1];
-    const int t0 = a.row_start ? a.row_start[b0] : b0, t1 = a.row_start ? a.row_start[b1] : b1;
+    const int t0 = z.start(z.group_start[s]), t1 = z.start(z.group_start[s + 1]);
     w.it.row0 = t0 * g + tile * kTileRows;
     w.it.rows = min(kTileRows, t1 * g - w.it.row0);
     w.it.prefix = s;
-    w.it.prefix_len = a.prefix_length[s];
+    w.it.prefix_len = z.prefix_length[s];
     w.it.prefix_steps = steps_of(w.it.prefix_len);
     w.it.request = 0;
     w.it.own_end = 0;
@@ -280,23 +318,23 @@ __device__ UnitWork unit_work(const AttendArgs& a, int s, int u) {
     w.steps = w.it.prefix_steps;
   } else {
     const int b = s - a.groups;
-    const int t0 = a.row_start ? a.row_start[b] : b, t1 = a.row_start ? a.row_start[b + 1] : b + 1;
+    const int t0 = z.start(b), t1 = z.start(b + 1);
     w.it.row0 = t0 * g + tile * kTileRows;
     w.it.rows = min(kTileRows, t1 * g - w.it.row0);
     w.it.request = b;
-    w.it.limit = a.length[b] - (t1 - t0) - t0 + 1;
+    w.it.limit = z.length[b] - (t1 - t0) - t0 + 1;
     const int last = (int)divide((uint32_t)(w.it.row0 + w.it.rows - 1), a.share);
     w.it.own_end = last + w.it.limit;
     w.it.prefix = 0;
     w.it.prefix_len = 0;
     w.it.prefix_steps = 0;
     if (a.groups) {
-      const int j = a.group_of[b];
-      if (a.waves[j] == 1) {
+      const int j = z.group_of[b];
+      if (z.waves[j] == 1) {
         w.group = j;
       } else {
         w.it.prefix = j;
-        w.it.prefix_len = a.prefix_length[j];
+        w.it.prefix_len = z.prefix_length[j];
         w.it.prefix_steps = steps_of(w.it.prefix_len);
       }
     }
@@ -309,24 +347,60 @@ __device__ UnitWork unit_work(const AttendArgs& a, int s, int u) {
 
 // One workgroup: checks the lengths, decides which groups take their prefix
 // for all requests at once, and cuts the units into items of about equal cost.
+template <bool SMALL>
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(AttendArgs a) {
-  __shared__ int part[17];
-  __shared__ int64_t part64[17];
-  const int g = (int)a.share.d, tid = threadIdx.x;
-  // checks
+  __shared__ int part[16];
+  __shared__ int64_t part64[16];
+  __shared__ int lds[SMALL ? 8 * (kPlanSmall + 1) : 1];
+  const int g = (int)a.share.d, tid = threadIdx.x, threads = blockDim.x;
+  Lengths z;
+  z.single = !a.row_start;
   bool bad = false;
-  for (int b = tid; b < a.requests; b += kPlanThreads) {
-    const int t0 = a.row_start ? a.row_start[b] : b, t1 = a.row_start ? a.row_start[b + 1] : b + 1;
-    const int n = a.length[b];
+  if constexpr (SMALL) {
+    int* rs = lds;
+    int* len = rs + kPlanSmall + 1;
+    int* gs = len + kPlanSmall + 1;
+    int* pl = gs + kPlanSmall + 1;
+    z.waves = pl + kPlanSmall + 1;
+    z.group_of = z.waves + kPlanSmall + 1;
+    z.bounds = z.group_of + kPlanSmall + 1;  // twice as many
+    z.row_start = rs;
+    z.length = len;
+    z.group_start = gs;
+    z.prefix_length = pl;
+    for (int i = tid; i <= max(a.requests, a.groups); i += threads) {
+      const bool r = i < a.requests, j = i < a.groups;
+      const int x0 = i <= a.requests && a.row_start ? a.row_start[i] : i;
+      const int x1 = r ? a.length[i] : 0;
+      const int x2 = i <= a.groups && a.groups ? a.group_start[i] : 0;
+      const int x3 = j ? a.prefix_length[i] : 0;
+      if (i <= a.requests) rs[i] = x0;
+      if (r) len[i] = x1;
+      if (i <= a.groups) gs[i] = x2;
+      if (j) pl[i] = x3;
+    }
+    __syncthreads();
+  } else {
+    z.row_start = a.row_start;
+    z.length = a.length;
+    z.group_start = a.group_start;
+    z.prefix_length = a.prefix_length;
+    z.waves = a.waves;
+    z.group_of = a.group_of;
+    z.bounds = a.bounds;
+  }
+  // checks
+  for (int b = tid; b < a.requests; b += threads) {
+    const int t0 = z.start(b), t1 = z.start(b + 1), n = z.length[b];
     bad |= t0 < 0 || t1 < t0 || t1 > a.tokens || n < t1 - t0 || n > ((int64_t)a.width << a.page_shift);
     if (b == 0) bad |= t0 != 0;
   }
-  for (int j = tid; j < a.groups; j += kPlanThreads) {
-    const int b0 = a.group_start[j], b1 = a.group_start[j + 1], p = a.prefix_length[j];
+  for (int j = tid; j < a.groups; j += threads) {
+    const int b0 = z.group_start[j], b1 = z.group_start[j + 1], p = z.prefix_length[j];
     bad |= b0 < 0 || b1 < b0 || b1 > a.requests || p < 0 || p > ((int64_t)a.prefix_width << a.page_shift);
     if (j == 0) bad |= b0 != 0;
     if (j == a.groups - 1) bad |= b1 != a.requests;
-    a.waves[j] = 0;
+    z.waves[j] = 0;
   }
   if (__syncthreads_or(bad)) {
     if (tid == 0) {
@@ -338,54 +412,54 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(AttendArgs a) {
     return;
   }
   // waves along the rows that the requests of a group take one by one
-  for (int b = tid; b < a.requests && a.groups; b += kPlanThreads) {
-    const int t0 = a.row_start ? a.row_start[b] : b, t1 = a.row_start ? a.row_start[b + 1] : b + 1;
-    const int j = last_at_most(a.group_start, a.groups, b);
-    a.group_of[b] = j;
-    atomicAdd(&a.waves[j], row_waves((t1 - t0) * g));
+  for (int b = tid; b < a.requests && a.groups; b += threads) {
+    const int j = last_at_most(z.group_start, a.groups, b);
+    z.group_of[b] = j;
+    atomicAdd(&z.waves[j], row_waves((z.start(b + 1) - z.start(b)) * g));
   }
   __syncthreads();
   // units: a group's (its prefix, if that is shared), then a request's
   const int segments = a.groups + a.requests;
   int units = 0;
-  for (int s0 = 0; s0 < segments; s0 += kPlanThreads) {
+  for (int s0 = 0; s0 < segments; s0 += threads) {
     const int s = s0 + tid;
     int count = 0;
     if (s < a.groups) {
-      const int b0 = a.group_start[s], b1 = a.group_start[s + 1];
-      const int t0 = a.row_start ? a.row_start[b0] : b0, t1 = a.row_start ? a.row_start[b1] : b1;
-      const int rows = (t1 - t0) * g;
-      const bool shared = a.prefix_length[s] > 0 && row_waves(rows) * 4 <= a.waves[s] * 3;
-      a.waves[s] = shared ? 1 : 0;
+      const int rows = (z.start(z.group_start[s + 1]) - z.start(z.group_start[s])) * g;
+      const bool shared = z.prefix_length[s] > 0 && row_waves(rows) * 4 <= z.waves[s] * 3;
+      z.waves[s] = shared ? 1 : 0;
       count = shared ? (rows + kTileRows - 1) / kTileRows : 0;
     } else if (s < segments) {
       const int b = s - a.groups;
-      const int t0 = a.row_start ? a.row_start[b] : b, t1 = a.row_start ? a.row_start[b + 1] : b + 1;
-      count = ((t1 - t0) * g + kTileRows - 1) / kTileRows;
+      count = ((z.start(b + 1) - z.start(b)) * g + kTileRows - 1) / kTileRows;
     }
     int all;
     const int before = group_before(count, all, part);
-    if (s < segments) a.bounds[s] = units + before;
+    if (s < segments) z.bounds[s] = units + before;
     units += all;
   }
-  if (tid == 0) a.bounds[segments] = units;
+  if (tid == 0) z.bounds[segments] = units;
   __syncthreads();
   int64_t total = 0;
-  for (int u = tid; u < units; u += kPlanThreads) {
-    const int s = last_at_most(a.bounds, segments, u);
-    total += unit_work(a, s, u).cost;
+  UnitWork w;
+  int s = 0;
+  for (int u = tid; u < units; u += threads) {
+    s = last_at_most(z.bounds, segments, u);
+    w = unit_work(a, z, s, u);
+    total += w.cost;
   }
   group_before(total, total, part64);
   const int64_t fair = (total + a.split_slots - 1) / a.split_slots;
   const int chunk = (int)(fair < kMinSplitCost ? kMinSplitCost : fair > 0x7fffffff ? 0x7fffffff : fair);
   int items = 0, rows_acc = 0;
-  for (int u0 = 0; u0 < units; u0 += kPlanThreads) {
+  for (int u0 = 0; u0 < units; u0 += threads) {
     const int u = u0 + tid;
-    UnitWork w;
     int splits = 0, per = 1, partial = 0;
     if (u < units) {
-      const int s = last_at_most(a.bounds, segments, u);
-      w = unit_work(a, s, u);
+      if (units > threads) {  // else it is there
+        s = last_at_most(z.bounds, segments, u);
+        w = unit_work(a, z, s, u);
+      }
       splits = max(1, (w.cost + chunk - 1) / chunk);
       per = max(1, (w.steps + splits - 1) / splits);
       splits = max(1, (w.steps + per - 1) / per);
@@ -402,15 +476,14 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(AttendArgs a) {
       x.rows = w.it.rows;
       x.acc = partial ? acc : -1;
       x.splits = splits;
+      x.own = s >= a.groups;
       x.group_unit = -1;
       x.group_row = 0;
       x.pad = 0;
       if (w.group >= 0) {
-        const int b0 = a.group_start[w.group];
-        x.group_unit = a.bounds[w.group];
-        x.group_row = (a.row_start ? a.row_start[b0] : b0) * g;
+        x.group_unit = z.bounds[w.group];
+        x.group_row = z.start(z.group_start[w.group]) * g;
       }
-      x.own = u >= a.bounds[a.groups];
       a.units[u] = x;
       for (int i = 0; i < splits; ++i) {
         Item it = w.it;
@@ -432,6 +505,8 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(AttendArgs a) {
 
 // Joins the partial results of a request's unit, its own splits' and those of
 // its group's prefix: m = max m_i, l = sum l_i 2^(m_i - m), o likewise.
+constexpr int kJoinAtOnce = 8;
+
 template <bool FP16>
 __global__ void __launch_bounds__(256) join_kernel(AttendArgs a) {
   const int u = blockIdx.x / a.kv_heads, head = blockIdx.x % a.kv_heads;
@@ -451,25 +526,44 @@ __global__ void __launch_bounds__(256) join_kernel(AttendArgs a) {
   const float vs = a.vs ? a.vs[head] : 1.0f;
   for (int i = threadIdx.x; i < x.rows * quads; i += 256) {
     const int r = i / quads, c = i % quads;
+    const int row = x.row0 + r;
     float m = -INFINITY, l = 0.0f;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    auto add = [&](int64_t row) {
-      const int64_t at = row * a.kv_heads + head;
-      const float2 ml = a.ml[at];
-      if (ml.x == -INFINITY && ml.y == 0.0f) return;  // it has seen no key
-      const f32x4 y = *(const f32x4*)(a.acc + at * a.dim + c * 4);
-      const float top = fmaxf(m, ml.x), f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top),
-                  h = ml.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml.x - top);
-      o = o * f + y * h;
-      l = l * f + ml.y * h;
-      m = top;
+    // n partial results, `step` rows apart; eight are on their way at a time
+    auto add = [&](int first, int step, int n) {
+      for (int s0 = 0; s0 < n; s0 += kJoinAtOnce) {
+        float2 ml[kJoinAtOnce];
+        f32x4 y[kJoinAtOnce];
+#pragma unroll
+        for (int k = 0; k < kJoinAtOnce; ++k) {
+          const int64_t at = (int64_t)(first + min(s0 + k, n - 1) * step) * a.kv_heads + head;
+          ml[k] = a.ml[at];
+          y[k] = *(const f32x4*)(a.acc + at * a.dim + c * 4);
+        }
+        float top = m;
+#pragma unroll
+        for (int k = 0; k < kJoinAtOnce; ++k) {
+          if (s0 + k >= n) ml[k] = make_float2(-INFINITY, 0.0f);
+          top = fmaxf(top, ml[k].x);
+        }
+        const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top);
+        // (before the first key of a row l and o are 0, or NaN where a key was)
+        l = m == -INFINITY ? l : l * f;
+        o = m == -INFINITY ? o : o * f;
+        m = top;
+#pragma unroll
+        for (int k = 0; k < kJoinAtOnce; ++k) {
+          if (s0 + k >= n) continue;
+          const float h = ml[k].x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml[k].x - top);
+          l += ml[k].y * h;
+          o += y[k] * h;
+        }
+      }
     };
-    for (int s = 0; s < x.splits; ++s) add(x.acc + s * x.rows + r);
-    const int row = x.row0 + r;
+    add(x.acc + r, x.rows, x.splits);
     if (x.group_unit >= 0) {
-      const int tile = (row - x.group_row) / kTileRows;
-      const Unit y = a.units[x.group_unit + tile];
-      for (int s = 0; s < y.splits; ++s) add(y.acc + s * y.rows + row - y.row0);
+      const Unit y = a.units[x.group_unit + (row - x.group_row) / kTileRows];
+      add(y.acc + row - y.row0, y.rows, y.splits);
     }
     const float f = l > 0.0f || l != l ? vs / l : 0.0f;
     const uint32_t token = divide((uint32_t)row, a.share);
@@ -491,6 +585,10 @@ __global__ void __launch_bounds__(256) join_kernel(AttendArgs a) {
 }  // namespace
 
 hipError_t launch_tables(const TablesArgs& a, hipStream_t st) {
+  if (a.rows <= kFusedRows && a.num_tokens <= kFusedTokens) {
+    tables_fused_kernel<<<dim3(1), dim3(a.rows <= 256 && a.num_tokens <= 1024 ? 256 : kScanThreads), 0, st>>>(a);
+    return hipGetLastError();
+  }
   tables_scan_kernel<<<dim3(1), dim3(kScanThreads), 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
@@ -513,7 +611,11 @@ hipError_t launch_store(const StoreArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_attend_plan(const AttendArgs& a, hipStream_t st) {
-  plan_kernel<<<dim3(1), dim3(kPlanThreads), 0, st>>>(a);
+  const dim3 threads(a.unit_cap <= 256 ? 256 : kPlanThreads);
+  if (a.requests <= kPlanSmall && a.groups <= kPlanSmall)
+    plan_kernel<true><<<dim3(1), threads, 0, st>>>(a);
+  else
+    plan_kernel<false><<<dim3(1), threads, 0, st>>>(a);
   return hipGetLastError();
 }
 

@@ -9,7 +9,7 @@ come from torch's allocator.  Errors raise ``KvrError``.
 """
 from __future__ import annotations
 
-import ctypes
+import functools
 import struct
 from typing import NamedTuple, Optional
 
@@ -41,45 +41,56 @@ def _refuse(where: str, msg: str):
 
 
 def _vector(where: str, name: str, t, dtype, n, device) -> int:
-    """data_ptr of a contiguous vector of n values on the device."""
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device:
-        _refuse(where, f"{name} must be a {dtype} tensor on {device}")
-    if t.dim() != 1 or (n is not None and t.shape[0] != n) or (t.shape[0] > 1 and not t.is_contiguous()):
-        _refuse(where, f"{name} must be a contiguous vector" + ("" if n is None else f" of {n}"))
-    return t.data_ptr()
+    """data_ptr of a contiguous vector of n values (None: of any number) on the device."""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.device == device and t.is_contiguous() and \
+            t.dim() == 1 and (n is None or t.shape[0] == n):
+        return t.data_ptr()
+    _refuse(where, f"{name} must be a contiguous vector" + ("" if n is None else f" of {n}") + f" of {dtype} on "
+                   f"{device}")
 
 
 def _table(where: str, name: str, t, rows, device):
-    if not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or t.device != device:
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.int32 or t.device != device:
         _refuse(where, f"{name} must be a torch.int32 tensor on {device}")
-    if t.dim() != 2 or t.shape[0] != rows or (t.shape[1] > 1 and t.stride(1) != 1):
-        _refuse(where, f"{name} must be [{rows}, pages], the pages of a row contiguous")
+    if t.dim() != 2 or t.shape[0] != rows:
+        _refuse(where, f"{name} must be [{rows}, pages]")
     width = t.shape[1]
-    stride = t.stride(0)
+    stride, one = t.stride()
+    if width > 1 and one != 1:
+        _refuse(where, f"the pages of a row of {name} must be contiguous")
     if rows > 1 and stride < width:
         _refuse(where, f"the rows of {name} overlap")
     return t.data_ptr(), width, stride if stride > width else width
 
 
 def _gpu(where: str, name: str, t) -> torch.device:
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
         _refuse(where, f"{name} must be a tensor on a GPU")
     return t.device
 
 
-class _on:
-    """Makes the tensors' device current (nothing to do where it is)."""
+def _stream(device: torch.device) -> int:
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
-    def __init__(self, device: torch.device):
-        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
 
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
+def _here(device: torch.device) -> bool:
+    return device.index == torch._C._cuda_getDevice()
 
-    def __exit__(self, *a):
-        if self.guard is not None:
-            self.guard.__exit__(*a)
+
+@functools.lru_cache(maxsize=4096)
+def _tables_bytes(rows: int) -> int:
+    """Workspace of kvr_block_tables, which only the number of rows decides."""
+    return kvr_block_tables_workspace(TABLES_RECORD.pack(TABLES_RECORD.size, rows, 1, 1, 1, 0, 1, *[0] * 11))
+
+
+@functools.lru_cache(maxsize=65536)
+def _attention_bytes(code: int, kv_heads: int, dim: int, q_code: int, tokens: int, requests: int, groups: int,
+                     heads: int) -> int:
+    """Workspace of kvr_shared_attention, which these sizes decide (-1: refused)."""
+    return kvr_attention_workspace(
+        CACHE_RECORD.pack(CACHE_RECORD.size, code, 1, 1, kv_heads, dim, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0),
+        ATTENTION_RECORD.pack(ATTENTION_RECORD.size, q_code, tokens, requests, groups, heads, 0, 0, 1.0, 0, 0, 0, 0, 0,
+                              0, 0, 0, 1, 0, 0, 0, 0, 0, 0, 0, 0))
 
 
 def block_tables(held: torch.Tensor, delta: torch.Tensor, table: torch.Tensor, ring: torch.Tensor,
@@ -97,6 +108,9 @@ def block_tables(held: torch.Tensor, delta: torch.Tensor, table: torch.Tensor, r
     """
     where = "block_tables"
     device = _gpu(where, "held", held)
+    if not _here(device):
+        with torch.cuda.device(device):
+            return block_tables(held, delta, table, ring, state, page_size, num_tokens, base=base, in_place=in_place)
     rows = held.shape[0] if held.dim() == 1 else -1
     i32 = torch.int32
     p_held = _vector(where, "held", held, i32, None, device)
@@ -105,24 +119,22 @@ def block_tables(held: torch.Tensor, delta: torch.Tensor, table: torch.Tensor, r
     p_ring = _vector(where, "ring", ring, i32, None, device)
     p_state = _vector(where, "state", state, torch.int64, 3, device)
     p_table, width, stride = _table(where, "table", table, rows, device)
-    num_tokens = int(num_tokens)
-    if not 0 <= num_tokens < 1 << 31:
-        _refuse(where, "num_tokens must be in 0..2^31 - 1")
-    if not 0 < page_size <= 1024:
-        _refuse(where, "page_size must be a power of two in 1..1024")
-    with _on(device):
-        held_out = held if in_place else torch.empty_like(held)
-        state_out = state if in_place else torch.empty_like(state)
-        row_start = torch.empty(rows + 1, dtype=i32, device=device)
-        places = torch.empty((2, num_tokens), dtype=i32, device=device)
-        slots, positions = places.unbind(0)
-        args = bytearray(TABLES_RECORD.size)
-        TABLES_RECORD.pack_into(args, 0, TABLES_RECORD.size, rows, width, page_size, ring.shape[0], num_tokens, stride,
-                                p_held, p_delta, p_base, p_table, p_ring, p_state, held_out.data_ptr(),
-                                state_out.data_ptr(), row_start.data_ptr(), slots.data_ptr(), positions.data_ptr())
-        nbytes = kvr_block_tables_workspace(args)
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        kvr_block_tables(args, ws.data_ptr(), nbytes, torch.cuda.current_stream(device).cuda_stream)
+    if not 0 <= num_tokens < 1 << 31 or not 0 < page_size <= 1024:
+        _refuse(where, "num_tokens must be in 0..2^31 - 1, page_size a power of two in 1..1024")
+    nbytes = _tables_bytes(rows)
+    # one allocation: the outputs, then the workspace on a 256-byte boundary
+    ends = rows, 2 * rows + 1, 2 * rows + 1 + num_tokens, 2 * rows + 1 + 2 * num_tokens
+    whole = torch.empty((ends[3] + 63 & -64) + nbytes // 4, dtype=i32, device=device)
+    held_out, row_start, slots, positions, work = whole.tensor_split((*ends[:3], ends[3]))
+    if in_place:
+        held_out = held
+    state_out = state if in_place else torch.empty_like(state)
+    at = whole.data_ptr()
+    kvr_block_tables(
+        TABLES_RECORD.pack(TABLES_RECORD.size, rows, width, page_size, ring.shape[0], num_tokens, stride, p_held,
+                           p_delta, p_base, p_table, p_ring, p_state, p_held if in_place else at,
+                           state_out.data_ptr(), at + 4 * ends[0], at + 4 * ends[1], at + 4 * ends[2]),
+        at + 4 * (ends[3] + 63 & -64), nbytes, _stream(device))
     return BlockTables(held_out, state_out, row_start, slots, positions)
 
 
@@ -148,10 +160,8 @@ def _cache_args(where: str, kc: torch.Tensor, vc: torch.Tensor, ks, vs, device):
         _refuse(where, "the elements of a head must be contiguous")
     p_ks = 0 if ks is None else _vector(where, "k_scale", ks, torch.float32, heads, device)
     p_vs = 0 if vs is None else _vector(where, "v_scale", vs, torch.float32, heads, device)
-    args = bytearray(CACHE_RECORD.size)
-    CACHE_RECORD.pack_into(args, 0, CACHE_RECORD.size, code, pages, page, heads, dim, kc.data_ptr(), vc.data_ptr(),
-                           a0, a1, a2, b0, b1, b2, p_ks, p_vs)
-    return args
+    return CACHE_RECORD.pack(CACHE_RECORD.size, code, pages, page, heads, dim, kc.data_ptr(), vc.data_ptr(), a0, a1, a2,
+                             b0, b1, b2, p_ks, p_vs)
 
 
 def _status(where: str, status, device) -> int:
@@ -168,21 +178,22 @@ def cache_store(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache
     float8_e4m3fn cache holds x / scale[head]."""
     where = "cache_store"
     device = _gpu(where, "k", k)
+    if not _here(device):
+        with torch.cuda.device(device):
+            return cache_store(k, v, k_cache, v_cache, slots, k_scale=k_scale, v_scale=v_scale, status=status)
     cache = _cache_args(where, k_cache, v_cache, k_scale, v_scale, device)
-    if k.dtype != v.dtype or v.device != device or k.dim() != 3 or k.shape != v.shape or \
-            k.shape[1:] != k_cache.shape[2:]:
+    shape = k.shape
+    if k.dtype is not v.dtype or v.device != device or len(shape) != 3 or shape != v.shape or \
+            shape[1:] != k_cache.shape[2:]:
         _refuse(where, f"k and v must be [tokens, {k_cache.shape[2]}, {k_cache.shape[3]}], of one type, on {device}")
-    tokens = k.shape[0]
     a0, a1, a2 = k.stride()
     b0, b1, b2 = v.stride()
     if a2 != 1 or b2 != 1:
         _refuse(where, "the elements of a head must be contiguous")
-    p_slots = _vector(where, "slots", slots, torch.int32, tokens, device)
-    args = bytearray(STORE_RECORD.size)
-    STORE_RECORD.pack_into(args, 0, STORE_RECORD.size, DTYPE_CODES.get(k.dtype, -1), tokens, 0, k.data_ptr(),
-                           v.data_ptr(), a0, a1, b0, b1, p_slots, _status(where, status, device))
-    with _on(device):
-        kvr_cache_store(cache, args, torch.cuda.current_stream(device).cuda_stream)
+    p_slots = _vector(where, "slots", slots, torch.int32, shape[0], device)
+    kvr_cache_store(cache, STORE_RECORD.pack(STORE_RECORD.size, DTYPE_CODES.get(k.dtype, -1), shape[0], 0, k.data_ptr(),
+                                             v.data_ptr(), a0, a1, b0, b1, p_slots, _status(where, status, device)),
+                    _stream(device))
 
 
 def shared_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
@@ -207,47 +218,51 @@ def shared_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     """
     where = "shared_attention"
     device = _gpu(where, "q", q)
+    if not _here(device):
+        with torch.cuda.device(device):
+            return shared_attention(q, k_cache, v_cache, row_start, table, length, group_start, prefix_table,
+                                    prefix_length, scale=scale, k_scale=k_scale, v_scale=v_scale, out=out, lse=lse,
+                                    status=status)
     cache = _cache_args(where, k_cache, v_cache, k_scale, v_scale, device)
-    if q.dim() != 3 or q.shape[2] != k_cache.shape[3]:
-        _refuse(where, f"q must be [tokens, heads, {k_cache.shape[3]}]")
-    tokens, heads, dim = q.shape
-    requests = length.shape[0] if isinstance(length, torch.Tensor) and length.dim() == 1 else -1
+    _, _, kv_heads, dim = k_cache.shape
+    if q.dim() != 3 or q.shape[2] != dim:
+        _refuse(where, f"q must be [tokens, heads, {dim}]")
+    tokens, heads, _ = q.shape
     i32 = torch.int32
     p_length = _vector(where, "length", length, i32, None, device)
+    requests = length.shape[0]
     p_rows = 0 if row_start is None else _vector(where, "row_start", row_start, i32, requests + 1, device)
     p_table, width, stride = _table(where, "table", table, requests, device)
     groups = p_start = p_prefix = p_plen = pwidth = pstride = 0
     if prefix_length is not None or group_start is not None or prefix_table is not None:
         if prefix_length is None or group_start is None or prefix_table is None:
             _refuse(where, "group_start, prefix_table and prefix_length go together")
-        groups = prefix_length.shape[0] if prefix_length.dim() == 1 else -1
         p_plen = _vector(where, "prefix_length", prefix_length, i32, None, device)
+        groups = prefix_length.shape[0]
         p_start = _vector(where, "group_start", group_start, i32, groups + 1, device)
         p_prefix, pwidth, pstride = _table(where, "prefix_table", prefix_table, groups, device)
-    with _on(device):
-        if out is None:
-            out = torch.empty_like(q, memory_format=torch.contiguous_format)
-        elif out.shape != q.shape or out.dtype != q.dtype or out.device != device:
-            _refuse(where, "out must be like q")
-        q0, q1, q2 = q.stride()
-        o0, o1, o2 = out.stride()
-        if q2 != 1 or o2 != 1:
-            _refuse(where, "the elements of a head must be contiguous")
-        p_lse = 0
-        if lse is not None:
-            if lse.dtype != torch.float32 or lse.device != device or lse.shape != (tokens, heads) or \
-                    not lse.is_contiguous():
-                _refuse(where, f"lse must be a contiguous float32 [{tokens}, {heads}] on {device}")
-            p_lse = lse.data_ptr()
-        args = bytearray(ATTENTION_RECORD.size)
-        ATTENTION_RECORD.pack_into(
-            args, 0, ATTENTION_RECORD.size, DTYPE_CODES.get(q.dtype, -1), tokens, requests, groups, heads, width,
-            pwidth, dim ** -0.5 if scale is None else float(scale), 0, q.data_ptr(), out.data_ptr(), p_lse, q0, q1,
-            o0, o1, p_rows, p_length, p_table, p_start, p_prefix, p_plen, stride, pstride,
-            _status(where, status, device))
-        nbytes = kvr_attention_workspace(cache, args)
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        kvr_shared_attention(cache, args, ws.data_ptr(), nbytes, torch.cuda.current_stream(device).cuda_stream)
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    elif out.shape != q.shape or out.dtype != q.dtype or out.device != device:
+        _refuse(where, "out must be like q")
+    q0, q1, q2 = q.stride()
+    o0, o1, o2 = out.stride()
+    if q2 != 1 or o2 != 1:
+        _refuse(where, "the elements of a head must be contiguous")
+    p_lse = 0
+    if lse is not None:
+        if lse.dtype != torch.float32 or lse.device != device or lse.shape != (tokens, heads) or \
+                not lse.is_contiguous():
+            _refuse(where, f"lse must be a contiguous float32 [{tokens}, {heads}] on {device}")
+        p_lse = lse.data_ptr()
+    code = DTYPE_CODES.get(q.dtype, -1)
+    args = ATTENTION_RECORD.pack(ATTENTION_RECORD.size, code, tokens, requests, groups, heads, width, pwidth,
+                                 dim ** -0.5 if scale is None else scale, 0, q.data_ptr(), out.data_ptr(), p_lse, q0,
+                                 q1, o0, o1, p_rows, p_length, p_table, p_start, p_prefix, p_plen, stride, pstride,
+                                 _status(where, status, device))
+    nbytes = _attention_bytes(DTYPE_CODES[k_cache.dtype], kv_heads, dim, code, tokens, requests, groups, heads)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    kvr_shared_attention(cache, args, ws.data_ptr(), nbytes, _stream(device))
     return out
 
 
