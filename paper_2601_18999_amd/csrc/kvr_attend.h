@@ -93,7 +93,7 @@ __device__ __forceinline__ int swizzle_v(int row) {
 // the larger (the sum) of a lane's value and that of the same row's lane in the other half wave
 __device__ __forceinline__ float half_max(float x) {
   const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+  return __builtin_elementwise_maximum(__uint_as_float(s[0]), __uint_as_float(s[1]));
 }
 __device__ __forceinline__ float half_sum(float x) {
   const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -427,6 +427,14 @@ __device__ __forceinline__ bool holds_odd(const char* tile, int lane) {
 
 typedef const __attribute__((address_space(4))) AttendArgs Args;
 
+// A tile that every row sees to its end, and one that some may not.
+struct Plain {
+  static constexpr bool edge = false;
+};
+struct Edge {
+  static constexpr bool edge = true;
+};
+
 template <int D, class T, bool FP8, int RW>
 __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it, int head, float scale, char* lds) {
   typedef Shape<D, RW> S;
@@ -496,10 +504,25 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
     if (bad && a.status) atomicOr(a.status, (uint32_t)KVR_DEV_BAD_PAGE);
     return p.key0 + KT <= p.end && !__any(bad);
   };
-  // the scores of a tile, p, and their product with V
-  auto seen_of = [&](const Place& p) { return (p.shared ? p.end : min(limit, p.end)) - p.key0; };
-  // a row of this tile may stand before some of its own keys
-  auto edge_of = [&](const Place& p) { return !p.shared && p.key0 + KT > limit0; };
+  // Tiles before `plain` are seen by all rows: no masks in their loop, and no
+  // second way to multiply V, which would keep two copies of the results.
+  const int plain = max(0, min(tiles, (it.prefix_steps + limit0 / kStepKeys - it.step0) * (kStepKeys / KT)));
+  // scores to p
+  auto weigh = [&](auto kind, const Place& p, f32x16(&s)[KB]) {
+    const int seen = (kind.edge && !p.shared ? min(limit, p.end) : p.end) - p.key0;
+    x.softmax(s, kind.edge || p.key0 + KT > p.end, seen, scale, hh);
+  };
+  // and their product with V
+  auto multiply = [&](auto kind, const Place& p, const char* vt, const f32x16(&s)[KB]) {
+    if constexpr (kind.edge) {
+      const int seen = (p.shared ? p.end : min(limit, p.end)) - p.key0;
+      if (holds_odd<T, S::kTileBytes>(vt, lane)) {
+        x.values_seen(vt, s, seen, hh);
+        return;
+      }
+    }
+    x.values(vt, s, lane);
+  };
 
   if constexpr (RW == 1 && !FP8) {
     typedef Direct<D, 1> L;
@@ -528,7 +551,7 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
       L::template load<true>(a, kc, page, whole, p.key0, p.end, 0, lane, k_to);
       if (mine > 1) load_ids(1);
       L::template load<false>(a, vc, page, whole, p.key0, p.end, 0, lane, v_to);
-      for (int j = 0; j < mine; ++j) {
+      auto round = [&](auto kind, int j) {
         // in flight, oldest first: K of this tile, the next one's page numbers, V of this tile
         const bool more = j + 1 < mine;
         const Place p1 = place(wave + 4 * (j + 1));
@@ -543,23 +566,21 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
           L::template load<true>(a, kc, page, whole1, p1.key0, p1.end, 0, lane, k_to);
           if (j + 2 < mine) load_ids(j + 2);
         }
-        const bool edge = edge_of(p);
-        const int seen = seen_of(p);
-        x.softmax(s, edge || p.key0 + KT > p.end, seen, scale, hh);
+        weigh(kind, p, s);
         if (j + 2 < mine)
           wait_loads<N + 1>();
         else if (more)
           wait_loads<N>();
         else
           wait_loads<0>();
-        if (edge && holds_odd<T, S::kTileBytes>(vt, lane))
-          x.values_seen(vt, s, seen, hh);
-        else
-          x.values(vt, s, lane);
+        multiply(kind, p, vt, s);
         wait_lds();
         if (more) L::template load<false>(a, vc, page, whole1, p1.key0, p1.end, 0, lane, v_to);
         p = p1;
-      }
+      };
+      int j = 0;
+      for (; j < mine && wave + 4 * j < plain; ++j) round(Plain(), j);
+      for (; j < mine; ++j) round(Edge(), j);
     }
   } else if constexpr (RW == 1) {
     typedef Widened<D, T, 1> L;
@@ -573,66 +594,64 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
     pages(p, row0, L::kRows, page);
     ld.fetch(a, kc, vc, page, whole_of(p, page), p.key0, p.end, lane);
     pages(p1, row0, L::kRows, page);
-    for (int j = 0; j < mine; ++j) {
+    auto round = [&](auto kind, int j) {
       ld.store(kt, vt, lane);
       ld.fetch(a, kc, vc, page, whole_of(p1, page), p1.key0, p1.end, lane);
       const Place p2 = place(wave + 4 * (j + 2));
       pages(p2, row0, L::kRows, page);
       f32x16 s[KB];
       x.scores(kt, s, n, hh);
-      const bool edge = edge_of(p);
-      const int seen = seen_of(p);
-      x.softmax(s, edge || p.key0 + KT > p.end, seen, scale, hh);
-      if (edge && holds_odd<T, S::kTileBytes>(vt, lane))
-        x.values_seen(vt, s, seen, hh);
-      else
-        x.values(vt, s, lane);
+      weigh(kind, p, s);
+      multiply(kind, p, vt, s);
       p = p1;
       p1 = p2;
-    }
+    };
+    int j = 0;
+    for (; j < mine && wave + 4 * j < plain; ++j) round(Plain(), j);
+    for (; j < mine; ++j) round(Edge(), j);
   } else {
     // two buffers; one barrier a tile
-    char* group = lds + kg * 4 * S::kTileBytes;
-    const int rounds = (tiles + KG - 1) / KG;
-    Place p = place(kg), p1 = place(KG + kg);
-    auto work = [&](const char* kt, const char* vt) {
-      if (p.key0 >= p.end) return;
+    static_assert(KG == 1, "the waves share every tile");
+    Place p = place(0), p1 = place(1);
+    const bool idle = wave * 32 >= it.rows;  // no row: it only loads
+    auto work = [&](auto kind, const char* kt, const char* vt) {
+      if (idle) return;
       f32x16 s[KB];
       x.scores(kt, s, n, hh);
-      const bool edge = edge_of(p);
-      const int seen = seen_of(p);
-      x.softmax(s, edge || p.key0 + KT > p.end, seen, scale, hh);
-      if (edge && holds_odd<T, S::kTileBytes>(vt, lane))
-        x.values_seen(vt, s, seen, hh);
-      else
-        x.values(vt, s, lane);
+      weigh(kind, p, s);
+      multiply(kind, p, vt, s);
     };
     if constexpr (!FP8) {
       typedef Direct<D, RW> L;
       int page[L::kN];
       const int row0 = L::first(rw, lane), step = RW * L::kRows;
-      const uint32_t to = lds_offset(group);
-      pages(p, row0, step, page);
-      bool whole = whole_of(p, page);
-      L::template load<true>(a, kc, page, whole, p.key0, p.end, rw, lane, to);
-      L::template load<false>(a, vc, page, whole, p.key0, p.end, rw, lane, to + S::kTileBytes);
-      pages(p1, row0, step, page);
-      for (int round = 0; round < rounds; ++round) {
+      const uint32_t to = lds_offset(lds);
+      if (tiles > 0) {
+        pages(p, row0, step, page);
+        bool whole = whole_of(p, page);
+        L::template load<true>(a, kc, page, whole, p.key0, p.end, rw, lane, to);
+        L::template load<false>(a, vc, page, whole, p.key0, p.end, rw, lane, to + S::kTileBytes);
+        pages(p1, row0, step, page);
+      }
+      auto round = [&](auto kind, int j) {
         wait_loads<0>();
         barrier();
-        const uint32_t b1 = (round + 1 & 1) * 2 * S::kTileBytes;
-        const char* kt = group + (round & 1) * 2 * S::kTileBytes;
-        const Place p2 = place((round + 2) * KG + kg);
-        if (round + 1 < rounds) {
-          whole = whole_of(p1, page);
+        const uint32_t b1 = (j + 1 & 1) * 2 * S::kTileBytes;
+        const char* kt = lds + (j & 1) * 2 * S::kTileBytes;
+        const Place p2 = place(j + 2);
+        if (j + 1 < tiles) {
+          const bool whole = whole_of(p1, page);
           L::template load<true>(a, kc, page, whole, p1.key0, p1.end, rw, lane, to + b1);
           L::template load<false>(a, vc, page, whole, p1.key0, p1.end, rw, lane, to + b1 + S::kTileBytes);
           pages(p2, row0, step, page);
         }
-        work(kt, kt + S::kTileBytes);
+        work(kind, kt, kt + S::kTileBytes);
         p = p1;
         p1 = p2;
-      }
+      };
+      int j = 0;
+      for (; j < plain; ++j) round(Plain(), j);
+      for (; j < tiles; ++j) round(Edge(), j);
     } else {
       typedef Widened<D, T, RW> L;
       int page[L::kN];
@@ -641,19 +660,22 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
       pages(p, row0, L::kRows, page);
       ld.fetch(a, kc, vc, page, whole_of(p, page), p.key0, p.end, thread);
       pages(p1, row0, L::kRows, page);
-      ld.store(group, group + S::kTileBytes, thread);
-      for (int round = 0; round < rounds; ++round) {
+      ld.store(lds, lds + S::kTileBytes, thread);
+      auto round = [&](auto kind, int j) {
         barrier();
-        char* kt = group + (round & 1) * 2 * S::kTileBytes;
-        char* kt1 = group + (round + 1 & 1) * 2 * S::kTileBytes;
-        const Place p2 = place((round + 2) * KG + kg);
+        char* kt = lds + (j & 1) * 2 * S::kTileBytes;
+        char* kt1 = lds + (j + 1 & 1) * 2 * S::kTileBytes;
+        const Place p2 = place(j + 2);
         ld.fetch(a, kc, vc, page, whole_of(p1, page), p1.key0, p1.end, thread);
         pages(p2, row0, L::kRows, page);
-        work(kt, kt + S::kTileBytes);
+        work(kind, kt, kt + S::kTileBytes);
         ld.store(kt1, kt1 + S::kTileBytes, thread);
         p = p1;
         p1 = p2;
-      }
+      };
+      int j = 0;
+      for (; j < plain; ++j) round(Plain(), j);
+      for (; j < tiles; ++j) round(Edge(), j);
     }
   }
   const float m = x.m, l = half_sum(x.l);

@@ -505,7 +505,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(AttendArgs a) {
 
 // Joins the partial results of a request's unit, its own splits' and those of
 // its group's prefix: m = max m_i, l = sum l_i 2^(m_i - m), o likewise.
-constexpr int kJoinAtOnce = 8;
+constexpr int kJoinAtOnce = 4;
 
 template <bool FP16>
 __global__ void __launch_bounds__(256) join_kernel(AttendArgs a) {
