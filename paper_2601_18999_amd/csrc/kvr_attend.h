@@ -152,6 +152,11 @@ __device__ __forceinline__ void load16_to_lds(global_bytes from, uint32_t to) {
 __device__ __forceinline__ void load4_to_lds(global_ints from, uint32_t to) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(to) : "memory");
 }
+// The same with one base for the wave and 32-bit offsets.
+__device__ __forceinline__ void load16_to_lds(uint64_t base, uint32_t offset, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(to)
+               : "memory");
+}
 template <int N>
 __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
@@ -207,6 +212,36 @@ struct Direct {
     }
 #pragma unroll
     for (int i = 0; i < kN; ++i) load16_to_lds(p[i], to + (i * RW + wave) * 1024);
+  }
+
+  // Pages of kRows tokens or more: the rows of one load stand in one page, so
+  // a load has one base, in scalar registers, and lane offsets that stay the
+  // same from tile to tile.  kOffsets of them: the swizzle of load i's rows.
+  static constexpr int kOffsets = RW * kRows % 16 ? 2 : 1;
+  static_assert(RW == 1 || RW * kRows % 8 == 0, "two offsets are enough");
+  struct Offsets {
+    uint32_t k[kOffsets], v;
+  };
+  static __device__ __forceinline__ Offsets offsets(const AttendArgs& a, int wave, int lane) {
+    Offsets o;
+#pragma unroll
+    for (int i = 0; i < kOffsets; ++i)
+      o.k[i] = lane / kChunks * a.kc_slot +
+               (((lane % kChunks) ^ swizzle_k<D>(i * RW * kRows + first(wave, lane))) << 4);
+    o.v = lane / kChunks * a.vc_slot + (((lane % kChunks) ^ swizzle_v<D>(first(wave, lane))) << 4);
+    return o;
+  }
+  template <bool KEYS>
+  static __device__ __forceinline__ void load(const AttendArgs& a, global_bytes base, const int (&page)[kN],
+                                              const Offsets& o, int key0, int wave, uint32_t to) {
+    const uint32_t page_bytes = KEYS ? a.kc_page : a.vc_page, slot_bytes = KEYS ? a.kc_slot : a.vc_slot;
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const uint32_t slot = (uint32_t)(key0 + (i * RW + wave) * kRows) & (uint32_t)a.page_mask;
+      const uint32_t at = (uint32_t)__builtin_amdgcn_readfirstlane(page[i]);
+      const uint64_t from = (uint64_t)base + (uint64_t)at * page_bytes + (uint64_t)slot * slot_bytes;
+      load16_to_lds(from, KEYS ? o.k[i % kOffsets] : o.v, to + (i * RW + wave) * 1024);
+    }
   }
 };
 
@@ -626,11 +661,21 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
       int page[L::kN];
       const int row0 = L::first(rw, lane), step = RW * L::kRows;
       const uint32_t to = lds_offset(lds);
+      const typename L::Offsets offsets = L::offsets(a, rw, lane);
+      const bool uniform = (1 << a.page_shift) >= L::kRows;
+      auto load = [&](const Place& q, uint32_t at) {
+        const bool whole = whole_of(q, page);
+        if (whole && uniform) {
+          L::template load<true>(a, kc, page, offsets, q.key0, rw, at);
+          L::template load<false>(a, vc, page, offsets, q.key0, rw, at + S::kTileBytes);
+        } else {
+          L::template load<true>(a, kc, page, whole, q.key0, q.end, rw, lane, at);
+          L::template load<false>(a, vc, page, whole, q.key0, q.end, rw, lane, at + S::kTileBytes);
+        }
+      };
       if (tiles > 0) {
         pages(p, row0, step, page);
-        bool whole = whole_of(p, page);
-        L::template load<true>(a, kc, page, whole, p.key0, p.end, rw, lane, to);
-        L::template load<false>(a, vc, page, whole, p.key0, p.end, rw, lane, to + S::kTileBytes);
+        load(p, to);
         pages(p1, row0, step, page);
       }
       auto round = [&](auto kind, int j) {
@@ -640,9 +685,7 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
         const char* kt = lds + (j & 1) * 2 * S::kTileBytes;
         const Place p2 = place(j + 2);
         if (j + 1 < tiles) {
-          const bool whole = whole_of(p1, page);
-          L::template load<true>(a, kc, page, whole, p1.key0, p1.end, rw, lane, to + b1);
-          L::template load<false>(a, vc, page, whole, p1.key0, p1.end, rw, lane, to + b1 + S::kTileBytes);
+          load(p1, to + b1);
           pages(p2, row0, step, page);
         }
         work(kind, kt, kt + S::kTileBytes);
