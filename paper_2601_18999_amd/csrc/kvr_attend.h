@@ -312,6 +312,9 @@ __device__ __forceinline__ s16x4 round4(float a, float b, float c, float d) {
   return __builtin_bit_cast(s16x4, __builtin_convertvector(x, typename T::x4));
 }
 
+// kinds of instructions for the scheduler
+constexpr int kProducts = 0x8, kReads = 0x100;
+
 constexpr float kSlack = 8.0f;  // p < 2^8: far from the largest half, and l from the largest float
 
 // A wave's 32 rows: queries, running maximum (log2 units) and sum, results.
@@ -321,21 +324,58 @@ struct Rows {
   f32x16 o[D / 32];
   float m, l;
 
-  // Scores of KB * 32 keys in LDS.
-  template <int KB>
-  __device__ __forceinline__ void scores(const char* kt, f32x16 (&s)[KB], int n, int hh) {
+  static __device__ __forceinline__ s16x8 key_chunk(const char* kt, int row, int i, int hh) {
+    return *(const s16x8*)(kt + row * 2 * D + (((2 * i + hh) ^ swizzle_k<D>(row)) << 4));
+  }
+
+  // Elements c * 32 .. of 16 keys (step q of the tile), as the second product
+  // takes them.  The transposing read: 16 lanes name four rows of 16 elements,
+  // four lanes a row, and lane i of them gets column i.
+  static __device__ __forceinline__ s16x8 value_chunk(const char* vt, int q, int c, int lane) {
+    const int hh = lane >> 5, sl = lane & 15, dh = (lane >> 4) & 1;
+    s16x4 x[2];
 #pragma unroll
-    for (int b = 0; b < KB; ++b)
+    for (int j = 0; j < 2; ++j) {
+      const int vr = q * 16 + j * 8 + hh * 4 + sl / 4;
+      const int ch = c * 4 + dh * 2 + (sl & 3) / 2;
+      const char* p8 = vt + vr * 2 * D + ((ch ^ swizzle_v<D>(vr)) << 4) + (sl & 1) * 8;
+      x[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(lds_char*)p8);
+    }
+    return __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+
+  // Scores of KB * 32 keys in LDS.  The reads of a block of 32 keys are on
+  // their way while the block before it is multiplied (a read takes as long as
+  // several products), and the first values' while the last one is.
+  template <int KB, bool VALUES>
+  __device__ __forceinline__ void scores(const char* kt, const char* vt, f32x16 (&s)[KB], s16x8 (&first)[D / 32], int n,
+                                         int hh) {
+    constexpr int N = D / 16, V = VALUES ? D / 32 : 0;
+    s16x8 f[2][N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[0][i] = key_chunk(kt, n, i, hh);
+    __builtin_amdgcn_sched_group_barrier(kReads, N, 0);
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
 #pragma unroll
-    for (int b = 0; b < KB; ++b)
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) {
-        const int kr = b * 32 + n;
-        const s16x8 x = *(const s16x8*)(kt + kr * 2 * D + (((2 * i + hh) ^ swizzle_k<D>(kr)) << 4));
-        s[b] = T::mfma(x, q[i], s[b]);
+      for (int i = 0; i < N; ++i) {
+        if (b + 1 < KB)
+          f[(b + 1) & 1][i] = key_chunk(kt, (b + 1) * 32 + n, i, hh);
+        else if (i < V)
+          first[i] = value_chunk(vt, 0, i, n + 32 * hh);
+        s[b] = T::mfma(f[b & 1][i], q[i], s[b]);
       }
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        __builtin_amdgcn_sched_group_barrier(kProducts, 1, 0);
+        if (b + 1 < KB)
+          __builtin_amdgcn_sched_group_barrier(kReads, 1, 0);
+        else if (i < V)
+          __builtin_amdgcn_sched_group_barrier(kReads, 2, 0);
+      }
+    }
   }
 
   // Scores to p; keys from `seen` on are hidden where `edge` says that there are such.
@@ -380,33 +420,26 @@ struct Rows {
       }
   }
 
-  // O^T += V^T P^T
-  template <int KB>
-  __device__ __forceinline__ void values(const char* vt, const f32x16 (&s)[KB], int lane) {
-    const int hh = lane >> 5, sl = lane & 15, dh = (lane >> 4) & 1;
+  // O^T += V^T P^T; with VALUES the first step's values are there.
+  template <int KB, bool VALUES>
+  __device__ __forceinline__ void values(const char* vt, const f32x16 (&s)[KB], const s16x8 (&first)[D / 32],
+                                         int lane) {
+    constexpr int N = D / 32;
+    s16x8 f[2][N];
 #pragma unroll
-    for (int b = 0; b < KB; ++b)
+    for (int c = 0; c < N; ++c) f[0][c] = VALUES ? first[c] : value_chunk(vt, 0, c, lane);
 #pragma unroll
-      for (int st = 0; st < 2; ++st) {
-        const s16x4 lo = round4<T>(s[b][8 * st], s[b][8 * st + 1], s[b][8 * st + 2], s[b][8 * st + 3]);
-        const s16x4 hi = round4<T>(s[b][8 * st + 4], s[b][8 * st + 5], s[b][8 * st + 6], s[b][8 * st + 7]);
-        const s16x8 p = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    for (int q = 0; q < 2 * KB; ++q) {
+      const int b = q / 2, st = q % 2;
+      const s16x4 lo = round4<T>(s[b][8 * st], s[b][8 * st + 1], s[b][8 * st + 2], s[b][8 * st + 3]);
+      const s16x4 hi = round4<T>(s[b][8 * st + 4], s[b][8 * st + 5], s[b][8 * st + 6], s[b][8 * st + 7]);
+      const s16x8 p = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
-          s16x4 x[2];
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            // the transposing read: 16 lanes name four rows of 16 elements, four
-            // lanes a row, and lane i of them gets column i
-            const int vr = b * 32 + st * 16 + j * 8 + hh * 4 + sl / 4;
-            const int ch = c * 4 + dh * 2 + (sl & 3) / 2;
-            const char* p8 = vt + vr * 2 * D + ((ch ^ swizzle_v<D>(vr)) << 4) + (sl & 1) * 8;
-            x[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (__attribute__((address_space(3))) s16x4*)(lds_char*)p8);
-          }
-          o[c] = T::mfma(__builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7), p, o[c]);
-        }
+      for (int c = 0; c < N; ++c) {
+        if (q + 1 < 2 * KB) f[(q + 1) & 1][c] = value_chunk(vt, q + 1, c, lane);
+        o[c] = T::mfma(f[q & 1][c], p, o[c]);
       }
+    }
   }
 
   // The same key by key, for a tile whose V holds an infinity or NaN that some
@@ -548,7 +581,7 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
     x.softmax(s, kind.edge || p.key0 + KT > p.end, seen, scale, hh);
   };
   // and their product with V
-  auto multiply = [&](auto kind, const Place& p, const char* vt, const f32x16(&s)[KB]) {
+  auto multiply = [&](auto kind, const Place& p, const char* vt, const f32x16(&s)[KB], const s16x8(&first)[DB]) {
     if constexpr (kind.edge) {
       const int seen = (p.shared ? p.end : min(limit, p.end)) - p.key0;
       if (holds_odd<T, S::kTileBytes>(vt, lane)) {
@@ -556,7 +589,7 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
         return;
       }
     }
-    x.values(vt, s, lane);
+    x.template values<KB, (RW > 1)>(vt, s, first, lane);
   };
 
   if constexpr (RW == 1 && !FP8) {
@@ -593,8 +626,9 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
         bool whole1 = false;
         wait_loads<N>();
         f32x16 s[KB];
+        s16x8 first[DB];
         if (more) read_ids(j + 1);
-        x.scores(kt, s, n, hh);
+        x.template scores<KB, false>(kt, vt, s, first, n, hh);
         wait_lds();
         if (more) {
           whole1 = whole_of(p1, page);
@@ -608,7 +642,7 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
           wait_loads<N>();
         else
           wait_loads<0>();
-        multiply(kind, p, vt, s);
+        multiply(kind, p, vt, s, first);
         wait_lds();
         if (more) L::template load<false>(a, vc, page, whole1, p1.key0, p1.end, 0, lane, v_to);
         p = p1;
@@ -635,9 +669,10 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
       const Place p2 = place(wave + 4 * (j + 2));
       pages(p2, row0, L::kRows, page);
       f32x16 s[KB];
-      x.scores(kt, s, n, hh);
+      s16x8 first[DB];
+      x.template scores<KB, (RW > 1)>(kt, vt, s, first, n, hh);
       weigh(kind, p, s);
-      multiply(kind, p, vt, s);
+      multiply(kind, p, vt, s, first);
       p = p1;
       p1 = p2;
     };
@@ -652,9 +687,10 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
     auto work = [&](auto kind, const char* kt, const char* vt) {
       if (idle) return;
       f32x16 s[KB];
-      x.scores(kt, s, n, hh);
+      s16x8 first[DB];
+      x.template scores<KB, (RW > 1)>(kt, vt, s, first, n, hh);
       weigh(kind, p, s);
-      multiply(kind, p, vt, s);
+      multiply(kind, p, vt, s, first);
     };
     if constexpr (!FP8) {
       typedef Direct<D, RW> L;
