@@ -688,9 +688,16 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
       if (idle) return;
       f32x16 s[KB];
       s16x8 first[DB];
+      // a wave that multiplies goes first: two waves of a SIMD else fall into
+      // step, and the matrix and the vector unit wait for each other (9,216 new
+      // tokens: 731 -> 708 us)
+      __builtin_amdgcn_s_setprio(1);
       x.template scores<KB, (RW > 1)>(kt, vt, s, first, n, hh);
+      __builtin_amdgcn_s_setprio(0);
       weigh(kind, p, s);
+      __builtin_amdgcn_s_setprio(1);
       multiply(kind, p, vt, s, first);
+      __builtin_amdgcn_s_setprio(0);
     };
     if constexpr (!FP8) {
       typedef Direct<D, RW> L;
