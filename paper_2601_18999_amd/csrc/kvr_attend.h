@@ -29,7 +29,7 @@
 // the rounded result; the sum l adds the unrounded p.
 #pragma once
 
-#include "kvr_serve.h"
+#include "kvr_plan.h"
 
 namespace kvr {
 namespace {
@@ -853,8 +853,25 @@ template <int D, class T, bool FP8>
 __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(AttendArgs a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const int item = blockIdx.x / a.kv_heads, head = blockIdx.x % a.kv_heads;
-  if (item >= a.hdr->items) return;
-  const Item it = a.items[item];
+  Item it;
+  if (a.fused) {
+    static_assert(4 * plan_words(kPlanFused) + (int)sizeof(Item) <= attend_lds<D>(), "the plan's LDS");
+    Item* mine = (Item*)(lds + 4 * plan_words(kPlanFused));
+    const int items = make_plan<kPlanFused>(a, (int*)lds, blockIdx.x == 0, [&](int i, const Item& x) {
+      if (i == item) *mine = x;
+    });
+    if (item >= items) return;
+    __syncthreads();
+    it = *mine;
+    // the same in all lanes: in scalar registers
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(Item) / 4); ++i)
+      ((int*)&it)[i] = __builtin_amdgcn_readfirstlane(((int*)&it)[i]);
+    __syncthreads();
+  } else {
+    if (item >= a.hdr->items) return;
+    it = a.items[item];
+  }
   const float scale = FP8 && a.ks ? a.scale_log2 * a.ks[head] : a.scale_log2;
   if (it.rows > 32)
     attend_item<D, T, FP8, 4>(a, it, head, scale, lds);

@@ -1,7 +1,7 @@
 // kvr_serve.hip - kernels of the serving operators but the attention itself:
 // page tables and slot maps, the store of new keys and values, and the plan
 // and the join of the attention.
-#include "kvr_serve.h"
+#include "kvr_plan.h"
 
 namespace kvr {
 namespace {
@@ -9,49 +9,6 @@ namespace {
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-// Sum over the lanes before this one, and (by reference) over all lanes.
-template <class V>
-__device__ __forceinline__ V wave_before(V x, V& all) {
-  const int lane = threadIdx.x & 63;
-  V s = x;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const V y = __shfl_up(s, d);
-    if (lane >= d) s += y;
-  }
-  all = __shfl(s, 63);
-  return s - x;
-}
-
-// The same over a workgroup of up to 16 waves; `part` is 16 values of LDS.
-// Every thread of the workgroup calls it.
-template <class V>
-__device__ __forceinline__ V group_before(V x, V& all, V* part) {
-  const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6, lane = threadIdx.x & 63;
-  V w;
-  const V s = wave_before(x, w);
-  __syncthreads();
-  if (lane == 0) part[wave] = w;
-  __syncthreads();
-  const V y = lane < waves ? part[lane] : V(0);
-  const V before = wave_before(y, all);
-  return s + __shfl(before, wave);
-}
-
-// Largest i of [0, n) with start[i] <= x, for start ascending and start[0] <= x.
-template <class P>
-__device__ __forceinline__ int last_at_most(P start, int n, int x) {
-  int lo = 0, hi = n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (start[mid] <= x)
-      lo = mid;
-    else
-      hi = mid;
-  }
-  return lo;
-}
 
 // ---------------------------------------------------------------- page tables
 
@@ -192,18 +149,35 @@ __global__ void __launch_bounds__(kScanThreads) tables_fused_kernel(TablesArgs a
 constexpr int kFillThreads = 256, kFillTokens = 4;  // tokens of a thread
 
 // Slots and positions of the new tokens, the pages they gain, and the pages
-// that are given back.
+// that are given back.  With STAGED, up to kStagedRows rows, the sums are
+// searched in LDS (FILL_FIGURE).
+constexpr int kStagedRows = 4096;
+template <bool STAGED>
 __global__ void __launch_bounds__(kFillThreads) tables_fill_kernel(TablesArgs a) {
+  __shared__ int staged[STAGED ? kStagedRows + 1 : 1];
   const TablesHdr h = *a.hdr;
   const int t0 = blockIdx.x * kFillThreads * kFillTokens;
+  if constexpr (STAGED) {
+    if (t0 < a.num_tokens)
+      for (int r = threadIdx.x; r <= a.rows; r += kFillThreads) staged[r] = a.row_start[r];
+    __syncthreads();
+  }
+  const int* row_start = STAGED ? staged : a.row_start;
 #pragma unroll
   for (int i = 0; i < kFillTokens; ++i) {
     const int t = t0 + i * kFillThreads + threadIdx.x;
-    if (t < a.num_tokens) place_token(a, h, a.row_start, a.gain_at, t);
+    if (t < a.num_tokens) place_token(a, h, row_start, a.gain_at, t);
   }
-  if (h.rejected) return;
+  if (h.rejected || h.give == 0) return;
+  const int* give_at = a.give_at;
+  if constexpr (STAGED) {
+    __syncthreads();
+    for (int r = threadIdx.x; r < a.rows; r += kFillThreads) staged[r] = a.give_at[r];
+    __syncthreads();
+    give_at = staged;
+  }
   for (int g = blockIdx.x * kFillThreads + threadIdx.x; g < h.give; g += gridDim.x * kFillThreads)
-    drop_page(a, h, a.give_at, g);
+    drop_page(a, h, give_at, g);
 }
 
 // ---------------------------------------------------------------- cache store
@@ -266,239 +240,12 @@ __global__ void __launch_bounds__(256) store_kernel(StoreArgs a) {
 
 // ---------------------------------------------------------------- attention: the plan
 
-constexpr int kPlanThreads = 1024;
-constexpr int kPlanSmall = 1024;  // requests, groups: their lengths then stand in LDS
-constexpr int kMinSplitCost = 8;  // least cost of an item that a unit is split into
-
-// Waves along the rows that `rows` rows take in tiles of kTileRows.
-__device__ __forceinline__ int row_waves(int rows) {
-  const int rest = rows % kTileRows;
-  return rows / kTileRows * 4 + (rest == 0 ? 0 : rest <= 32 ? 1 : 4);
-}
-
-__device__ __forceinline__ int steps_of(int keys) { return (keys + kStepKeys - 1) / kStepKeys; }
-
-struct UnitWork {
-  Item it;
-  int steps, cost;
-  int group;  // the group whose shared partial results the unit's rows have, or -1
-};
-
-// The lengths, in LDS or (many requests) where the caller has them, and what
-// the plan finds on its way.
-struct Lengths {
-  const int *row_start, *length, *group_start, *prefix_length;
-  int *bounds, *group_of, *waves;
-  bool single;  // one token each: row_start[b] = b
-  __device__ __forceinline__ int start(int b) const { return single ? b : row_start[b]; }
-};
-
-// Unit u of segment s (a group, or groups + a request).  A request's last
-// rows, which see the most keys, come first: the workgroups that start last
-// are then the short ones (9,216 new tokens of 32 heads: 924 -> 804 us with
-// the scheduler that build.py names).
-__device__ UnitWork unit_work(const AttendArgs& a, const Lengths& z, int s, int u) {
-  const int tile = s < a.groups ? u - z.bounds[s] : z.bounds[s + 1] - 1 - u;
-  UnitWork w;
-  const int g = (int)a.share.d;
-  w.group = -1;
-  w.it.pad = 0;
-  w.it.acc = -1;
-  w.it.step0 = 0;
-  if (s < a.groups) {
-    const int t0 = z.start(z.group_start[s]), t1 = z.start(z.group_start[s + 1]);
-    w.it.row0 = t0 * g + tile * kTileRows;
-    w.it.rows = min(kTileRows, t1 * g - w.it.row0);
-    w.it.prefix = s;
-    w.it.prefix_len = z.prefix_length[s];
-    w.it.prefix_steps = steps_of(w.it.prefix_len);
-    w.it.request = 0;
-    w.it.own_end = 0;
-    w.it.limit = 0;
-    w.steps = w.it.prefix_steps;
-  } else {
-    const int b = s - a.groups;
-    const int t0 = z.start(b), t1 = z.start(b + 1);
-    w.it.row0 = t0 * g + tile * kTileRows;
-    w.it.rows = min(kTileRows, t1 * g - w.it.row0);
-    w.it.request = b;
-    w.it.limit = z.length[b] - (t1 - t0) - t0 + 1;
-    const int last = (int)divide((uint32_t)(w.it.row0 + w.it.rows - 1), a.share);
-    w.it.own_end = last + w.it.limit;
-    w.it.prefix = 0;
-    w.it.prefix_len = 0;
-    w.it.prefix_steps = 0;
-    if (a.groups) {
-      const int j = z.group_of[b];
-      if (z.waves[j] == 1) {
-        w.group = j;
-      } else {
-        w.it.prefix = j;
-        w.it.prefix_len = z.prefix_length[j];
-        w.it.prefix_steps = steps_of(w.it.prefix_len);
-      }
-    }
-    w.steps = w.it.prefix_steps + steps_of(w.it.own_end);
-  }
-  w.it.step1 = w.steps;
-  w.cost = w.steps * row_waves(w.it.rows);
-  return w;
-}
-
-// One workgroup: checks the lengths, decides which groups take their prefix
-// for all requests at once, and cuts the units into items of about equal cost.
+// The plan in a launch of its own: the items in memory.
 template <bool SMALL>
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(AttendArgs a) {
-  __shared__ int part[16];
-  __shared__ int64_t part64[16];
-  __shared__ int lds[SMALL ? 8 * (kPlanSmall + 1) : 1];
-  const int g = (int)a.share.d, tid = threadIdx.x, threads = blockDim.x;
-  Lengths z;
-  z.single = !a.row_start;
-  bool bad = false;
-  if constexpr (SMALL) {
-    int* rs = lds;
-    int* len = rs + kPlanSmall + 1;
-    int* gs = len + kPlanSmall + 1;
-    int* pl = gs + kPlanSmall + 1;
-    z.waves = pl + kPlanSmall + 1;
-    z.group_of = z.waves + kPlanSmall + 1;
-    z.bounds = z.group_of + kPlanSmall + 1;  // twice as many
-    z.row_start = rs;
-    z.length = len;
-    z.group_start = gs;
-    z.prefix_length = pl;
-    for (int i = tid; i <= max(a.requests, a.groups); i += threads) {
-      const bool r = i < a.requests, j = i < a.groups;
-      const int x0 = i <= a.requests && a.row_start ? a.row_start[i] : i;
-      const int x1 = r ? a.length[i] : 0;
-      const int x2 = i <= a.groups && a.groups ? a.group_start[i] : 0;
-      const int x3 = j ? a.prefix_length[i] : 0;
-      if (i <= a.requests) rs[i] = x0;
-      if (r) len[i] = x1;
-      if (i <= a.groups) gs[i] = x2;
-      if (j) pl[i] = x3;
-    }
-    __syncthreads();
-  } else {
-    z.row_start = a.row_start;
-    z.length = a.length;
-    z.group_start = a.group_start;
-    z.prefix_length = a.prefix_length;
-    z.waves = a.waves;
-    z.group_of = a.group_of;
-    z.bounds = a.bounds;
-  }
-  // checks
-  for (int b = tid; b < a.requests; b += threads) {
-    const int t0 = z.start(b), t1 = z.start(b + 1), n = z.length[b];
-    bad |= t0 < 0 || t1 < t0 || t1 > a.tokens || n < t1 - t0 || n > ((int64_t)a.width << a.page_shift);
-    if (b == 0) bad |= t0 != 0;
-  }
-  for (int j = tid; j < a.groups; j += threads) {
-    const int b0 = z.group_start[j], b1 = z.group_start[j + 1], p = z.prefix_length[j];
-    bad |= b0 < 0 || b1 < b0 || b1 > a.requests || p < 0 || p > ((int64_t)a.prefix_width << a.page_shift);
-    if (j == 0) bad |= b0 != 0;
-    if (j == a.groups - 1) bad |= b1 != a.requests;
-    z.waves[j] = 0;
-  }
-  if (__syncthreads_or(bad)) {
-    if (tid == 0) {
-      a.hdr->units = 0;
-      a.hdr->items = 0;
-      a.hdr->rejected = 1;
-      if (a.status) atomicOr(a.status, (uint32_t)KVR_DEV_BAD_LENGTH);
-    }
-    return;
-  }
-  // waves along the rows that the requests of a group take one by one
-  for (int b = tid; b < a.requests && a.groups; b += threads) {
-    const int j = last_at_most(z.group_start, a.groups, b);
-    z.group_of[b] = j;
-    atomicAdd(&z.waves[j], row_waves((z.start(b + 1) - z.start(b)) * g));
-  }
-  __syncthreads();
-  // units: a group's (its prefix, if that is shared), then a request's
-  const int segments = a.groups + a.requests;
-  int units = 0;
-  for (int s0 = 0; s0 < segments; s0 += threads) {
-    const int s = s0 + tid;
-    int count = 0;
-    if (s < a.groups) {
-      const int rows = (z.start(z.group_start[s + 1]) - z.start(z.group_start[s])) * g;
-      const bool shared = z.prefix_length[s] > 0 && row_waves(rows) * 4 <= z.waves[s] * 3;
-      z.waves[s] = shared ? 1 : 0;
-      count = shared ? (rows + kTileRows - 1) / kTileRows : 0;
-    } else if (s < segments) {
-      const int b = s - a.groups;
-      count = ((z.start(b + 1) - z.start(b)) * g + kTileRows - 1) / kTileRows;
-    }
-    int all;
-    const int before = group_before(count, all, part);
-    if (s < segments) z.bounds[s] = units + before;
-    units += all;
-  }
-  if (tid == 0) z.bounds[segments] = units;
-  __syncthreads();
-  int64_t total = 0;
-  UnitWork w;
-  int s = 0;
-  for (int u = tid; u < units; u += threads) {
-    s = last_at_most(z.bounds, segments, u);
-    w = unit_work(a, z, s, u);
-    total += w.cost;
-  }
-  group_before(total, total, part64);
-  const int64_t fair = (total + a.split_slots - 1) / a.split_slots;
-  const int chunk = (int)(fair < kMinSplitCost ? kMinSplitCost : fair > 0x7fffffff ? 0x7fffffff : fair);
-  int items = 0, rows_acc = 0;
-  for (int u0 = 0; u0 < units; u0 += threads) {
-    const int u = u0 + tid;
-    int splits = 0, per = 1, partial = 0;
-    if (u < units) {
-      if (units > threads) {  // else it is there
-        s = last_at_most(z.bounds, segments, u);
-        w = unit_work(a, z, s, u);
-      }
-      splits = max(1, (w.cost + chunk - 1) / chunk);
-      per = max(1, (w.steps + splits - 1) / splits);
-      splits = max(1, (w.steps + per - 1) / per);
-      partial = s < a.groups || w.group >= 0 || splits > 1 ? splits * w.it.rows : 0;
-    }
-    int all_items, all_rows;
-    const int i0 = items + group_before(splits, all_items, part);
-    const int acc = rows_acc + group_before(partial, all_rows, part);
-    items += all_items;
-    rows_acc += all_rows;
-    if (u < units) {
-      Unit x;
-      x.row0 = w.it.row0;
-      x.rows = w.it.rows;
-      x.acc = partial ? acc : -1;
-      x.splits = splits;
-      x.own = s >= a.groups;
-      x.group_unit = -1;
-      x.group_row = 0;
-      x.pad = 0;
-      if (w.group >= 0) {
-        x.group_unit = z.bounds[w.group];
-        x.group_row = z.start(z.group_start[w.group]) * g;
-      }
-      a.units[u] = x;
-      for (int i = 0; i < splits; ++i) {
-        Item it = w.it;
-        it.step0 = min(w.steps, i * per);
-        it.step1 = min(w.steps, (i + 1) * per);
-        it.acc = partial ? acc + i * w.it.rows : -1;
-        a.items[i0 + i] = it;
-      }
-    }
-  }
-  if (tid == 0) {
-    a.hdr->units = units;
-    a.hdr->items = items;
-    a.hdr->rejected = 0;
-  }
+  __shared__ int lds[SMALL ? plan_words(kPlanSmall) : plan_words(0)];
+  const int units = make_plan<SMALL ? kPlanSmall : 0>(a, lds, true, [&](int i, const Item& it) { a.items[i] = it; });
+  (void)units;
 }
 
 // ---------------------------------------------------------------- attention: the join
@@ -597,7 +344,10 @@ hipError_t launch_tables(const TablesArgs& a, hipStream_t st) {
   int blocks = (a.num_tokens + per - 1) / per;
   const int least = a.rows / kFillThreads + 1 < 64 ? a.rows / kFillThreads + 1 : 64;
   if (blocks < least) blocks = least;
-  tables_fill_kernel<<<dim3(blocks), dim3(kFillThreads), 0, st>>>(a);
+  if (a.rows <= kStagedRows)
+    tables_fill_kernel<true><<<dim3(blocks), dim3(kFillThreads), 0, st>>>(a);
+  else
+    tables_fill_kernel<false><<<dim3(blocks), dim3(kFillThreads), 0, st>>>(a);
   return hipGetLastError();
 }
 
@@ -610,7 +360,15 @@ hipError_t launch_store(const StoreArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+// Up to 64 units each workgroup plans for itself, which saves a launch (eight
+// requests 18.8 -> 15.9 us, 33 requests 26.8 -> 25.1 us; with 72 units it was
+// no faster).
+bool attend_fused(const AttendArgs& a) {
+  return a.unit_cap <= kPlanFused && a.requests <= kPlanFused && a.groups <= kPlanFused;
+}
+
 hipError_t launch_attend_plan(const AttendArgs& a, hipStream_t st) {
+  if (a.fused) return hipSuccess;
   const dim3 threads(a.unit_cap <= 256 ? 256 : kPlanThreads);
   if (a.requests <= kPlanSmall && a.groups <= kPlanSmall)
     plan_kernel<true><<<dim3(1), threads, 0, st>>>(a);

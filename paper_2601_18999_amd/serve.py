@@ -123,9 +123,11 @@ def block_tables(held: torch.Tensor, delta: torch.Tensor, table: torch.Tensor, r
         _refuse(where, "num_tokens must be in 0..2^31 - 1, page_size a power of two in 1..1024")
     nbytes = _tables_bytes(rows)
     # one allocation: the outputs, then the workspace on a 256-byte boundary
-    ends = rows, 2 * rows + 1, 2 * rows + 1 + num_tokens, 2 * rows + 1 + 2 * num_tokens
-    whole = torch.empty((ends[3] + 63 & -64) + nbytes // 4, dtype=i32, device=device)
-    held_out, row_start, slots, positions, work = whole.tensor_split((*ends[:3], ends[3]))
+    outputs = 2 * rows + 1 + 2 * num_tokens
+    work = outputs + 63 & -64
+    whole = torch.empty(work + nbytes // 4, dtype=i32, device=device)
+    held_out, row_start, slots, positions, _ = torch.split_with_sizes(
+        whole, (rows, rows + 1, num_tokens, num_tokens, work - outputs + nbytes // 4))
     if in_place:
         held_out = held
     state_out = state if in_place else torch.empty_like(state)
@@ -133,8 +135,9 @@ def block_tables(held: torch.Tensor, delta: torch.Tensor, table: torch.Tensor, r
     kvr_block_tables(
         TABLES_RECORD.pack(TABLES_RECORD.size, rows, width, page_size, ring.shape[0], num_tokens, stride, p_held,
                            p_delta, p_base, p_table, p_ring, p_state, p_held if in_place else at,
-                           state_out.data_ptr(), at + 4 * ends[0], at + 4 * ends[1], at + 4 * ends[2]),
-        at + 4 * (ends[3] + 63 & -64), nbytes, _stream(device))
+                           state_out.data_ptr(), at + 4 * rows, at + 4 * (2 * rows + 1),
+                           at + 4 * (2 * rows + 1 + num_tokens)),
+        at + 4 * work, nbytes, _stream(device))
     return BlockTables(held_out, state_out, row_start, slots, positions)
 
 
