@@ -93,14 +93,13 @@ __device__ __forceinline__ int ring_at(int from, int i, int size) {
   return (int)(at >= (uint32_t)size ? at - size : at);
 }
 
-// Slot and position of new token t.  Its row is found in row_start; the first
-// token of a gained page writes its table entry (a gained page always has one).
+// Slot and position of new token t, of row r.  The first token of a gained
+// page writes its table entry (a gained page always has one).
 __device__ __forceinline__ void place_token(const TablesArgs& a, const TablesHdr& h, const int* row_start,
-                                            const int* gain_at, int t) {
+                                            const int* gain_at, int t, int r) {
   int slot = -1, position = -1;
   if (!h.rejected && t < h.tokens) {
     const int mask = (1 << a.page_shift) - 1;
-    const int r = last_at_most(row_start, a.rows, t);
     const int held = a.held_out[r] - a.delta[r];
     const int at = held + t - row_start[r];
     const int col = at >> a.page_shift, before = (int)(((int64_t)held + mask) >> a.page_shift);
@@ -119,9 +118,8 @@ __device__ __forceinline__ void place_token(const TablesArgs& a, const TablesHdr
   a.positions[t] = position;
 }
 
-// Puts back dropped page g.
-__device__ __forceinline__ void drop_page(const TablesArgs& a, const TablesHdr& h, const int* give_at, int g) {
-  const int r = last_at_most(give_at, a.rows, g);
+// Puts back dropped page g, of row r.
+__device__ __forceinline__ void drop_page(const TablesArgs& a, const TablesHdr& h, const int* give_at, int g, int r) {
   const int mask = (1 << a.page_shift) - 1;
   const int after = (int)(((int64_t)a.held_out[r] + mask) >> a.page_shift);
   a.ring[ring_at((int)h.tail, g, a.ring_size)] = a.table[r * a.table_stride + after + g - give_at[r]];
@@ -141,43 +139,50 @@ __global__ void __launch_bounds__(kScanThreads) tables_fused_kernel(TablesArgs a
   __shared__ int row_start[kFusedRows + 1], gain_at[kFusedRows], give_at[kFusedRows];
   const TablesHdr h = scan_rows(a, part, row_start, gain_at, give_at);
   for (int r = threadIdx.x; r <= a.rows; r += blockDim.x) a.row_start[r] = row_start[r];
-  for (int t = threadIdx.x; t < a.num_tokens; t += blockDim.x) place_token(a, h, row_start, gain_at, t);
+  for (int t = threadIdx.x; t < a.num_tokens; t += blockDim.x) place_token(a, h, row_start, gain_at, t, last_at_most(row_start, a.rows, t));
   if (h.rejected) return;
-  for (int g = threadIdx.x; g < h.give; g += blockDim.x) drop_page(a, h, give_at, g);
+  for (int g = threadIdx.x; g < h.give; g += blockDim.x) drop_page(a, h, give_at, g, last_at_most(give_at, a.rows, g));
 }
 
-constexpr int kFillThreads = 256, kFillTokens = 4;  // tokens of a thread
+// last_at_most(start, n, x0 + lane) for a wave's neighbouring values: the wave
+// finds the first one's place, 64 probes at a time, and each lane its own among
+// the next 64 entries (a search by each lane reads log2(n) times in a row
+// instead of three).  All lanes are active.
+__device__ __forceinline__ int last_at_most_of_lanes(const int* start, int n, int x0) {
+  const int lane = threadIdx.x & 63, x = x0 + lane;
+  int lo = 0, len = n;
+  while (len > 1) {
+    const int step = (len + 63) / 64, at = lane * step;
+    const int probe = at < len ? start[lo + at] : 0x7fffffff;
+    const int k = max(0, __popcll(__ballot(probe <= x0)) - 1);
+    lo += k * step;
+    len = min(step, len - k * step);
+  }
+  const int next = lo + 1 + lane < n ? start[lo + 1 + lane] : 0x7fffffff;
+  int k = 0;
+#pragma unroll
+  for (int s = 32; s; s >>= 1)
+    if (__shfl(next, k + s - 1) <= x) k += s;
+  // (k = 63: the 64 entries may not reach)
+  return k < 63 ? lo + k : lo + k + last_at_most(start + lo + k, n - lo - k, x);
+}
+
+constexpr int kFillThreads = 256;
 
 // Slots and positions of the new tokens, the pages they gain, and the pages
-// that are given back.  With STAGED, up to kStagedRows rows, the sums are
-// searched in LDS (FILL_FIGURE).
-constexpr int kStagedRows = 4096;
-template <bool STAGED>
+// that are given back.
 __global__ void __launch_bounds__(kFillThreads) tables_fill_kernel(TablesArgs a) {
-  __shared__ int staged[STAGED ? kStagedRows + 1 : 1];
   const TablesHdr h = *a.hdr;
-  const int t0 = blockIdx.x * kFillThreads * kFillTokens;
-  if constexpr (STAGED) {
-    if (t0 < a.num_tokens)
-      for (int r = threadIdx.x; r <= a.rows; r += kFillThreads) staged[r] = a.row_start[r];
-    __syncthreads();
+  const int lane = threadIdx.x & 63, first = blockIdx.x * kFillThreads + (threadIdx.x - lane);
+  if (first < a.num_tokens) {
+    const int r = first < h.tokens && !h.rejected ? last_at_most_of_lanes(a.row_start, a.rows, first) : 0;
+    if (first + lane < a.num_tokens) place_token(a, h, a.row_start, a.gain_at, first + lane, r);
   }
-  const int* row_start = STAGED ? staged : a.row_start;
-#pragma unroll
-  for (int i = 0; i < kFillTokens; ++i) {
-    const int t = t0 + i * kFillThreads + threadIdx.x;
-    if (t < a.num_tokens) place_token(a, h, row_start, a.gain_at, t);
+  if (h.rejected) return;
+  for (int g = first; g < h.give; g += gridDim.x * kFillThreads) {
+    const int r = last_at_most_of_lanes(a.give_at, a.rows, g);
+    if (g + lane < h.give) drop_page(a, h, a.give_at, g + lane, r);
   }
-  if (h.rejected || h.give == 0) return;
-  const int* give_at = a.give_at;
-  if constexpr (STAGED) {
-    __syncthreads();
-    for (int r = threadIdx.x; r < a.rows; r += kFillThreads) staged[r] = a.give_at[r];
-    __syncthreads();
-    give_at = staged;
-  }
-  for (int g = blockIdx.x * kFillThreads + threadIdx.x; g < h.give; g += gridDim.x * kFillThreads)
-    drop_page(a, h, give_at, g);
 }
 
 // ---------------------------------------------------------------- cache store
@@ -340,14 +345,10 @@ hipError_t launch_tables(const TablesArgs& a, hipStream_t st) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   // blocks for the tokens; with few new tokens there may be many pages to give back
-  const int per = kFillThreads * kFillTokens;
-  int blocks = (a.num_tokens + per - 1) / per;
-  const int least = a.rows / kFillThreads + 1 < 64 ? a.rows / kFillThreads + 1 : 64;
+  int blocks = (a.num_tokens + kFillThreads - 1) / kFillThreads;
+  const int least = a.rows / 16 + 1 < 256 ? a.rows / 16 + 1 : 256;
   if (blocks < least) blocks = least;
-  if (a.rows <= kStagedRows)
-    tables_fill_kernel<true><<<dim3(blocks), dim3(kFillThreads), 0, st>>>(a);
-  else
-    tables_fill_kernel<false><<<dim3(blocks), dim3(kFillThreads), 0, st>>>(a);
+  tables_fill_kernel<<<dim3(blocks), dim3(kFillThreads), 0, st>>>(a);
   return hipGetLastError();
 }
 
