@@ -29,6 +29,8 @@
 // the rounded result; the sum l adds the unrounded p.
 #pragma once
 
+#include <type_traits>
+
 #include "kvr_plan.h"
 
 namespace kvr {
@@ -147,14 +149,18 @@ __device__ __forceinline__ uint32_t lds_offset(const void* p) {
   return (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(lds_char*)p);
 }
 __device__ __forceinline__ void load16_to_lds(global_bytes from, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from),
+               "s"(__builtin_amdgcn_readfirstlane(to))
+               : "memory");
 }
 __device__ __forceinline__ void load4_to_lds(global_ints from, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(to) : "memory");
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from),
+               "s"(__builtin_amdgcn_readfirstlane(to))
+               : "memory");
 }
 // The same with one base for the wave and 32-bit offsets.
 __device__ __forceinline__ void load16_to_lds(uint64_t base, uint32_t offset, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(to)
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(__builtin_amdgcn_readfirstlane(to))
                : "memory");
 }
 template <int N>
@@ -216,31 +222,28 @@ struct Direct {
 
   // Pages of kRows tokens or more: the rows of one load stand in one page, so
   // a load has one base, in scalar registers, and lane offsets that stay the
-  // same from tile to tile.  kOffsets of them: the swizzle of load i's rows.
-  static constexpr int kOffsets = RW * kRows % 16 ? 2 : 1;
-  static_assert(RW == 1 || RW * kRows % 8 == 0, "two offsets are enough");
+  // same from tile to tile but for the swizzle of load i (the rows of one load
+  // and i's multiples share no bits, so the swizzles are xored).
   struct Offsets {
-    uint32_t k[kOffsets], v;
+    uint32_t k_row, k_chunk, v_row, v_chunk;
   };
   static __device__ __forceinline__ Offsets offsets(const AttendArgs& a, int wave, int lane) {
-    Offsets o;
-#pragma unroll
-    for (int i = 0; i < kOffsets; ++i)
-      o.k[i] = lane / kChunks * a.kc_slot +
-               (((lane % kChunks) ^ swizzle_k<D>(i * RW * kRows + first(wave, lane))) << 4);
-    o.v = lane / kChunks * a.vc_slot + (((lane % kChunks) ^ swizzle_v<D>(first(wave, lane))) << 4);
-    return o;
+    const uint32_t row = lane / kChunks, chunk = lane % kChunks;
+    return {row * a.kc_slot, (chunk ^ swizzle_k<D>(first(wave, lane))) << 4, row * a.vc_slot,
+            (chunk ^ swizzle_v<D>(first(wave, lane))) << 4};
   }
-  template <bool KEYS>
-  static __device__ __forceinline__ void load(const AttendArgs& a, global_bytes base, const int (&page)[kN],
-                                              const Offsets& o, int key0, int wave, uint32_t to) {
+  // page_of(i): the page of load i's rows, the same in all lanes
+  template <bool KEYS, class PageOf>
+  static __device__ __forceinline__ void load(const AttendArgs& a, global_bytes base, PageOf page_of, const Offsets& o,
+                                              int key0, int wave, uint32_t to) {
     const uint32_t page_bytes = KEYS ? a.kc_page : a.vc_page, slot_bytes = KEYS ? a.kc_slot : a.vc_slot;
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       const uint32_t slot = (uint32_t)(key0 + (i * RW + wave) * kRows) & (uint32_t)a.page_mask;
-      const uint32_t at = (uint32_t)__builtin_amdgcn_readfirstlane(page[i]);
-      const uint64_t from = (uint64_t)base + (uint64_t)at * page_bytes + (uint64_t)slot * slot_bytes;
-      load16_to_lds(from, KEYS ? o.k[i % kOffsets] : o.v, to + (i * RW + wave) * 1024);
+      const uint64_t from = (uint64_t)base + (uint64_t)(uint32_t)page_of(i) * page_bytes + (uint64_t)slot * slot_bytes;
+      const uint32_t swizzle = (uint32_t)(KEYS ? swizzle_k<D>(i * RW * kRows) : swizzle_v<D>(i * RW * kRows)) << 4;
+      const uint32_t offset = KEYS ? o.k_row + (o.k_chunk ^ swizzle) : o.v_row + (o.v_chunk ^ swizzle);
+      load16_to_lds(from, offset, to + (i * RW + wave) * 1024);
     }
   }
 };
@@ -344,37 +347,38 @@ struct Rows {
     return __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7);
   }
 
-  // Scores of KB * 32 keys in LDS.  The reads of a block of 32 keys are on
-  // their way while the block before it is multiplied (a read takes as long as
-  // several products), and the first values' while the last one is.
-  template <int KB, bool VALUES>
+  // Scores of KB * 32 keys in LDS.  A chunk is read AHEAD products before its
+  // own (a read takes as long as several products), and with VALUES the first
+  // values while the last products run.
+  template <int KB, int AHEAD, bool VALUES>
   __device__ __forceinline__ void scores(const char* kt, const char* vt, f32x16 (&s)[KB], s16x8 (&first)[D / 32], int n,
                                          int hh) {
-    constexpr int N = D / 16, V = VALUES ? D / 32 : 0;
-    s16x8 f[2][N];
+    constexpr int N = D / 16, F = KB * N, V = VALUES ? D / 32 : 0;
+    static_assert(V <= AHEAD && AHEAD <= F, "chunks ahead");
+    s16x8 f[F];
 #pragma unroll
-    for (int i = 0; i < N; ++i) f[0][i] = key_chunk(kt, n, i, hh);
-    __builtin_amdgcn_sched_group_barrier(kReads, N, 0);
+    for (int i = 0; i < AHEAD; ++i) f[i] = key_chunk(kt, i / N * 32 + n, i % N, hh);
+    __builtin_amdgcn_sched_group_barrier(kReads, AHEAD, 0);
 #pragma unroll
-    for (int b = 0; b < KB; ++b) {
+    for (int b = 0; b < KB; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        if (b + 1 < KB)
-          f[(b + 1) & 1][i] = key_chunk(kt, (b + 1) * 32 + n, i, hh);
-        else if (i < V)
-          first[i] = value_chunk(vt, 0, i, n + 32 * hh);
-        s[b] = T::mfma(f[b & 1][i], q[i], s[b]);
-      }
+    for (int i = 0; i < F; ++i) {
+      const int next = i + AHEAD;
+      if (next < F)
+        f[next] = key_chunk(kt, next / N * 32 + n, next % N, hh);
+      else if (next - F < V)
+        first[next - F] = value_chunk(vt, 0, next - F, n + 32 * hh);
+      s[i / N] = T::mfma(f[i], q[i % N], s[i / N]);
+    }
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        __builtin_amdgcn_sched_group_barrier(kProducts, 1, 0);
-        if (b + 1 < KB)
-          __builtin_amdgcn_sched_group_barrier(kReads, 1, 0);
-        else if (i < V)
-          __builtin_amdgcn_sched_group_barrier(kReads, 2, 0);
-      }
+    for (int i = 0; i < F; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kProducts, 1, 0);
+      if (i + AHEAD < F)
+        __builtin_amdgcn_sched_group_barrier(kReads, 1, 0);
+      else if (i + AHEAD - F < V)
+        __builtin_amdgcn_sched_group_barrier(kReads, 2, 0);
     }
   }
 
@@ -507,6 +511,9 @@ template <int D, class T, bool FP8, int RW>
 __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it, int head, float scale, char* lds) {
   typedef Shape<D, RW> S;
   constexpr int KG = S::kKeyGroups, KT = S::kKeys, KB = KT / 32, DB = D / 32;
+  // reads ahead, as many as there are registers for
+  constexpr int kAhead = D == 256 || FP8 ? 4 : D == 64 && RW == 1 ? 4 : 8;
+  constexpr bool kEarly = RW > 1 && D <= 128 && !FP8;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rw = wave % RW, kg = wave / RW, thread = tid % (64 * RW);
   const int n = lane & 31, hh = lane >> 5;
@@ -589,7 +596,7 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
         return;
       }
     }
-    x.template values<KB, (RW > 1)>(vt, s, first, lane);
+    x.template values<KB, kEarly>(vt, s, first, lane);
   };
 
   if constexpr (RW == 1 && !FP8) {
@@ -605,20 +612,39 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
       const int key = min(p.key0 + n, p.end - 1);
       load4_to_lds(p.table + (key >> a.page_shift), id_to + (j & 1) * 256);
     };
-    int page[N];
-    auto read_ids = [&](int j) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) page[i] = ids[(j & 1) * 64 + i * L::kRows + L::first(0, lane)];
+    const typename L::Offsets offsets = L::offsets(a, 0, lane);
+    const bool uniform = (1 << a.page_shift) >= L::kRows;
+    // whether all rows of tile j are keys in pages of the cache; a page outside it is reported
+    auto whole_of_ids = [&](const Place& p, int j) {
+      const bool bad = (uint32_t)ids[(j & 1) * 64 + n] >= (uint32_t)a.num_pages;
+      if (bad && a.status) atomicOr(a.status, (uint32_t)KVR_DEV_BAD_PAGE);
+      return p.key0 + KT <= p.end && !__any(bad);
     };
+    auto load = [&](auto keys, const Place& p, int j, bool whole) {
+      constexpr bool K = decltype(keys)::value;
+      const int* id = ids + (j & 1) * 64;
+      if (whole && uniform) {
+        const int of_load = id[lane * L::kRows % KT];  // lane i: load i's
+        L::template load<K>(a, K ? kc : vc, [&](int i) { return __builtin_amdgcn_readlane(of_load, i); }, offsets,
+                            p.key0, 0, K ? k_to : v_to);
+      } else {
+        int page[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) page[i] = id[i * L::kRows + L::first(0, lane)];
+        wait_lds();
+        L::template load<K>(a, K ? kc : vc, page, whole, p.key0, p.end, 0, lane, K ? k_to : v_to);
+      }
+    };
+    constexpr std::true_type keys{};
+    constexpr std::false_type vals{};
     if (mine > 0) {
       Place p = place(wave);
       load_ids(0);
       wait_loads<0>();
-      read_ids(0);
-      const bool whole = whole_of(p, page);
-      L::template load<true>(a, kc, page, whole, p.key0, p.end, 0, lane, k_to);
+      const bool whole = whole_of_ids(p, 0);
+      load(keys, p, 0, whole);
       if (mine > 1) load_ids(1);
-      L::template load<false>(a, vc, page, whole, p.key0, p.end, 0, lane, v_to);
+      load(vals, p, 0, whole);
       auto round = [&](auto kind, int j) {
         // in flight, oldest first: K of this tile, the next one's page numbers, V of this tile
         const bool more = j + 1 < mine;
@@ -627,12 +653,11 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
         wait_loads<N>();
         f32x16 s[KB];
         s16x8 first[DB];
-        if (more) read_ids(j + 1);
-        x.template scores<KB, false>(kt, vt, s, first, n, hh);
+        x.template scores<KB, kAhead, false>(kt, vt, s, first, n, hh);
+        if (more) whole1 = whole_of_ids(p1, j + 1);
         wait_lds();
         if (more) {
-          whole1 = whole_of(p1, page);
-          L::template load<true>(a, kc, page, whole1, p1.key0, p1.end, 0, lane, k_to);
+          load(keys, p1, j + 1, whole1);
           if (j + 2 < mine) load_ids(j + 2);
         }
         weigh(kind, p, s);
@@ -644,7 +669,7 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
           wait_loads<0>();
         multiply(kind, p, vt, s, first);
         wait_lds();
-        if (more) L::template load<false>(a, vc, page, whole1, p1.key0, p1.end, 0, lane, v_to);
+        if (more) load(vals, p1, j + 1, whole1);
         p = p1;
       };
       int j = 0;
@@ -670,7 +695,7 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
       pages(p2, row0, L::kRows, page);
       f32x16 s[KB];
       s16x8 first[DB];
-      x.template scores<KB, (RW > 1)>(kt, vt, s, first, n, hh);
+      x.template scores<KB, kAhead, kEarly>(kt, vt, s, first, n, hh);
       weigh(kind, p, s);
       multiply(kind, p, vt, s, first);
       p = p1;
@@ -692,7 +717,7 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
       // step, and the matrix and the vector unit wait for each other (9,216 new
       // tokens: 731 -> 708 us)
       __builtin_amdgcn_s_setprio(1);
-      x.template scores<KB, (RW > 1)>(kt, vt, s, first, n, hh);
+      x.template scores<KB, kAhead, kEarly>(kt, vt, s, first, n, hh);
       __builtin_amdgcn_s_setprio(0);
       weigh(kind, p, s);
       __builtin_amdgcn_s_setprio(1);
@@ -709,8 +734,9 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
       auto load = [&](const Place& q, uint32_t at) {
         const bool whole = whole_of(q, page);
         if (whole && uniform) {
-          L::template load<true>(a, kc, page, offsets, q.key0, rw, at);
-          L::template load<false>(a, vc, page, offsets, q.key0, rw, at + S::kTileBytes);
+          auto page_of = [&](int i) { return __builtin_amdgcn_readfirstlane(page[i]); };
+          L::template load<true>(a, kc, page_of, offsets, q.key0, rw, at);
+          L::template load<false>(a, vc, page_of, offsets, q.key0, rw, at + S::kTileBytes);
         } else {
           L::template load<true>(a, kc, page, whole, q.key0, q.end, rw, lane, at);
           L::template load<false>(a, vc, page, whole, q.key0, q.end, rw, lane, at + S::kTileBytes);

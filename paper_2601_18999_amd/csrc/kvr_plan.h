@@ -214,7 +214,7 @@ __device__ __forceinline__ int make_plan(const AttendArgs& a, int* lds, bool wri
   }
   if (__syncthreads_or(bad)) {
     if (tid == 0 && write) {
-      a.hdr->units = 0;
+      a.hdr->joins = 0;
       a.hdr->items = 0;
       a.hdr->rejected = 1;
       if (a.status) atomicOr(a.status, (uint32_t)KVR_DEV_BAD_LENGTH);
@@ -261,7 +261,7 @@ __device__ __forceinline__ int make_plan(const AttendArgs& a, int* lds, bool wri
   group_before(total, total, part64);
   const int64_t fair = (total + a.split_slots - 1) / a.split_slots;
   const int chunk = (int)(fair < kMinSplitCost ? kMinSplitCost : fair > 0x7fffffff ? 0x7fffffff : fair);
-  int items = 0, rows_acc = 0;
+  int items = 0, rows_acc = 0, joins = 0;
   for (int u0 = 0; u0 < units; u0 += threads) {
     const int u = u0 + tid;
     int splits = 0, per = 1, partial = 0;
@@ -278,15 +278,19 @@ __device__ __forceinline__ int make_plan(const AttendArgs& a, int* lds, bool wri
     int all_items, all_rows;
     const int i0 = items + group_before(splits, all_items, part);
     const int acc = rows_acc + group_before(partial, all_rows, part);
+    int all_joins = 0;
+    const int parts = partial && s >= a.groups ? (w.it.rows * (a.dim / 4) + 255) / 256 : 0;
+    const int join_at = joins + (write ? group_before(parts, all_joins, part) : 0);
     items += all_items;
     rows_acc += all_rows;
+    joins += all_joins;
     if (u < units) {
       Unit x;
       x.row0 = w.it.row0;
       x.rows = w.it.rows;
       x.acc = partial ? acc : -1;
       x.splits = splits;
-      x.own = s >= a.groups;
+      x.pad1 = 0;
       x.group_unit = -1;
       x.group_row = 0;
       x.pad = 0;
@@ -295,6 +299,8 @@ __device__ __forceinline__ int make_plan(const AttendArgs& a, int* lds, bool wri
         x.group_row = z.start(z.group_start[w.group]) * g;
       }
       if (write) a.units[u] = x;
+      if (write)
+        for (int i = 0; i < parts; ++i) a.joins[join_at + i] = make_int2(u, i);
       for (int i = 0; i < splits; ++i) {
         Item it = w.it;
         it.step0 = min(w.steps, i * per);
@@ -305,7 +311,7 @@ __device__ __forceinline__ int make_plan(const AttendArgs& a, int* lds, bool wri
     }
   }
   if (tid == 0 && write) {
-    a.hdr->units = units;
+    a.hdr->joins = joins;
     a.hdr->items = items;
     a.hdr->rejected = 0;
   }

@@ -84,8 +84,7 @@ struct Unit {
   int32_t row0, rows;
   int32_t acc, splits;           // first partial row (-1: written directly), items
   int32_t group_unit, group_row; // first unit of its group's prefix (-1: none) and that unit's row0
-  int32_t own;                   // 1: a request's unit (0: a group's)
-  int32_t pad;
+  int32_t pad, pad1;
 };
 
 struct Item {
@@ -100,7 +99,7 @@ struct Item {
 };
 
 struct PlanHdr {
-  int32_t units, items, rejected, pad;
+  int32_t joins, items, rejected, pad;  // joins: parts of the units whose results are joined
 };
 
 struct AttendArgs {
@@ -120,6 +119,7 @@ struct AttendArgs {
   int32_t* group_of;  // [requests]
   int32_t* waves;     // [groups] row waves of its requests, then: 1 = shared
   Unit* units;
+  int2* joins;  // unit and part of it (256 quads of four elements)
   Item* items;
   float2* ml;  // [partial row][kv head] running maximum (log2 units) and sum
   float* acc;  // [partial row][kv head][dim]
@@ -127,7 +127,7 @@ struct AttendArgs {
   float scale_log2;
   int32_t tokens, requests, groups, heads, kv_heads, dim;
   int32_t page_shift, page_mask, num_pages, width, prefix_width;
-  int32_t unit_cap, item_cap, split_slots;
+  int32_t unit_cap, item_cap, join_cap, split_slots;
   int32_t fused;  // 1: no plan kernel
 };
 

@@ -261,7 +261,6 @@ constexpr int kJoinAtOnce = 4;
 
 template <bool FP16>
 __global__ void __launch_bounds__(256) join_kernel(AttendArgs a) {
-  const int u = blockIdx.x / a.kv_heads, head = blockIdx.x % a.kv_heads;
   const int quads = a.dim / 4;
   if (a.hdr->rejected) {  // nothing was computed: every result is NaN
     const int64_t all = (int64_t)a.tokens * a.heads * quads, step = (int64_t)gridDim.x * 256;
@@ -272,12 +271,15 @@ __global__ void __launch_bounds__(256) join_kernel(AttendArgs a) {
     }
     return;
   }
-  if (u >= a.hdr->units) return;
-  const Unit x = a.units[u];
-  if (!x.own || x.acc < 0) return;
-  const float vs = a.vs ? a.vs[head] : 1.0f;
-  for (int i = threadIdx.x; i < x.rows * quads; i += 256) {
-    const int r = i / quads, c = i % quads;
+  // a block takes 256 quads (four elements of a row) of a unit and head at a time
+  const int64_t tasks = (int64_t)a.hdr->joins * a.kv_heads;
+  for (int64_t task = blockIdx.x; task < tasks; task += gridDim.x) {
+    const int head = (int)(task % a.kv_heads);
+    const int2 join = a.joins[task / a.kv_heads];
+    const Unit x = a.units[join.x];
+    const float vs = a.vs ? a.vs[head] : 1.0f;
+    const int i = join.y * 256 + threadIdx.x, r = i / quads, c = i % quads;
+    if (r >= x.rows) continue;
     const int row = x.row0 + r;
     float m = -INFINITY, l = 0.0f;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -379,7 +381,10 @@ hipError_t launch_attend_plan(const AttendArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_attend_join(const AttendArgs& a, bool fp16, hipStream_t st) {
-  const dim3 blocks((uint32_t)a.unit_cap * (uint32_t)a.kv_heads);
+  // what there is to join only the plan knows: as many blocks as the device
+  // holds at once, or fewer where there cannot be so many parts
+  const int64_t parts = (int64_t)a.join_cap * a.kv_heads;
+  const dim3 blocks((uint32_t)(parts < 8 * kComputeUnits ? parts : 8 * kComputeUnits));
   if (fp16)
     join_kernel<true><<<blocks, dim3(256), 0, st>>>(a);
   else

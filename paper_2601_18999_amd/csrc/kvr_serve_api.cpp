@@ -77,8 +77,8 @@ kvr_status check_buffers(const kvr_cache* c) {
 }
 
 struct AttendLayout {
-  size_t bounds, group_of, waves, units, items, ml, acc, bytes;
-  int32_t unit_cap, item_cap, split_slots;
+  size_t bounds, group_of, waves, units, joins, items, ml, acc, bytes;
+  int32_t unit_cap, item_cap, join_cap, split_slots;
 };
 
 kvr_status check(const kvr_cache* c, const kvr_attention* a) {
@@ -123,6 +123,10 @@ kvr_status lay_out(const kvr_cache* c, const kvr_attention* a, AttendLayout* l) 
   at += round_up((size_t)a->num_groups * 4);
   l->units = at;
   at += round_up((size_t)units * sizeof(kvr::Unit));
+  l->joins = at;
+  const int64_t joins = rows * c->dim / 1024 + units;
+  l->join_cap = (int32_t)(joins < kInt ? joins : kInt);
+  at += round_up((size_t)joins * sizeof(int2));
   l->items = at;
   at += round_up((size_t)items * sizeof(kvr::Item));
   l->ml = at;
@@ -295,6 +299,7 @@ kvr_status kvr_shared_attention(const kvr_cache* c, const kvr_attention* s, void
   a.group_of = reinterpret_cast<int32_t*>(ws + l.group_of);
   a.waves = reinterpret_cast<int32_t*>(ws + l.waves);
   a.units = reinterpret_cast<kvr::Unit*>(ws + l.units);
+  a.joins = reinterpret_cast<int2*>(ws + l.joins);
   a.items = reinterpret_cast<kvr::Item*>(ws + l.items);
   a.ml = reinterpret_cast<float2*>(ws + l.ml);
   a.acc = reinterpret_cast<float*>(ws + l.acc);
@@ -313,6 +318,7 @@ kvr_status kvr_shared_attention(const kvr_cache* c, const kvr_attention* s, void
   a.prefix_width = s->prefix_width;
   a.unit_cap = l.unit_cap;
   a.item_cap = l.item_cap;
+  a.join_cap = l.join_cap;
   a.split_slots = l.split_slots;
   a.fused = kvr::attend_fused(a);
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
