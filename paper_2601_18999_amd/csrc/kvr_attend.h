@@ -525,14 +525,15 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
   const uint32_t token = divide(row, a.share);
   const int qhead = head * (int)a.share.d + (int)(row - token * a.share.d);
   Rows<D, T> x;
-  {
+  // called when the first page numbers are on their way: both arrive together
+  auto load_queries = [&]() {
     const char* p = a.q + token * a.q_tok + qhead * a.q_head + hh * 16;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) x.q[i] = *(const s16x8*)(p + i * 32);
     // waited for here: a wait inside the loop would be for the tiles' loads too
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) asm volatile("" : "+v"(x.q[i]));
-  }
+  };
 #pragma unroll
   for (int b = 0; b < DB; ++b)
 #pragma unroll
@@ -640,6 +641,7 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
     if (mine > 0) {
       Place p = place(wave);
       load_ids(0);
+      load_queries();
       wait_loads<0>();
       const bool whole = whole_of_ids(p, 0);
       load(keys, p, 0, whole);
@@ -686,6 +688,7 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
     const int row0 = lane / L::kChunks;
     Place p = place(wave), p1 = place(wave + 4);
     pages(p, row0, L::kRows, page);
+    load_queries();
     ld.fetch(a, kc, vc, page, whole_of(p, page), p.key0, p.end, lane);
     pages(p1, row0, L::kRows, page);
     auto round = [&](auto kind, int j) {
@@ -744,6 +747,7 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
       };
       if (tiles > 0) {
         pages(p, row0, step, page);
+        load_queries();
         load(p, to);
         pages(p1, row0, step, page);
       }
@@ -770,6 +774,7 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
       L ld;
       const int row0 = thread / L::kChunks;
       pages(p, row0, L::kRows, page);
+      load_queries();
       ld.fetch(a, kc, vc, page, whole_of(p, page), p.key0, p.end, thread);
       pages(p1, row0, L::kRows, page);
       ld.store(lds, lds + S::kTileBytes, thread);
@@ -895,8 +900,8 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(AttendArg
       ((int*)&it)[i] = __builtin_amdgcn_readfirstlane(((int*)&it)[i]);
     __syncthreads();
   } else {
+    it = a.items[item];  // (there is room for as many as there are workgroups)
     if (item >= a.hdr->items) return;
-    it = a.items[item];
   }
   const float scale = FP8 && a.ks ? a.scale_log2 * a.ks[head] : a.scale_log2;
   if (it.rows > 32)
