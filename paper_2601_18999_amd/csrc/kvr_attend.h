@@ -199,25 +199,19 @@ struct Direct {
   static __device__ __forceinline__ void load(const AttendArgs& a, global_bytes base, const int (&page)[kN], bool whole,
                                               int key0, int end, int wave, int lane, uint32_t to) {
     const uint32_t page_bytes = KEYS ? a.kc_page : a.vc_page, slot_bytes = KEYS ? a.kc_slot : a.vc_slot;
-    global_bytes p[kN];
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       const int row = i * RW * kRows + first(wave, lane);
       const int ch = (lane % kChunks) ^ (KEYS ? swizzle_k<D>(row) : swizzle_v<D>(row));
-      p[i] = row_address(base + ch * 16, page[i], (key0 + row) & a.page_mask, page_bytes, slot_bytes);
-    }
-    if (!whole) {
-#pragma unroll
-      for (int i = 0; i < kN; ++i) {
-        const int key = key0 + i * RW * kRows + first(wave, lane);
-        if (key >= end)
-          p[i] = (global_bytes)kNoRow;
+      global_bytes p = row_address(base + ch * 16, page[i], (key0 + row) & a.page_mask, page_bytes, slot_bytes);
+      if (!whole) {
+        if (key0 + row >= end)
+          p = (global_bytes)kNoRow;
         else if ((uint32_t)page[i] >= (uint32_t)a.num_pages)
-          p[i] = (global_bytes)kBadRow;
+          p = (global_bytes)kBadRow;
       }
+      load16_to_lds(p, to + (i * RW + wave) * 1024);
     }
-#pragma unroll
-    for (int i = 0; i < kN; ++i) load16_to_lds(p[i], to + (i * RW + wave) * 1024);
   }
 
   // Pages of kRows tokens or more: the rows of one load stand in one page, so
@@ -242,7 +236,9 @@ struct Direct {
       const uint32_t slot = (uint32_t)(key0 + (i * RW + wave) * kRows) & (uint32_t)a.page_mask;
       const uint64_t from = (uint64_t)base + (uint64_t)(uint32_t)page_of(i) * page_bytes + (uint64_t)slot * slot_bytes;
       const uint32_t swizzle = (uint32_t)(KEYS ? swizzle_k<D>(i * RW * kRows) : swizzle_v<D>(i * RW * kRows)) << 4;
-      const uint32_t offset = KEYS ? o.k_row + (o.k_chunk ^ swizzle) : o.v_row + (o.v_chunk ^ swizzle);
+      uint32_t chunk = KEYS ? o.k_chunk : o.v_chunk;
+      if (swizzle) asm volatile("" : "+v"(chunk));  // xored here, not kept for each i (and spilled)
+      const uint32_t offset = (KEYS ? o.k_row : o.v_row) + (chunk ^ swizzle);
       load16_to_lds(from, offset, to + (i * RW + wave) * 1024);
     }
   }
@@ -263,27 +259,40 @@ struct Widened {
 
   __device__ __forceinline__ void fetch(const AttendArgs& a, global_bytes kc, global_bytes vc, const int (&page)[kN],
                                         bool whole, int key0, int end, int thread) {
-    global_bytes pk[kN], pv[kN];
     const int at = thread % kChunks * 16;
-#pragma unroll
-    for (int i = 0; i < kN; ++i) {
+    auto place = [&](int i, global_bytes& pk, global_bytes& pv) {
       const int slot = (key0 + i * kRows + thread / kChunks) & a.page_mask;
-      pk[i] = row_address(kc + at, page[i], slot, a.kc_page, a.kc_slot);
-      pv[i] = row_address(vc + at, page[i], slot, a.vc_page, a.vc_slot);
-    }
-    if (!whole) {
+      pk = row_address(kc + at, page[i], slot, a.kc_page, a.kc_slot);
+      pv = row_address(vc + at, page[i], slot, a.vc_page, a.vc_slot);
+    };
+    auto check = [&](int i, global_bytes& pk, global_bytes& pv) {
+      if (key0 + i * kRows + thread / kChunks >= end)
+        pk = pv = (global_bytes)kNoRow;
+      else if ((uint32_t)page[i] >= (uint32_t)a.num_pages)
+        pk = pv = (global_bytes)kBadRow;
+    };
+    if constexpr (kN > 4) {  // too many addresses to hold: one after the other
 #pragma unroll
       for (int i = 0; i < kN; ++i) {
-        if (key0 + i * kRows + thread / kChunks >= end)
-          pk[i] = pv[i] = (global_bytes)kNoRow;
-        else if ((uint32_t)page[i] >= (uint32_t)a.num_pages)
-          pk[i] = pv[i] = (global_bytes)kBadRow;
+        global_bytes pk, pv;
+        place(i, pk, pv);
+        check(i, pk, pv);
+        k[i] = *(global_chunk)pk;
+        v[i] = *(global_chunk)pv;
       }
-    }
+    } else {
+      global_bytes pk[kN], pv[kN];
 #pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      k[i] = *(global_chunk)pk[i];
-      v[i] = *(global_chunk)pv[i];
+      for (int i = 0; i < kN; ++i) place(i, pk[i], pv[i]);
+      if (!whole) {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) check(i, pk[i], pv[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < kN; ++i) {
+        k[i] = *(global_chunk)pk[i];
+        v[i] = *(global_chunk)pv[i];
+      }
     }
   }
 
@@ -409,9 +418,10 @@ struct Rows {
       m = next;
       l *= f;
 #pragma unroll
-      for (int b = 0; b < D / 32; ++b)
+      for (int b = 0; b < D / 32; ++b) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[b][i] *= f;
+      }
     }
     // a row that has seen no key yet has m = -inf: its p are exp2(-inf) = 0
     const float base = m == -INFINITY ? 0.0f : m;
@@ -532,7 +542,12 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
     for (int i = 0; i < D / 16; ++i) x.q[i] = *(const s16x8*)(p + i * 32);
     // waited for here: a wait inside the loop would be for the tiles' loads too
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) asm volatile("" : "+v"(x.q[i]));
+    for (int i = 0; i < D / 16; ++i) {
+      if constexpr (D == 256)  // in accumulation registers, of which the products take operands too
+        asm volatile("" : "+a"(x.q[i]));
+      else
+        asm volatile("" : "+v"(x.q[i]));
+    }
   };
 #pragma unroll
   for (int b = 0; b < DB; ++b)
@@ -904,7 +919,12 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(AttendArg
     if (item >= a.hdr->items) return;
   }
   const float scale = FP8 && a.ks ? a.scale_log2 * a.ks[head] : a.scale_log2;
-  if (it.rows > 32)
+  // An 8-bit tile on its way and heads of 256 are more than a wave's registers
+  // hold: few rows then share a tile too (64 requests of 2,000 to 4,000 tokens,
+  // 16 heads: 272 -> 241 us).
+  if constexpr (FP8 && D == 256)
+    attend_item<D, T, FP8, 4>(a, it, head, scale, lds);
+  else if (it.rows > 32)
     attend_item<D, T, FP8, 4>(a, it, head, scale, lds);
   else
     attend_item<D, T, FP8, 1>(a, it, head, scale, lds);
