@@ -926,7 +926,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(AttendArg
     attend_item<D, T, FP8, 4>(a, it, head, scale, lds);
   else if (it.rows > 32)
     attend_item<D, T, FP8, 4>(a, it, head, scale, lds);
-  else
+  else  // (sharing tiles here too: 256 requests of one group 196 instead of 183 us)
     attend_item<D, T, FP8, 1>(a, it, head, scale, lds);
 }
 

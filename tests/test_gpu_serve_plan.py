@@ -74,10 +74,30 @@ def test_more_units_than_planning_threads():
 
 
 @pytest.mark.parametrize("heads,new", [(5, 3), (7, 2), (3, 11), (40, 1)])
-def test_requests_that_cross_the_tiles_of_their_group(heads, new):
+@pytest.mark.parametrize("prefix", [300, 6000])
+def test_requests_that_cross_the_tiles_of_their_group(heads, new, prefix):
     # rows of a request that lie in two tiles of 128 rows of its group's prefix
     n = 40
-    p = R.Problem([new] * n, [new + i % 50 for i in range(n)], [n], [300], heads=heads, kv_heads=1, dim=64)
+    p = R.Problem([new] * n, [new + i % 50 for i in range(n)], [n], [prefix], heads=heads, kv_heads=1, dim=64)
+    R.check(*attend(p), p, on_device(p))
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("types", [(BF16, BF16), (FP16, FP16), (BF16, FP8), (FP16, FP8)],
+                         ids=["bf16", "fp16", "bf16-fp8", "fp16-fp8"])
+@pytest.mark.parametrize("page,first", [(1, True), (16, False), (256, True)])
+def test_prefixes_taken_for_a_whole_group(dim, types, page, first):
+    # long enough to be shared: with requests that have no new token, and an empty group between
+    new = [1, 1, 0, 2, 1, 1, 1, 3, 1, 1, 1, 0, 1]
+    own = [a + 37 * i % 150 for i, a in enumerate(new)]
+    p = R.Problem(new, own, [10, 0, 3], [5003, 70, 4800], heads=6, kv_heads=2, dim=dim, page=page, dtype=types[0],
+                  cache=types[1], heads_first=first).spoil()
+    R.check(*attend(p), p, on_device(p))
+
+
+def test_own_tokens_of_length_zero_behind_a_shared_prefix():
+    # the only own token is the new one, of every request
+    p = R.Problem([1] * 40, [1] * 40, [40], [3001], heads=4, kv_heads=1, dim=128)
     R.check(*attend(p), p, on_device(p))
 
 
