@@ -12,10 +12,10 @@ import tempfile
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkvr.so")
-SOURCES = ["kvr_device.hip", "kvr_api.cpp", "kvr_serve.hip", "kvr_serve_api.cpp", "kvr_attend_64.hip",
-           "kvr_attend_128.hip", "kvr_attend_256.hip"]
+# the simulator, and the serving operators
+SOURCES = ["csrc/kvr_device.hip", "csrc/kvr_api.cpp", "csrc_serve/kvr_serve.hip", "csrc_serve/kvr_serve_api.cpp",
+           "csrc_serve/kvr_attend_64.hip", "csrc_serve/kvr_attend_128.hip", "csrc_serve/kvr_attend_256.hip"]
 ARCH = os.environ.get("KVR_OFFLOAD_ARCH", "gfx950")
 
 FLAGS = [
@@ -31,7 +31,7 @@ FLAGS = [
 # of single sources: in the attention kernels scalar registers are short, and
 # this scheduler counts them (without it they spill into the inner loop: 924
 # against 804 us for 9,216 new tokens of 32 heads)
-EXTRA = {f"kvr_attend_{d}.hip": ["-mllvm", "-amdgpu-use-amdgpu-trackers=1"] for d in (64, 128, 256)}
+EXTRA = {f"csrc_serve/kvr_attend_{d}.hip": ["-mllvm", "-amdgpu-use-amdgpu-trackers=1"] for d in (64, 128, 256)}
 
 
 def hipcc() -> str:
@@ -56,9 +56,9 @@ def build(verbose: bool = False) -> str:
             print(err, file=sys.stderr)
 
     with tempfile.TemporaryDirectory() as tdir, ThreadPoolExecutor(max_workers=len(SOURCES)) as pool:
-        objects = [os.path.join(tdir, os.path.splitext(s)[0] + ".o") for s in SOURCES]
+        objects = [os.path.join(tdir, os.path.splitext(os.path.basename(s))[0] + ".o") for s in SOURCES]
         list(pool.map(run, [[hipcc(), f"--offload-arch={ARCH}", *FLAGS, *EXTRA.get(s, []), "-c", "-o", o,
-                             os.path.join(CSRC, s)]
+                             os.path.join(HERE, s)]
                             for s, o in zip(SOURCES, objects)]))
         run([hipcc(), f"--offload-arch={ARCH}", "-fPIC", "-shared", "-o", tmp, *objects])
     os.replace(tmp, LIB)

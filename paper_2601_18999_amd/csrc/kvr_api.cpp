@@ -14,7 +14,6 @@
 #include <string>
 
 #include "kvr_layout.h"
-#include "kvr_serve.h"
 
 namespace kvr {
 hipError_t launch_init(char* ws, const Layout& L, double rls_p0, hipStream_t st);
@@ -144,6 +143,7 @@ std::string describe_bits(uint32_t bits) {
 }  // namespace
 
 namespace kvr {
+// for the serving operators' entry points (csrc_serve/)
 kvr_status set_error(kvr_status st, const char* msg) noexcept {
   try {
     g_err = msg;
