@@ -29,6 +29,7 @@
 // the rounded result; the sum l adds the unrounded p.
 #pragma once
 
+#include <atomic>
 #include <type_traits>
 
 #include "kvr_plan.h"
@@ -61,6 +62,7 @@ struct Bf16 {
     return __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true));
   }
   static constexpr int kExponent = 0x7f80;  // exponent bits: all ones = infinity or NaN
+  static constexpr float kLift = 0.0f;
 };
 
 struct Fp16 {
@@ -77,6 +79,8 @@ struct Fp16 {
     return __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true));
   }
   static constexpr int kExponent = 0x7c00;
+  // p is up to 2^kLift at a row's maximum: halves end at 2^-24 below and 2^16 above
+  static constexpr float kLift = 7.0f;
 };
 
 // 16-byte chunks of a row in LDS stand at chunk ^ swizzle(row).  K is read a
@@ -128,7 +132,7 @@ struct Shape {
   static constexpr int kJoin = kKeyGroups == 1 ? 0 : kKeyGroups * RW * 32 * (8 + 4 * D);
   static constexpr int kMain = kTiles > kJoin ? kTiles : kJoin;
   static constexpr int kPages = RW == 1 ? 4 * 2 * 256 : 0;  // page numbers of a wave's next two tiles
-  static constexpr int kBytes = kMain + kPages + 64;        // + flags
+  static constexpr int kBytes = kMain + kPages;
 };
 
 template <int D>
@@ -327,7 +331,7 @@ __device__ __forceinline__ s16x4 round4(float a, float b, float c, float d) {
 // kinds of instructions for the scheduler
 constexpr int kProducts = 0x8, kReads = 0x100;
 
-constexpr float kSlack = 8.0f;  // p < 2^8: far from the largest half, and l from the largest float
+constexpr float kSlack = 8.0f;  // p <= 2^(kLift + 8): below the largest half, and l far below the largest float
 
 // A wave's 32 rows: queries, running maximum (log2 units) and sum, results.
 template <int D, class T>
@@ -410,9 +414,9 @@ struct Rows {
     top = max3(top, s[KB - 1][15], s[KB - 1][15]);
     top = half_max(top) * scale;
     // m need not be the maximum, only near it: o and l are scaled when a row's
-    // maximum has grown by more than 2^kSlack, which p then stays below
-    if (__any(top > m + kSlack)) {
-      const float next = fmaxf(m, top);
+    // maximum has grown by more than 2^kSlack
+    if (__any(top > m + (T::kLift + kSlack))) {
+      const float next = fmaxf(m, top - T::kLift);
       // before the first key of a row: nothing to scale
       const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - next);
       m = next;
@@ -895,6 +899,10 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
   }
 }
 
+// Many rows: bound by the matrix and the vector unit, whose times add up (9,216
+// new tokens of 32 / 8 heads of 128: 710 to 720 us, 970 to 990 TFLOP/s, where a
+// library product reaches 1,264).  Few rows: bound by memory (64 requests in
+// four groups, 243 MB: 50 us, 4.9 TB/s, where a copy reaches 5.1).
 template <int D, class T, bool FP8>
 __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(AttendArgs a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -934,9 +942,17 @@ template <int D, class T, bool FP8>
 hipError_t launch_attend_as(const AttendArgs& a, hipStream_t st) {
   constexpr int lds = attend_lds<D>();
   static_assert(lds * (D == 256 ? 1 : 2) <= 160 * 1024, "LDS of a compute unit");
-  static const hipError_t set = hipFuncSetAttribute((const void*)attend_kernel<D, T, FP8>,
-                                                    hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-  if (set != hipSuccess) return set;
+  // once a device: LDS beyond the default limit
+  static std::atomic<uint64_t> allowed{0};
+  int device = 0;
+  hipError_t e = hipGetDevice(&device);
+  if (e != hipSuccess) return e;
+  const uint64_t bit = device < 64 ? 1ull << device : 0;
+  if (!(allowed.load(std::memory_order_relaxed) & bit)) {
+    e = hipFuncSetAttribute((const void*)attend_kernel<D, T, FP8>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+    allowed.fetch_or(bit, std::memory_order_relaxed);
+  }
   attend_kernel<D, T, FP8><<<dim3((uint32_t)a.item_cap * (uint32_t)a.kv_heads), dim3(256), lds, st>>>(a);
   return hipGetLastError();
 }

@@ -157,6 +157,40 @@ def test_a_row_is_the_same_with_and_without_a_group():
     R.check(*attend(q), q, want)
 
 
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("cache", [None, FP8], ids=["16-bit", "8-bit"])
+def test_keys_and_values_laid_out_differently(dim, cache):
+    p = R.Problem([1, 100], [333, 300], [1, 1], [64, 200], heads=4, kv_heads=2, dim=dim, cache=cache)
+    args = p.args()
+    pages, page, heads, _ = args[2].shape
+    v = torch.empty((heads, pages, 2, page, dim), dtype=args[2].dtype, device=DEV)
+    v[:, :, 1] = args[2].permute(2, 0, 1, 3)
+    args[2] = v[:, :, 1].permute(1, 2, 0, 3)
+    assert args[2].stride() != args[1].stride()
+    R.check(K.shared_attention(*args, **p.kwargs()), None, p, on_device(p))
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
+def test_many_small_weights_beside_a_large_one(dtype):
+    # one key with a score 17 above 30,000 others: their weights, 4e-8 each and 1.2e-3 in all, count
+    p = R.Problem([1], [30001], heads=1, kv_heads=1, dim=64, dtype=dtype, page=64)
+    p.q[:] = 0
+    p.q[..., 0] = 1.0
+    p.scale = 1.0
+    p.k_cache[..., 0] = 0.0
+    p.v_cache[:] = 100.0
+    first = (p.table[0, 0], 0)
+    p.k_cache[first[0], first[1], 0, 0] = 17.0
+    p.v_cache[first[0], first[1]] = 0.0
+    ref, size, _ = p.expect()
+    out, _ = attend(p)
+    # p and the result rounded once each; halves have steps of 2^-24 * 2^-7 at the small end: half a step each
+    u = 2.0 ** -8 if dtype == BF16 else 2.0 ** -11
+    step = 0.0 if dtype == BF16 else 30000 * 100.0 * 2.0 ** -32
+    err = (out.double().cpu() - ref).abs()
+    assert (err <= 2.1 * u * ref.abs() + 8e-4 * size + step).all(), (float(err.max()), float(ref.max()))
+
+
 @pytest.mark.parametrize("rows,tokens", [(1024, 4096), (1025, 100), (1024, 4097), (1, 1), (64, 0), (4096, 5000)])
 def test_table_sizes_around_the_forms(rows, tokens):
     rng = np.random.default_rng(rows + tokens)
