@@ -221,7 +221,8 @@ struct Direct {
   // Pages of kRows tokens or more: the rows of one load stand in one page, so
   // a load has one base, in scalar registers, and lane offsets that stay the
   // same from tile to tile but for the swizzle of load i (the rows of one load
-  // and i's multiples share no bits, so the swizzles are xored).
+  // and i's multiples share no bits, so the swizzles are xored).  Addresses by
+  // lane, as smaller pages need them: 757 instead of 739 us for 9,216 tokens.
   struct Offsets {
     uint32_t k_row, k_chunk, v_row, v_chunk;
   };
@@ -525,7 +526,8 @@ template <int D, class T, bool FP8, int RW>
 __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it, int head, float scale, char* lds) {
   typedef Shape<D, RW> S;
   constexpr int KG = S::kKeyGroups, KT = S::kKeys, KB = KT / 32, DB = D / 32;
-  // reads ahead, as many as there are registers for
+  // reads ahead, as many as there are registers for (9,216 new tokens: 739 us
+  // without, 731 with them)
   constexpr int kAhead = D == 256 || FP8 ? 4 : D == 64 && RW == 1 ? 4 : 8;
   constexpr bool kEarly = RW > 1 && D <= 128 && !FP8;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);

@@ -70,8 +70,10 @@ __device__ __forceinline__ int last_at_most(P start, int n, int x) {
 
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanSmall = 1024;  // requests, groups: their lengths then stand in LDS
-constexpr int kPlanFused = 64;    // ... and units: each workgroup of the attention then makes the plan itself
-constexpr int kMinSplitCost = 8;  // least cost of an item that a unit is split into
+constexpr int kPlanFused = 256;   // ... and units: each workgroup of the attention may make the plan itself
+// Least cost of an item that a unit is split into (over 15 calls of all kinds 4
+// and 16 were 2% slower).
+constexpr int kMinSplitCost = 8;
 
 constexpr int plan_words(int cap) { return 48 + (cap ? 8 * (cap + 1) : 0); }
 

@@ -13,7 +13,8 @@
 namespace kvr {
 
 // Compute units of a gfx950 device and the attention workgroups that one of
-// them holds: the width that the attention work is split for.
+// them holds: the width that the attention work is split for (for three or four
+// a unit 15 calls of all kinds were 2 and 5% slower).
 constexpr int kComputeUnits = 256;
 constexpr int kAttendSlots = 2 * kComputeUnits;
 constexpr int kTileRows = 128;  // most query rows of an attention workgroup

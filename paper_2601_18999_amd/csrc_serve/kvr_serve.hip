@@ -365,11 +365,14 @@ hipError_t launch_store(const StoreArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-// Up to 64 units each workgroup plans for itself, which saves a launch (eight
-// requests 18.8 -> 15.9 us, 33 requests 26.8 -> 25.1 us; with 72 units it was
-// no faster).
+// Each workgroup plans for itself, which saves a launch, while the device holds
+// most of them at once (eight requests, 18.8 -> 15.9 us; 64 requests, 77.5 ->
+// 76.3; 157 requests of one key head, 20.8 -> 18.8).  Where they come in several
+// rounds each round pays (127 requests, eight heads of 256: 90 -> 99 us).
 bool attend_fused(const AttendArgs& a) {
-  return a.unit_cap <= kPlanFused && a.requests <= kPlanFused && a.groups <= kPlanFused;
+  const int64_t held = (a.dim == 256 ? 1 : 2) * kComputeUnits;
+  return a.unit_cap <= kPlanFused && a.requests <= kPlanFused && a.groups <= kPlanFused &&
+         (int64_t)a.unit_cap * a.kv_heads <= 2 * held;
 }
 
 hipError_t launch_attend_plan(const AttendArgs& a, hipStream_t st) {
