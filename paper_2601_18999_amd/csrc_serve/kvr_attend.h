@@ -916,6 +916,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(AttendArg
     const int items = make_plan<kPlanFused>(a, (int*)lds, blockIdx.x == 0, [&](int i, const Item& x) {
       if (i == item) *mine = x;
     });
+    if (items < 0 && a.direct) fill_with_nan(a);
     if (item >= items) return;
     __syncthreads();
     it = *mine;
@@ -926,6 +927,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(AttendArg
     __syncthreads();
   } else {
     it = a.items[item];  // (there is room for as many as there are workgroups)
+    if (a.direct && a.hdr->rejected) fill_with_nan(a);
     if (item >= a.hdr->items) return;
   }
   const float scale = FP8 && a.ks ? a.scale_log2 * a.ks[head] : a.scale_log2;

@@ -74,6 +74,7 @@ constexpr int kPlanFused = 256;   // ... and units: each workgroup of the attent
 // Least cost of an item that a unit is split into (over 15 calls of all kinds 4
 // and 16 were 2% slower).
 constexpr int kMinSplitCost = 8;
+constexpr int kMinSharedSteps = 4;  // of a prefix that is taken for a group
 
 constexpr int plan_words(int cap) { return 48 + (cap ? 8 * (cap + 1) : 0); }
 
@@ -93,8 +94,19 @@ __device__ __forceinline__ int steps_of(int keys) { return (keys + kStepKeys - 1
 // heads: 256 keys 34.3 apart, 33.6 together, 2,048 keys 67.9 and 40.5; 16
 // requests: 512 keys 19.0 and 19.8, 1,024 keys 21.1 and 20.9).
 __device__ __forceinline__ bool worth_sharing(int apart, int together, int steps, int kv_heads) {
-  return (int64_t)together * 4 <= (int64_t)apart * 3 && steps >= 4 &&
+  return (int64_t)together * 4 <= (int64_t)apart * 3 && steps >= kMinSharedSteps &&
          (int64_t)(apart - together) * steps * kv_heads >= 256;
+}
+
+// Lengths that are not valid: nothing was computed, every result is NaN.
+__device__ __forceinline__ void fill_with_nan(const AttendArgs& a) {
+  const int quads = a.dim / 4;
+  const int64_t all = (int64_t)a.tokens * a.heads * quads, step = (int64_t)gridDim.x * blockDim.x;
+  for (int64_t i = blockIdx.x * (int64_t)blockDim.x + threadIdx.x; i < all; i += step) {
+    const int64_t th = i / quads;
+    *(int2*)(a.out + th / a.heads * a.o_tok + th % a.heads * a.o_head + i % quads * 8) = make_int2(-1, -1);
+    if (a.lse && i % quads == 0) a.lse[th] = __uint_as_float(0x7fc00000u);
+  }
 }
 
 struct UnitWork {
@@ -169,7 +181,7 @@ __device__ UnitWork unit_work(const AttendArgs& a, const Lengths& z, int s, int 
 // CAP > 0: the lengths of up to CAP requests and groups stand in LDS.  `write`:
 // what others read of the plan (its header and units) is written; every item
 // goes to emit(its number, the item).  `lds`: plan_words(CAP) words.  Returns
-// the number of items.
+// the number of items, -1 for lengths that are not valid.
 template <int CAP, class Emit>
 __device__ __forceinline__ int make_plan(const AttendArgs& a, int* lds, bool write, Emit emit) {
   constexpr bool SMALL = CAP > 0;
@@ -233,7 +245,7 @@ __device__ __forceinline__ int make_plan(const AttendArgs& a, int* lds, bool wri
       a.hdr->rejected = 1;
       if (a.status) atomicOr(a.status, (uint32_t)KVR_DEV_BAD_LENGTH);
     }
-    return 0;
+    return -1;
   }
   // waves along the rows that the requests of a group take one by one
   for (int b = tid; b < a.requests && a.groups; b += threads) {

@@ -129,13 +129,15 @@ struct AttendArgs {
   int32_t tokens, requests, groups, heads, kv_heads, dim;
   int32_t page_shift, page_mask, num_pages, width, prefix_width;
   int32_t unit_cap, item_cap, join_cap, split_slots;
-  int32_t fused;  // 1: no plan kernel
+  int32_t fused, direct;  // 1: no plan kernel; no join kernel
 };
 
 hipError_t launch_tables(const TablesArgs& a, hipStream_t st);
 hipError_t launch_store(const StoreArgs& a, hipStream_t st);
 // whether every workgroup of the attention makes the plan itself
 bool attend_fused(const AttendArgs& a);
+// whether there can be nothing to join
+bool attend_direct(const AttendArgs& a);
 hipError_t launch_attend_plan(const AttendArgs& a, hipStream_t st);
 hipError_t launch_attend_join(const AttendArgs& a, bool fp16, hipStream_t st);
 // fp16: queries and results are 16-bit IEEE, else bfloat16; fp8: the cache

@@ -321,6 +321,7 @@ kvr_status kvr_shared_attention(const kvr_cache* c, const kvr_attention* s, void
   a.join_cap = l.join_cap;
   a.split_slots = l.split_slots;
   a.fused = kvr::attend_fused(a);
+  a.direct = kvr::attend_direct(a);
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const bool fp16 = s->dtype == KVR_FP16, fp8 = c->dtype == KVR_FP8;
   hipError_t e = kvr::launch_attend_plan(a, stream);

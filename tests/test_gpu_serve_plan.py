@@ -95,6 +95,21 @@ def test_prefixes_taken_for_a_whole_group(dim, types, page, first):
     R.check(*attend(p), p, on_device(p))
 
 
+@pytest.mark.parametrize("own,prefix", [(64, 0), (128, 0), (129, 0), (512, 0), (513, 0), (320, 192), (321, 192),
+                                        (320, 193), (64, 64)])
+@pytest.mark.parametrize("requests", [1, 16, 17, 300])
+def test_tables_with_room_for_few_keys(own, prefix, requests):
+    # at most eight steps of 64 keys (two where there are more than 32 rows) and a short prefix: nothing to join;
+    # one token more, and there may be.  Valid lengths, then one that is not.
+    p = R.Problem([1] * requests, [own - 7 * i % own for i in range(requests)], [requests] if prefix else [],
+                  [prefix] if prefix else [], heads=2, kv_heads=1, dim=64, page=1)
+    R.check(*attend(p), p, on_device(p))
+    p.length[-1] = p.table.shape[1] + 1
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    out, lse = attend(p, status=status)
+    assert int(status) == 1 and torch.isnan(out).all() and torch.isnan(lse).all()
+
+
 def test_own_tokens_of_length_zero_behind_a_shared_prefix():
     # the only own token is the new one, of every request
     p = R.Problem([1] * 40, [1] * 40, [40], [3001], heads=4, kv_heads=1, dim=128)
