@@ -78,10 +78,11 @@ constexpr int kMinSharedSteps = 4;  // of a prefix that is taken for a group
 
 constexpr int plan_words(int cap) { return 48 + (cap ? 8 * (cap + 1) : 0); }
 
-// Waves along the rows that `rows` rows take in tiles of kTileRows.
-__device__ __forceinline__ int row_waves(int rows) {
+// Waves along the rows that `rows` rows take in tiles of kTileRows; `few`: that
+// up to 32 rows take.
+__device__ __forceinline__ int row_waves(int rows, int few) {
   const int rest = rows % kTileRows;
-  return rows / kTileRows * 4 + (rest == 0 ? 0 : rest <= 32 ? 1 : 4);
+  return rows / kTileRows * 4 + (rest == 0 ? 0 : rest <= 32 ? few : 4);
 }
 
 __device__ __forceinline__ int steps_of(int keys) { return (keys + kStepKeys - 1) / kStepKeys; }
@@ -172,7 +173,7 @@ __device__ UnitWork unit_work(const AttendArgs& a, const Lengths& z, int s, int 
     w.steps = w.it.prefix_steps + steps_of(w.it.own_end);
   }
   w.it.step1 = w.steps;
-  w.cost = w.steps * row_waves(w.it.rows);
+  w.cost = w.steps * row_waves(w.it.rows, a.few_waves);
   return w;
 }
 
@@ -251,7 +252,7 @@ __device__ __forceinline__ int make_plan(const AttendArgs& a, int* lds, bool wri
   for (int b = tid; b < a.requests && a.groups; b += threads) {
     const int j = last_at_most(z.group_start, a.groups, b);
     z.group_of[b] = j;
-    atomicAdd(&z.waves[j], row_waves((z.start(b + 1) - z.start(b)) * g));
+    atomicAdd(&z.waves[j], row_waves((z.start(b + 1) - z.start(b)) * g, a.few_waves));
   }
   __syncthreads();
   // units: a group's (its prefix, if that is shared), then a request's
@@ -262,7 +263,7 @@ __device__ __forceinline__ int make_plan(const AttendArgs& a, int* lds, bool wri
     int count = 0;
     if (s < a.groups) {
       const int rows = (z.start(z.group_start[s + 1]) - z.start(z.group_start[s])) * g;
-      const bool shared = worth_sharing(z.waves[s], row_waves(rows), steps_of(z.prefix_length[s]), a.kv_heads);
+      const bool shared = worth_sharing(z.waves[s], row_waves(rows, a.few_waves), steps_of(z.prefix_length[s]), a.kv_heads);
       z.waves[s] = shared ? 1 : 0;
       count = shared ? (rows + kTileRows - 1) / kTileRows : 0;
     } else if (s < segments) {
@@ -286,7 +287,8 @@ __device__ __forceinline__ int make_plan(const AttendArgs& a, int* lds, bool wri
   }
   group_before(total, total, part64);
   const int64_t fair = (total + a.split_slots - 1) / a.split_slots;
-  const int chunk = (int)(fair < kMinSplitCost ? kMinSplitCost : fair > 0x7fffffff ? 0x7fffffff : fair);
+  const int least = kMinSplitCost * a.few_waves;
+  const int chunk = (int)(fair < least ? least : fair > 0x7fffffff ? 0x7fffffff : fair);
   int items = 0, rows_acc = 0, joins = 0;
   for (int u0 = 0; u0 < units; u0 += threads) {
     const int u = u0 + tid;

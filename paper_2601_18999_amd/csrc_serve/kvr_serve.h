@@ -129,6 +129,7 @@ struct AttendArgs {
   int32_t tokens, requests, groups, heads, kv_heads, dim;
   int32_t page_shift, page_mask, num_pages, width, prefix_width;
   int32_t unit_cap, item_cap, join_cap, split_slots;
+  int32_t few_waves;      // waves along the rows that up to 32 rows take (attend_kernel): 1 or 4
   int32_t fused, direct;  // 1: no plan kernel; no join kernel
 };
 

@@ -377,7 +377,7 @@ bool attend_direct(const AttendArgs& a) {
   const int64_t page = 1ll << a.page_shift;
   const int64_t own = (a.width * page + kStepKeys - 1) / kStepKeys;
   const int64_t prefix = a.groups ? (a.prefix_width * page + kStepKeys - 1) / kStepKeys : 0;
-  const int64_t waves = (int64_t)a.tokens * a.share.d <= 32 ? 1 : 4;
+  const int64_t waves = (int64_t)a.tokens * a.share.d <= 32 ? a.few_waves : 4;
   return prefix < kMinSharedSteps && (own + prefix) * waves <= kMinSplitCost;
 }
 

@@ -320,6 +320,7 @@ kvr_status kvr_shared_attention(const kvr_cache* c, const kvr_attention* s, void
   a.item_cap = l.item_cap;
   a.join_cap = l.join_cap;
   a.split_slots = l.split_slots;
+  a.few_waves = c->dtype == KVR_FP8 && c->dim == 256 ? 4 : 1;
   a.fused = kvr::attend_fused(a);
   a.direct = kvr::attend_direct(a);
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
