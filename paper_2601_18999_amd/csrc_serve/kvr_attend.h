@@ -221,8 +221,9 @@ struct Direct {
   // Pages of kRows tokens or more: the rows of one load stand in one page, so
   // a load has one base, in scalar registers, and lane offsets that stay the
   // same from tile to tile but for the swizzle of load i (the rows of one load
-  // and i's multiples share no bits, so the swizzles are xored).  Addresses by
-  // lane, as smaller pages need them: 757 instead of 739 us for 9,216 tokens.
+  // and i's multiples share no bits, so the swizzles are xored).  The offsets
+  // have 32 bits, so the rows have to be near enough (lanes_reach).  Addresses
+  // by lane, as other caches need them: 757 instead of 739 us for 9,216 tokens.
   struct Offsets {
     uint32_t k_row, k_chunk, v_row, v_chunk;
   };
@@ -635,7 +636,7 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
       load4_to_lds(p.table + (key >> a.page_shift), id_to + (j & 1) * 256);
     };
     const typename L::Offsets offsets = L::offsets(a, 0, lane);
-    const bool uniform = (1 << a.page_shift) >= L::kRows;
+    const bool uniform = a.one_base;
     // whether all rows of tile j are keys in pages of the cache; a page outside it is reported
     auto whole_of_ids = [&](const Place& p, int j) {
       const bool bad = (uint32_t)ids[(j & 1) * 64 + n] >= (uint32_t)a.num_pages;
@@ -754,7 +755,7 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
       const int row0 = L::first(rw, lane), step = RW * L::kRows;
       const uint32_t to = lds_offset(lds);
       const typename L::Offsets offsets = L::offsets(a, rw, lane);
-      const bool uniform = (1 << a.page_shift) >= L::kRows;
+      const bool uniform = a.one_base;
       auto load = [&](const Place& q, uint32_t at) {
         const bool whole = whole_of(q, page);
         if (whole && uniform) {

@@ -41,6 +41,13 @@ __host__ __device__ inline uint32_t divide(uint32_t n, const Divisor& v) {
   return (uint32_t)(((uint64_t)n * v.mul) >> (31 + v.shift));
 }
 
+// Whether the lanes of one load of a tile of a 16-bit cache reach their rows by
+// 32-bit offsets from the first row's.  A load brings 1,024 neighbouring bytes
+// to LDS, so it spans 512 / dim rows, `stride` bytes apart in the cache.
+constexpr bool lanes_reach(int dim, int64_t stride) {
+  return (512 / dim - 1) * stride + 2 * dim <= (int64_t)1 << 32;
+}
+
 // ---- page tables ----
 struct TablesHdr {
   int64_t head, tail;  // the ring before the call
@@ -131,6 +138,7 @@ struct AttendArgs {
   int32_t unit_cap, item_cap, join_cap, split_slots;
   int32_t few_waves;      // waves along the rows that up to 32 rows take (attend_kernel): 1 or 4
   int32_t fused, direct;  // 1: no plan kernel; no join kernel
+  int32_t one_base;       // 1: the rows of one load stand in one page and reach of one base
 };
 
 hipError_t launch_tables(const TablesArgs& a, hipStream_t st);

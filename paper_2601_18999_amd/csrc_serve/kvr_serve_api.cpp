@@ -321,6 +321,7 @@ kvr_status kvr_shared_attention(const kvr_cache* c, const kvr_attention* s, void
   a.join_cap = l.join_cap;
   a.split_slots = l.split_slots;
   a.few_waves = c->dtype == KVR_FP8 && c->dim == 256 ? 4 : 1;
+  a.one_base = c->page_size >= 512 / c->dim && kvr::lanes_reach(c->dim, a.kc_slot) && kvr::lanes_reach(c->dim, a.vc_slot);
   a.fused = kvr::attend_fused(a);
   a.direct = kvr::attend_direct(a);
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
