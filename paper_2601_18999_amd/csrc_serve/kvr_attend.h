@@ -893,7 +893,8 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
 #pragma unroll
       for (int g = 0; g < KG; ++g) {
         const float mg = jm[g * ROWS + rr];
-        if (mg != -INFINITY) ll += jl[g * ROWS + rr] * __builtin_amdgcn_exp2f(mg - mm);
+        // (a group without a maximum has the sum 0, or NaN where a score was)
+        ll += mg == -INFINITY ? jl[g * ROWS + rr] : jl[g * ROWS + rr] * __builtin_amdgcn_exp2f(mg - mm);
         y += *(const f32x4*)(jo + (g * ROWS + rr) * D + (c ^ (rr & 15)) * 4);
       }
       emit(rr, c * 4, y, ll);

@@ -35,3 +35,90 @@ def test_slots_far_apart(dim, page, stride, wide):
         if wide in (name, "both"):
             args[i] = slots_apart(args[i], stride, storage, (i - 1) << 20)
     R.check(K.shared_attention(*args, **p.kwargs()), None, p, on_device(p))
+
+
+NAN_TYPES = [(BF16, None), (FP16, None), (BF16, FP8)]
+NAN_IDS = ["bf16", "fp16", "bf16-fp8"]
+
+
+def put_nan(cache, table, t, head, element):
+    """NaN in one element of a token of the cache."""
+    page = cache.shape[1]
+    at = (int(table[t // page]), t % page, head, element)
+    if cache.dtype == FP8:
+        cache.view(torch.uint8)[at] = 0x7f
+    else:
+        cache[at] = float("nan")
+
+
+def check_beside_nan(out, lse, p):
+    """NaN exactly where the definition has it, in the result and in lse; the rest as everywhere."""
+    ref, size, ref_lse = on_device(p)
+    out, lse = out.cpu(), lse.cpu()
+    assert torch.equal(torch.isnan(out), torch.isnan(ref))
+    assert torch.equal(torch.isnan(lse), torch.isnan(ref_lse))
+    bad, bad_lse = torch.isnan(ref), torch.isnan(ref_lse)
+    R.check(out.masked_fill(bad, 0.0), lse.masked_fill(bad_lse, 0.0), p,
+            [ref.masked_fill(bad, 0.0), size.masked_fill(bad, 0.0), ref_lse.masked_fill(bad_lse, 0.0)])
+    return bad, bad_lse
+
+
+# single tokens: 32, 40 (one wave has no second tile), 128 and 20,011 keys (split); behind a prefix that is shared by a
+# group; 200 rows of one request
+@pytest.mark.parametrize("new,own,sizes,prefix", [([1], [32], (), ()), ([1], [40], (), ()), ([1], [128], (), ()),
+                                                  ([1], [20011], (), ()), ([1] * 24, [33] * 24, [24], [2100]),
+                                                  ([50], [90], (), ())],
+                         ids=["32", "40", "128", "20011", "group", "rows"])
+@pytest.mark.parametrize("types", NAN_TYPES, ids=NAN_IDS)
+@pytest.mark.parametrize("dim", [64, 256])
+def test_a_nan_key_makes_result_and_lse_nan(new, own, sizes, prefix, types, dim):
+    for t in {0, 31, own[0] - new[0] - 1, own[0] // 2 - 20 if own[0] > 100 else 5}:
+        p = R.Problem(new, own, sizes, prefix, heads=8, kv_heads=2, dim=dim, dtype=types[0], cache=types[1])
+        put_nan(p.k_cache, p.table[0], t, 1, 7)
+        out, lse = attend(p)
+        bad, bad_lse = check_beside_nan(out, lse, p)
+        assert bad[:new[0], 4:].all() and bad_lse[:new[0], 4:].all() and int(bad_lse.sum()) == 4 * new[0]
+
+
+def test_a_nan_key_of_a_shared_prefix_reaches_its_whole_group():
+    for prefix in (40, 2100):
+        p = R.Problem([1] * 24, [33] * 24, [20, 4], [prefix, 50], heads=4, kv_heads=2, dim=128)
+        put_nan(p.k_cache, p.prefix_table[0], prefix - 3, 0, 0)
+        out, lse = attend(p)
+        bad, bad_lse = check_beside_nan(out, lse, p)
+        assert bad_lse[:20, :2].all() and int(bad_lse.sum()) == 40
+
+
+def test_a_nan_query_makes_its_result_and_lse_nan():
+    for own in (1, 40, 3000):
+        p = R.Problem([1, 1, 30], [own, 9, 60], [2, 1], [70, 5], heads=4, kv_heads=2, dim=128)
+        p.q[0, 2, 5] = p.q[11, 0, 0] = float("nan")
+        out, lse = attend(p)
+        _, bad_lse = check_beside_nan(out, lse, p)
+        assert bad_lse[0, 2] and bad_lse[11, 0] and int(bad_lse.sum()) == 2
+
+
+def test_a_nan_value_leaves_lse():
+    for own in (40, 3000):
+        p = R.Problem([1, 3], [own, 90], heads=4, kv_heads=2, dim=128)
+        put_nan(p.v_cache, p.table[0], 20, 1, 9)
+        put_nan(p.v_cache, p.table[1], 50, 0, 100)
+        bad, bad_lse = check_beside_nan(*attend(p), p)
+        assert bad[0, 2:, 9].all() and bad[1:, :2, 100].all() and int(bad.sum()) == 8 and not bad_lse.any()
+
+
+@pytest.mark.parametrize("own,heads", [(40, 4), (5000, 4), (300, 80)], ids=["few", "split", "rows"])
+@pytest.mark.parametrize("cache", [None, FP8], ids=["16-bit", "8-bit"])
+@pytest.mark.parametrize("page", [-1, 1 << 30])
+def test_a_page_outside_the_cache_makes_result_and_lse_nan(own, heads, cache, page):
+    p = R.Problem([1, 1, 1], [own] * 3, [2, 1], [40, 5], heads=heads, kv_heads=2, dim=128, cache=cache)
+    want = on_device(p)
+    for at in {0, (own - 1) // 16, own // 32}:
+        q = R.Problem([1, 1, 1], [own] * 3, [2, 1], [40, 5], heads=heads, kv_heads=2, dim=128, cache=cache)
+        q.table[1, at] = page
+        status = torch.zeros(1, dtype=torch.int32, device=DEV)
+        out, lse = attend(q, status=status)
+        assert int(status) == 512
+        assert torch.isnan(out[1]).all() and torch.isnan(lse[1]).all()
+        for i in (0, 2):
+            R.check(out[i:i + 1], lse[i:i + 1], p, [x[i:i + 1] for x in want])
