@@ -179,9 +179,10 @@ __global__ void __launch_bounds__(kFillThreads) tables_fill_kernel(TablesArgs a)
     if (first + lane < a.num_tokens) place_token(a, h, a.row_start, a.gain_at, first + lane, r);
   }
   if (h.rejected) return;
-  for (int g = first; g < h.give; g += gridDim.x * kFillThreads) {
-    const int r = last_at_most_of_lanes(a.give_at, a.rows, g);
-    if (g + lane < h.give) drop_page(a, h, a.give_at, g + lane, r);
+  // (64 bits: the grid may have 2^31 threads)
+  for (int64_t at = first; at < h.give; at += (int64_t)gridDim.x * kFillThreads) {
+    const int g = (int)at, r = last_at_most_of_lanes(a.give_at, a.rows, g);
+    if (lane < h.give - g) drop_page(a, h, a.give_at, g + lane, r);
   }
 }
 
@@ -344,7 +345,7 @@ hipError_t launch_tables(const TablesArgs& a, hipStream_t st) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   // blocks for the tokens; with few new tokens there may be many pages to give back
-  int blocks = (a.num_tokens + kFillThreads - 1) / kFillThreads;
+  int blocks = (int)(((int64_t)a.num_tokens + kFillThreads - 1) / kFillThreads);
   const int least = a.rows / 16 + 1 < 256 ? a.rows / 16 + 1 : 256;
   if (blocks < least) blocks = least;
   tables_fill_kernel<<<dim3(blocks), dim3(kFillThreads), 0, st>>>(a);

@@ -1,5 +1,6 @@
 """The serving operators on the GPU at the edges of their number ranges and
 rules: wide strides, NaN, sizes around the forms of the plan."""
+import numpy as np
 import pytest
 import torch
 
@@ -122,3 +123,31 @@ def test_a_page_outside_the_cache_makes_result_and_lse_nan(own, heads, cache, pa
         assert torch.isnan(out[1]).all() and torch.isnan(lse[1]).all()
         for i in (0, 2):
             R.check(out[i:i + 1], lse[i:i + 1], p, [x[i:i + 1] for x in want])
+
+
+@pytest.mark.parametrize("tokens", [(1 << 31) - 1, (1 << 31) - 256, (1 << 31) - 257, 1 << 30])
+def test_tables_with_room_for_the_most_tokens(tokens):
+    # an upper bound of 2^31 tokens for a batch of few, which gives back more pages than a block of threads has
+    rows = 3000
+    rng = np.random.default_rng(11)
+    held = np.full(rows, 2, np.int32)
+    delta = np.where(np.arange(rows) % 5 == 4, 3, -2).astype(np.int32)
+    pool = 2 * rows + 2000
+    order = rng.permutation(pool).astype(np.int32)
+    table = np.full((rows, 5), -1, np.int32)
+    table[:, :2] = order[:2 * rows].reshape(rows, 2)
+    ring, state = np.roll(order, -2 * rows), np.array([0, 2000, 0])
+    new = int(np.maximum(delta, 0).sum())
+    want, bits = R.tables(held, delta, table, ring, state, 1, new, held)
+    assert not bits
+    on = [torch.from_numpy(x.copy()).to(DEV) for x in (held, delta, table, ring, state)]
+    note(f"tables rows={rows} tokens={tokens}")
+    r = K.block_tables(*on, 1, tokens, base=on[0])
+    got = dict(table=on[2], ring=on[3], held=r.held, state=r.state, row_start=r.row_start, slots=r.slots[:new],
+               positions=r.positions[:new])
+    for k, v in got.items():
+        np.testing.assert_array_equal(v.cpu().numpy(), want[k], err_msg=k)
+    for x in (r.slots, r.positions):
+        assert x.shape == (tokens,)
+        for a in range(new, tokens, 1 << 28):
+            assert int((x[a:a + (1 << 28)] != -1).sum()) == 0
