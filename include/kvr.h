@@ -332,7 +332,8 @@ enum { KVR_BF16 = 0, KVR_FP16 = 1, KVR_FP8 = 2 }; /* element types; KVR_FP8: OCP
  * d_row_start[r] = new tokens of the rows before r ([rows + 1]); and for new
  * token t, counted over the rows, d_slots[t] = page * page_size + place in
  * the page and d_positions[t] = d_base[r] + its place in the row (d_base NULL
- * = 0; the length of the request's prefix).  num_tokens is the length of the
+ * = 0; the length of the request's prefix; it may be d_held, and counts as it
+ * was before the call).  num_tokens is the length of the
  * last two, at least the number of new tokens; slots and positions behind
  * them are -1.
  * A batch that is not valid is rejected as a whole: the outputs are those of

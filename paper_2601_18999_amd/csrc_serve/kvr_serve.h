@@ -67,6 +67,7 @@ struct TablesArgs {
   int32_t *gain_at, *give_at;  // [rows + 1] pages taken / given back before a row
   int64_t table_stride;
   int32_t rows, width, page_shift, ring_size, num_tokens;
+  int32_t base_held;  // 1: base is held, which is updated in place
 };
 
 // ---- cache store ----

@@ -112,7 +112,7 @@ __device__ __forceinline__ void place_token(const TablesArgs& a, const TablesHdr
       if ((at & mask) == 0) *entry = page;
     }
     slot = (page << a.page_shift) | (at & mask);
-    position = (a.base ? a.base[r] : 0) + at;
+    position = (a.base_held ? held : a.base ? a.base[r] : 0) + at;
   }
   a.slots[t] = slot;
   a.positions[t] = position;

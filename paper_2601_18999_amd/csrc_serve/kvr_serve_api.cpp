@@ -155,7 +155,8 @@ kvr_status kvr_block_tables(const kvr_tables* t, void* d_workspace, size_t bytes
   if (!t->d_held || !t->d_delta || !t->d_table || !t->d_ring || !t->d_state || !t->d_held_out || !t->d_state_out ||
       !t->d_row_start || (t->num_tokens && (!t->d_slots || !t->d_positions)))
     return invalid("a required pointer is NULL");
-  if (t->d_held_out == t->d_delta || t->d_row_start == t->d_held || t->d_row_start == t->d_delta)
+  if (t->d_held_out == t->d_delta || t->d_row_start == t->d_held || t->d_row_start == t->d_delta ||
+      t->d_row_start == t->d_base || (t->d_held_out == t->d_base && t->d_held_out != t->d_held))
     return invalid("an output is an input");
   if (!d_workspace || !aligned(d_workspace, 16)) return invalid("the workspace must be on a 16-byte boundary");
   if (bytes < tables_bytes(t)) return set_error(KVR_ENOMEM, "workspace too small (kvr_block_tables_workspace)");
@@ -181,6 +182,7 @@ kvr_status kvr_block_tables(const kvr_tables* t, void* d_workspace, size_t bytes
   a.page_shift = log2_of(t->page_size);
   a.ring_size = t->ring_size;
   a.num_tokens = t->num_tokens;
+  a.base_held = t->d_base == t->d_held_out;
   const hipError_t e = kvr::launch_tables(a, static_cast<hipStream_t>(hip_stream));
   return e == hipSuccess ? KVR_OK : hip_failed(e, "table kernels launch");
 }

@@ -151,3 +151,21 @@ def test_tables_with_room_for_the_most_tokens(tokens):
         assert x.shape == (tokens,)
         for a in range(new, tokens, 1 << 28):
             assert int((x[a:a + (1 << 28)] != -1).sum()) == 0
+
+
+@pytest.mark.parametrize("rows", [9, 1500])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_positions_from_held_itself(rows, in_place):
+    # base is held: its values before the call, also where the call updates them
+    rng = np.random.default_rng(rows)
+    held = rng.integers(0, 9, rows).astype(np.int32)
+    delta = rng.integers(0, 4, rows).astype(np.int32)
+    table = rng.permutation(rows * 12).astype(np.int32).reshape(rows, 12)
+    ring, state = np.arange(rows * 12, dtype=np.int32), np.array([0, rows * 12, 0])
+    want, bits = R.tables(held, delta, table, ring, state, 1, int(delta.sum()), held)
+    assert not bits
+    on = [torch.from_numpy(x.copy()).to(DEV) for x in (held, delta, table, ring, state)]
+    r = K.block_tables(*on, 1, int(delta.sum()), base=on[0], in_place=in_place)
+    np.testing.assert_array_equal(r.positions.cpu().numpy(), want["positions"])
+    np.testing.assert_array_equal(r.held.cpu().numpy(), want["held"])
+    np.testing.assert_array_equal(r.slots.cpu().numpy(), want["slots"])

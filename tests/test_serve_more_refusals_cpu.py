@@ -1,0 +1,14 @@
+"""Refusals and limits of the serving operators' C ABI and of their functions
+on tensors, on the CPU, beside those of test_serve_abi_cpu.py."""
+import pytest
+
+import paper_2601_18999_amd as K
+from test_serve_abi_cpu import P, _names, _refused, attention, cache, store, tables
+
+
+BAD_BASES = [dict(d_base=3 * P), dict(d_held=5 * P, d_held_out=P)]
+
+
+@pytest.mark.parametrize("bad", BAD_BASES, ids=_names(BAD_BASES))
+def test_a_base_that_the_call_would_overwrite_is_refused(bad):
+    _refused(lambda: K.kvr_block_tables(tables(**bad), P, 1 << 20))
