@@ -418,7 +418,8 @@ kvr_status kvr_cache_store(const kvr_cache* c, const kvr_store* s, void* hip_str
  * tokens each, and the partial results are joined.  The order of the sums
  * depends on the lengths, not on the run: the same call gives the same bits.
  * Lengths that are not valid (negative or decreasing, longer than the
- * table's row, fewer own than new tokens) set KVR_DEV_BAD_LENGTH in d_status
+ * table's row or than 2^31 - 1024 tokens, fewer own than new tokens) set
+ * KVR_DEV_BAD_LENGTH in d_status
  * (optional) and every result is NaN; a page number that is not one of the
  * cache sets KVR_DEV_BAD_PAGE and the rows that see it are NaN. */
 typedef struct kvr_attention {

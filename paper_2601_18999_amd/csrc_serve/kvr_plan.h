@@ -229,12 +229,12 @@ __device__ __forceinline__ int make_plan(const AttendArgs& a, int* lds, bool wri
   // checks
   for (int b = tid; b < a.requests; b += threads) {
     const int t0 = z.start(b), t1 = z.start(b + 1), n = z.length[b];
-    bad |= t0 < 0 || t1 < t0 || t1 > a.tokens || n < t1 - t0 || n > ((int64_t)a.width << a.page_shift);
+    bad |= t0 < 0 || t1 < t0 || t1 > a.tokens || n < t1 - t0 || n > a.own_room;
     if (b == 0) bad |= t0 != 0;
   }
   for (int j = tid; j < a.groups; j += threads) {
     const int b0 = z.group_start[j], b1 = z.group_start[j + 1], p = z.prefix_length[j];
-    bad |= b0 < 0 || b1 < b0 || b1 > a.requests || p < 0 || p > ((int64_t)a.prefix_width << a.page_shift);
+    bad |= b0 < 0 || b1 < b0 || b1 > a.requests || p < 0 || p > a.prefix_room;
     if (j == 0) bad |= b0 != 0;
     if (j == a.groups - 1) bad |= b1 != a.requests;
     z.waves[j] = 0;

@@ -19,6 +19,9 @@ constexpr int kComputeUnits = 256;
 constexpr int kAttendSlots = 2 * kComputeUnits;
 constexpr int kTileRows = 128;  // most query rows of an attention workgroup
 constexpr int kStepKeys = 64;   // keys of one step: what the plan counts in
+// Most keys of a prefix or of a request: the first key of a tile, and of those
+// that are looked up ahead behind the last, fits 31 bits.
+constexpr int kMostKeys = 0x7fffffff - 1023;
 
 // n / d for n < 2^31 by a multiplication, exact (d >= 1, d < 2^31).
 struct Divisor {
@@ -135,7 +138,8 @@ struct AttendArgs {
   Divisor share;
   float scale_log2;
   int32_t tokens, requests, groups, heads, kv_heads, dim;
-  int32_t page_shift, page_mask, num_pages, width, prefix_width;
+  int32_t page_shift, page_mask, num_pages;
+  int32_t own_room, prefix_room;  // most tokens that a row of the tables has room for
   int32_t unit_cap, item_cap, join_cap, split_slots;
   int32_t few_waves;      // waves along the rows that up to 32 rows take (attend_kernel): 1 or 4
   int32_t fused, direct;  // 1: no plan kernel; no join kernel

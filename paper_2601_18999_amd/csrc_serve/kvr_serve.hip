@@ -375,9 +375,8 @@ bool attend_fused(const AttendArgs& a) {
 // shared, nothing can be joined: no join kernel (eight requests of up to 48 own
 // and 64 shared tokens: 16.3 -> 12.9 us a call).
 bool attend_direct(const AttendArgs& a) {
-  const int64_t page = 1ll << a.page_shift;
-  const int64_t own = (a.width * page + kStepKeys - 1) / kStepKeys;
-  const int64_t prefix = a.groups ? (a.prefix_width * page + kStepKeys - 1) / kStepKeys : 0;
+  const int64_t own = (a.own_room + kStepKeys - 1) / kStepKeys;
+  const int64_t prefix = a.groups ? (a.prefix_room + kStepKeys - 1) / kStepKeys : 0;
   const int64_t waves = (int64_t)a.tokens * a.share.d <= 32 ? a.few_waves : 4;
   return prefix < kMinSharedSteps && (own + prefix) * waves <= kMinSplitCost;
 }

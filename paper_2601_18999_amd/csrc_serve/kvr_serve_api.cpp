@@ -76,6 +76,12 @@ kvr_status check_buffers(const kvr_cache* c) {
   return KVR_OK;
 }
 
+// Tokens of a row of a table, at most as many as the kernels count.
+int32_t room(int32_t width, int32_t page_size) {
+  const int64_t n = (int64_t)width * page_size;
+  return (int32_t)(n < kvr::kMostKeys ? n : kvr::kMostKeys);
+}
+
 struct AttendLayout {
   size_t bounds, group_of, waves, units, joins, items, ml, acc, bytes;
   int32_t unit_cap, item_cap, join_cap, split_slots;
@@ -316,8 +322,8 @@ kvr_status kvr_shared_attention(const kvr_cache* c, const kvr_attention* s, void
   a.page_shift = log2_of(c->page_size);
   a.page_mask = c->page_size - 1;
   a.num_pages = c->num_pages;
-  a.width = s->width;
-  a.prefix_width = s->prefix_width;
+  a.own_room = room(s->width, c->page_size);
+  a.prefix_room = room(s->prefix_width, c->page_size);
   a.unit_cap = l.unit_cap;
   a.item_cap = l.item_cap;
   a.join_cap = l.join_cap;

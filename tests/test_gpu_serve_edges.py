@@ -169,3 +169,33 @@ def test_positions_from_held_itself(rows, in_place):
     np.testing.assert_array_equal(r.positions.cpu().numpy(), want["positions"])
     np.testing.assert_array_equal(r.held.cpu().numpy(), want["held"])
     np.testing.assert_array_equal(r.slots.cpu().numpy(), want["slots"])
+
+
+MOST = (1 << 31) - 1024  # tokens of a request or of a prefix
+
+
+@pytest.mark.parametrize("length,prefix", [((1 << 31) - 1, 5), (MOST + 1, 5), (9, MOST + 1), (9, (1 << 31) - 1)])
+def test_lengths_past_the_range_of_keys_are_reported(length, prefix):
+    p = R.Problem([1, 1], [9, 9], [2], [5], page=1024)
+    p.table = p.table[:, :1].repeat(1, 1 << 21)
+    p.prefix_table = p.prefix_table[:, :1].repeat(1, 1 << 21)
+    p.length[1], p.prefix_length[0] = length, prefix
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    out, lse = attend(p, status=status)
+    assert int(status) == 1 and torch.isnan(out).all() and torch.isnan(lse).all()
+
+
+def test_the_most_keys():
+    # one page of 1,024 tokens, named 2^21 - 1 times: the attention over that page, and its sum as often
+    p = R.Problem([1], [1024], heads=2, kv_heads=1, dim=64, page=1024)
+    ref, size, ref_lse = p.expect()
+    p.table = p.table[:, :1].repeat(1, (1 << 21) - 1)
+    p.length[0] = MOST
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    out, lse = attend(p, status=status)
+    assert int(status) == 0
+    # 512 workgroups at most, of four waves, two lanes to a row: 2^31 / 2^12 = 2^19 terms that a lane adds one by one
+    # in 32 bits, each rounding at most 2^-24 of the sum; in l and in o
+    err = (out.double().cpu() - ref).abs()
+    assert (err <= 2 * 2.0 ** -5 * size + 2.0 ** -8 * (ref.abs() + size)).all(), float(err.max())
+    assert ((lse.double().cpu() - ref_lse - np.log(2.0 ** 21 - 1)).abs() <= 2.0 ** -5 + 1e-3).all()
