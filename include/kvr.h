@@ -421,7 +421,10 @@ kvr_status kvr_cache_store(const kvr_cache* c, const kvr_store* s, void* hip_str
  * table's row or than 2^31 - 1024 tokens, fewer own than new tokens) set
  * KVR_DEV_BAD_LENGTH in d_status
  * (optional) and every result is NaN; a page number that is not one of the
- * cache sets KVR_DEV_BAD_PAGE and the rows that see it are NaN. */
+ * cache sets KVR_DEV_BAD_PAGE and the rows that see it are NaN.
+ * One launch holds fewer than 2^24 workgroups: tiles of 128 rows (a row is a
+ * query head of a token) and requests' and groups' last tiles, for each of
+ * kv_heads; more are refused. */
 typedef struct kvr_attention {
   uint32_t struct_size;
   int32_t dtype;        /* of d_q and d_out: KVR_BF16 or KVR_FP16; the cache's

@@ -884,7 +884,7 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
         }
     }
     __syncthreads();
-    for (int i = tid; i < it.rows * (D / 4); i += 256) {
+    for (int i = tid; i < it.rows * (D / 4); i += kAttendThreads) {
       const int rr = i / (D / 4), c = i % (D / 4);
       float mm = -INFINITY, ll = 0.0f;
 #pragma unroll
@@ -908,7 +908,7 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
 // library product reaches 1,264).  Few rows: bound by memory (64 requests in
 // four groups, 243 MB: 50 us, 4.9 TB/s, where a copy reaches 5.1).
 template <int D, class T, bool FP8>
-__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(AttendArgs a) {
+__global__ void __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) attend_kernel(AttendArgs a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const int item = blockIdx.x / a.kv_heads, head = blockIdx.x % a.kv_heads;
   Item it;
@@ -959,7 +959,7 @@ hipError_t launch_attend_as(const AttendArgs& a, hipStream_t st) {
     if (e != hipSuccess) return e;
     allowed.fetch_or(bit, std::memory_order_relaxed);
   }
-  attend_kernel<D, T, FP8><<<dim3((uint32_t)a.item_cap * (uint32_t)a.kv_heads), dim3(256), lds, st>>>(a);
+  attend_kernel<D, T, FP8><<<dim3((uint32_t)a.item_cap * (uint32_t)a.kv_heads), dim3(kAttendThreads), lds, st>>>(a);
   return hipGetLastError();
 }
 

@@ -17,6 +17,7 @@ namespace kvr {
 // a unit 15 calls of all kinds were 2 and 5% slower).
 constexpr int kComputeUnits = 256;
 constexpr int kAttendSlots = 2 * kComputeUnits;
+constexpr int kAttendThreads = 256;
 constexpr int kTileRows = 128;  // most query rows of an attention workgroup
 constexpr int kStepKeys = 64;   // keys of one step: what the plan counts in
 // Most keys of a prefix or of a request: the first key of a tile, and of those

@@ -116,7 +116,10 @@ kvr_status lay_out(const kvr_cache* c, const kvr_attention* a, AttendLayout* l) 
   const int64_t units = parts * (rows / kvr::kTileRows) + a->num_requests + a->num_groups;
   l->split_slots = kvr::kAttendSlots / c->kv_heads > 0 ? kvr::kAttendSlots / c->kv_heads : 1;
   const int64_t items = units + l->split_slots;
-  if (items * c->kv_heads > kInt) return invalid("too many heads and requests for one launch");
+  // (a launch has fewer than 2^32 threads)
+  if (items * c->kv_heads >= (1ll << 32) / kvr::kAttendThreads)
+    return invalid("too many heads and requests for one launch: (num_tokens * heads / kv_heads / 128 * (2 with groups) + "
+                   "num_requests + num_groups + 512 / kv_heads) * kv_heads must be below 2^24");
   const int64_t partial = parts * rows + (int64_t)l->split_slots * kvr::kTileRows;
   l->unit_cap = (int32_t)units;
   l->item_cap = (int32_t)items;

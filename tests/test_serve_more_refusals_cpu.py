@@ -12,3 +12,13 @@ BAD_BASES = [dict(d_base=3 * P), dict(d_held=5 * P, d_held_out=P)]
 @pytest.mark.parametrize("bad", BAD_BASES, ids=_names(BAD_BASES))
 def test_a_base_that_the_call_would_overwrite_is_refused(bad):
     _refused(lambda: K.kvr_block_tables(tables(**bad), P, 1 << 20))
+
+
+def test_more_workgroups_than_a_launch_holds_are_refused():
+    # a workgroup has 256 threads, a launch fewer than 2^32
+    most = 1 << 20
+    K.kvr_attention_workspace(cache(kv_heads=15), attention(num_tokens=most, num_requests=most, num_groups=0, heads=15))
+    for kv, heads in ((16, 16), (16, 64), (1024, 1024)):
+        big = (cache(kv_heads=kv), attention(num_tokens=most, num_requests=most, num_groups=0, heads=heads))
+        _refused(lambda: K.kvr_attention_workspace(*big))
+        _refused(lambda: K.kvr_shared_attention(*big, P, 1 << 60))
