@@ -312,7 +312,8 @@ void kvr_destroy(kvr_ctx* ctx);
  * may be captured into a graph.  Every struct begins with struct_size =
  * sizeof(the struct).  Strides count elements; the elements of a head are
  * neighbours, every head of every token starts on a 16-byte boundary, and a
- * page or token of the cache is below 2^31 bytes from the next.
+ * page or token of the cache is below 2^31 bytes from the next.  Where there
+ * is one page, token or head only, its stride has no meaning.
  * What only the device can see (lengths, page numbers) is checked there, as
  * stated at each operator, and or-ed into a status word (KVR_DEV_*).
  * ------------------------------------------------------------------------ */

@@ -61,18 +61,32 @@ kvr_status check(const kvr_cache* c) {
   return KVR_OK;
 }
 
-// 16-byte alignment of every head, for elements of `size` bytes.
-bool on_chunks(int64_t a, int64_t b, int64_t c, int size) { return ((a | b | c) * size & 15) == 0; }
+// A stride in bytes; where there is one of a kind there is no next one, and
+// whatever the caller's stride is has no meaning.
+int64_t step(int64_t stride, int64_t n, int size) { return n > 1 ? stride * size : 0; }
 
-kvr_status check_buffers(const kvr_cache* c) {
+bool on_chunks(int64_t a, int64_t b, int64_t c = 0) { return ((a | b | c) & 15) == 0; }
+
+// The strides of a cache in bytes.
+struct CacheSteps {
+  int64_t page, slot, head;
+};
+
+CacheSteps steps(const kvr_cache* c, int64_t page, int64_t slot, int64_t head) {
   const int size = c->dtype == KVR_FP8 ? 1 : 2;
+  return {step(page, c->num_pages, size), step(slot, c->page_size, size), step(head, c->kv_heads, size)};
+}
+
+kvr_status check_buffers(const kvr_cache* c, CacheSteps* k, CacheSteps* v) {
   if (!c->d_k || !c->d_v) return invalid("d_k and d_v are required");
-  if (!aligned(c->d_k, 16) || !aligned(c->d_v, 16) || !on_chunks(c->k_page, c->k_slot, c->k_head, size) ||
-      !on_chunks(c->v_page, c->v_slot, c->v_head, size))
+  *k = steps(c, c->k_page, c->k_slot, c->k_head);
+  *v = steps(c, c->v_page, c->v_slot, c->v_head);
+  if (!aligned(c->d_k, 16) || !aligned(c->d_v, 16) || !on_chunks(k->page, k->slot, k->head) ||
+      !on_chunks(v->page, v->slot, v->head))
     return invalid("every head of the cache must start on a 16-byte boundary");
   // the kernels multiply by these in 32 bits
-  for (const int64_t stride : {c->k_page, c->k_slot, c->v_page, c->v_slot})
-    if (stride < 0 || stride * size > kInt) return invalid("strides of pages and slots must be in 0..2^31 - 1 bytes");
+  for (const int64_t stride : {k->page, k->slot, v->page, v->slot})
+    if (stride < 0 || stride > kInt) return invalid("strides of pages and slots must be in 0..2^31 - 1 bytes");
   return KVR_OK;
 }
 
@@ -207,14 +221,17 @@ kvr_status kvr_cache_store(const kvr_cache* c, const kvr_store* s, void* hip_str
   if (s->num_tokens < 0 || s->num_tokens * chunks > kInt - 256)
     return invalid("num_tokens must be >= 0, num_tokens * kv_heads * dim / 8 below 2^31");
   if (s->num_tokens == 0) return KVR_OK;
-  st = check_buffers(c);
+  CacheSteps kc, vc;
+  st = check_buffers(c, &kc, &vc);
   if (st != KVR_OK) return st;
   if (!s->d_k || !s->d_v || !s->d_slots) return invalid("d_k, d_v and d_slots are required");
-  if (!aligned(s->d_k, 16) || !aligned(s->d_v, 16) || !on_chunks(s->k_token, s->k_head, 0, 2) ||
-      !on_chunks(s->v_token, s->v_head, 0, 2))
-    return invalid("every head of the keys and values must start on a 16-byte boundary");
-  const int size = c->dtype == KVR_FP8 ? 1 : 2;
   kvr::StoreArgs a;
+  a.k_tok = step(s->k_token, s->num_tokens, 2);
+  a.k_head = step(s->k_head, c->kv_heads, 2);
+  a.v_tok = step(s->v_token, s->num_tokens, 2);
+  a.v_head = step(s->v_head, c->kv_heads, 2);
+  if (!aligned(s->d_k, 16) || !aligned(s->d_v, 16) || !on_chunks(a.k_tok, a.k_head) || !on_chunks(a.v_tok, a.v_head))
+    return invalid("every head of the keys and values must start on a 16-byte boundary");
   a.k = static_cast<const char*>(s->d_k);
   a.v = static_cast<const char*>(s->d_v);
   a.kc = static_cast<char*>(c->d_k);
@@ -223,16 +240,12 @@ kvr_status kvr_cache_store(const kvr_cache* c, const kvr_store* s, void* hip_str
   a.vs = c->d_v_scale;
   a.slots = s->d_slots;
   a.status = s->d_status;
-  a.k_tok = s->k_token * 2;
-  a.k_head = s->k_head * 2;
-  a.v_tok = s->v_token * 2;
-  a.v_head = s->v_head * 2;
-  a.kc_page = c->k_page * size;
-  a.kc_slot = c->k_slot * size;
-  a.kc_head = c->k_head * size;
-  a.vc_page = c->v_page * size;
-  a.vc_slot = c->v_slot * size;
-  a.vc_head = c->v_head * size;
+  a.kc_page = kc.page;
+  a.kc_slot = kc.slot;
+  a.kc_head = kc.head;
+  a.vc_page = vc.page;
+  a.vc_slot = vc.slot;
+  a.vc_head = vc.head;
   a.chunks = kvr::make_divisor((uint32_t)chunks);
   a.tokens = s->num_tokens;
   a.dim_shift = log2_of(c->dim);
@@ -263,7 +276,8 @@ kvr_status kvr_shared_attention(const kvr_cache* c, const kvr_attention* s, void
   st = lay_out(c, s, &l);
   if (st != KVR_OK) return st;
   if (s->num_tokens == 0) return KVR_OK;
-  st = check_buffers(c);
+  CacheSteps kc, vc;
+  st = check_buffers(c, &kc, &vc);
   if (st != KVR_OK) return st;
   if (!s->d_q || !s->d_out || !s->d_length || (s->width && !s->d_table))
     return invalid("d_q, d_out, d_table and d_length are required");
@@ -271,14 +285,16 @@ kvr_status kvr_shared_attention(const kvr_cache* c, const kvr_attention* s, void
     return invalid("groups need d_group_start, d_prefix_table and d_prefix_length");
   if (s->table_stride < s->width || s->prefix_stride < s->prefix_width)
     return invalid("a table's stride must be at least its width");
-  if (!aligned(s->d_q, 16) || !aligned(s->d_out, 8) || !on_chunks(s->q_token, s->q_head, 0, 2) ||
-      ((s->out_token | s->out_head) & 3))
+  kvr::AttendArgs a;
+  a.q_tok = step(s->q_token, s->num_tokens, 2);
+  a.q_head = step(s->q_head, s->heads, 2);
+  a.o_tok = step(s->out_token, s->num_tokens, 2);
+  a.o_head = step(s->out_head, s->heads, 2);
+  if (!aligned(s->d_q, 16) || !aligned(s->d_out, 8) || !on_chunks(a.q_tok, a.q_head) || ((a.o_tok | a.o_head) & 7))
     return invalid("every head of the queries must start on a 16-byte boundary, of the results on an 8-byte one");
   if (!d_workspace || !aligned(d_workspace, 256)) return invalid("the workspace must be on a 256-byte boundary");
   if (bytes < l.bytes) return set_error(KVR_ENOMEM, "workspace too small (kvr_attention_workspace)");
-  const int size = c->dtype == KVR_FP8 ? 1 : 2;
   char* ws = static_cast<char*>(d_workspace);
-  kvr::AttendArgs a;
   a.q = static_cast<const char*>(s->d_q);
   a.out = static_cast<char*>(s->d_out);
   a.lse = s->d_lse;
@@ -286,16 +302,12 @@ kvr_status kvr_shared_attention(const kvr_cache* c, const kvr_attention* s, void
   a.vc = static_cast<const char*>(c->d_v);
   a.ks = c->d_k_scale;
   a.vs = c->d_v_scale;
-  a.q_tok = s->q_token * 2;
-  a.q_head = s->q_head * 2;
-  a.o_tok = s->out_token * 2;
-  a.o_head = s->out_head * 2;
-  a.kc_page = (uint32_t)(c->k_page * size);
-  a.kc_slot = (uint32_t)(c->k_slot * size);
-  a.kc_head = c->k_head * size;
-  a.vc_page = (uint32_t)(c->v_page * size);
-  a.vc_slot = (uint32_t)(c->v_slot * size);
-  a.vc_head = c->v_head * size;
+  a.kc_page = (uint32_t)kc.page;
+  a.kc_slot = (uint32_t)kc.slot;
+  a.kc_head = kc.head;
+  a.vc_page = (uint32_t)vc.page;
+  a.vc_slot = (uint32_t)vc.slot;
+  a.vc_head = vc.head;
   a.row_start = s->d_row_start;
   a.length = s->d_length;
   a.table = s->d_table;

@@ -199,3 +199,34 @@ def test_the_most_keys():
     err = (out.double().cpu() - ref).abs()
     assert (err <= 2 * 2.0 ** -5 * size + 2.0 ** -8 * (ref.abs() + size)).all(), float(err.max())
     assert ((lse.double().cpu() - ref_lse - np.log(2.0 ** 21 - 1)).abs() <= 2.0 ** -5 + 1e-3).all()
+
+
+def odd_where_one(x):
+    """The tensor with a stride of 1 in each dimension of one (but the last): a stride that no element follows."""
+    return torch.as_strided(x, x.shape, [1 if n == 1 else s for n, s in zip(x.shape[:-1], x.stride())] + [1])
+
+
+@pytest.mark.parametrize("cache", [None, FP8], ids=["16-bit", "8-bit"])
+@pytest.mark.parametrize("tokens,pages,page,heads", [(1, 20, 16, 4), (9, 1, 1024, 4), (1, 40, 1, 1), (1, 1, 64, 1),
+                                                     (7, 40, 1, 2), (5, 30, 16, 1)])
+def test_strides_that_nothing_follows(tokens, pages, page, heads, cache):
+    # one token, one page, pages of one token, one head: any stride does, in the store and in the attention
+    g = torch.Generator().manual_seed(tokens)
+    k, v, q = (torch.randn((tokens, heads, 64), generator=g).to(BF16).to(DEV) for _ in range(3))
+    caches = [torch.randn((pages, page, heads, 64), generator=g).to(cache or BF16).to(DEV) for _ in range(2)]
+    slots = torch.randperm(pages * page, generator=g)[:tokens].int().to(DEV)
+    table = torch.arange(pages, dtype=torch.int32, device=DEV)[None]
+    length = torch.tensor([min(pages * page, 30)], dtype=torch.int32, device=DEV)
+    start = torch.tensor([0, tokens], dtype=torch.int32, device=DEV)
+
+    def both(f):
+        copies = [f(c.view(torch.uint8).clone().view(c.dtype)) for c in caches]
+        K.cache_store(f(k), f(v), *copies, slots)
+        out = torch.full_like(q, 7.0)
+        K.shared_attention(f(q), *copies, start, table, length, out=f(out))
+        return out, [c.view(torch.uint8).cpu() for c in copies]
+
+    want, stored = both(lambda x: x)
+    got, odd = both(odd_where_one)
+    assert torch.equal(got, want) and all(torch.equal(a, b) for a, b in zip(odd, stored))
+    assert torch.isfinite(want).all()
