@@ -5,7 +5,9 @@ shared-prefix attention (``kvr_block_tables``, ``kvr_cache_store`` and
 The functions check what the C side cannot see (types, shapes, devices),
 marshal the arguments and launch on torch's current stream of the tensors'
 device.  They neither synchronise nor copy to the host; workspaces and outputs
-come from torch's allocator.  Errors raise ``KvrError``.
+come from torch's allocator.  Errors raise ``KvrError``.  They have no
+gradients: a call whose result would need one is refused (call under
+``torch.no_grad`` or ``torch.inference_mode``).
 """
 from __future__ import annotations
 
@@ -69,12 +71,14 @@ def _gpu(where: str, name: str, t) -> torch.device:
     return t.device
 
 
-def _stream(device: torch.device) -> int:
-    return torch._C._cuda_getCurrentRawStream(device.index)
+def _no_gradient(where: str) -> None:
+    """Called where an argument requires one."""
+    if torch.is_grad_enabled():
+        _refuse(where, "there is no gradient: call under torch.no_grad(), or with detached tensors")
 
 
-def _here(device: torch.device) -> bool:
-    return device.index == torch._C._cuda_getDevice()
+# of a device's index; of the current device
+_stream, _current = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
 @functools.lru_cache(maxsize=4096)
@@ -108,7 +112,7 @@ def block_tables(held: torch.Tensor, delta: torch.Tensor, table: torch.Tensor, r
     """
     where = "block_tables"
     device = _gpu(where, "held", held)
-    if not _here(device):
+    if device.index != _current():
         with torch.cuda.device(device):
             return block_tables(held, delta, table, ring, state, page_size, num_tokens, base=base, in_place=in_place)
     rows = held.shape[0] if held.dim() == 1 else -1
@@ -137,7 +141,7 @@ def block_tables(held: torch.Tensor, delta: torch.Tensor, table: torch.Tensor, r
                            p_delta, p_base, p_table, p_ring, p_state, p_held if in_place else at,
                            state_out.data_ptr(), at + 4 * rows, at + 4 * (2 * rows + 1),
                            at + 4 * (2 * rows + 1 + num_tokens)),
-        at + 4 * work, nbytes, _stream(device))
+        at + 4 * work, nbytes, _stream(device.index))
     return BlockTables(held_out, state_out, row_start, slots, positions)
 
 
@@ -163,6 +167,8 @@ def _cache_args(where: str, kc: torch.Tensor, vc: torch.Tensor, ks, vs, device):
         _refuse(where, "the elements of a head must be contiguous")
     p_ks = 0 if ks is None else _vector(where, "k_scale", ks, torch.float32, heads, device)
     p_vs = 0 if vs is None else _vector(where, "v_scale", vs, torch.float32, heads, device)
+    if (p_ks and ks.requires_grad) or (p_vs and vs.requires_grad):
+        _no_gradient(where)
     return CACHE_RECORD.pack(CACHE_RECORD.size, code, pages, page, heads, dim, kc.data_ptr(), vc.data_ptr(), a0, a1, a2,
                              b0, b1, b2, p_ks, p_vs)
 
@@ -181,9 +187,11 @@ def cache_store(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache
     float8_e4m3fn cache holds x / scale[head]."""
     where = "cache_store"
     device = _gpu(where, "k", k)
-    if not _here(device):
+    if device.index != _current():
         with torch.cuda.device(device):
             return cache_store(k, v, k_cache, v_cache, slots, k_scale=k_scale, v_scale=v_scale, status=status)
+    if k.requires_grad or v.requires_grad or k_cache.requires_grad or v_cache.requires_grad:
+        _no_gradient(where)
     cache = _cache_args(where, k_cache, v_cache, k_scale, v_scale, device)
     shape = k.shape
     if k.dtype is not v.dtype or v.device != device or len(shape) != 3 or shape != v.shape or \
@@ -196,7 +204,7 @@ def cache_store(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache
     p_slots = _vector(where, "slots", slots, torch.int32, shape[0], device)
     kvr_cache_store(cache, STORE_RECORD.pack(STORE_RECORD.size, DTYPE_CODES.get(k.dtype, -1), shape[0], 0, k.data_ptr(),
                                              v.data_ptr(), a0, a1, b0, b1, p_slots, _status(where, status, device)),
-                    _stream(device))
+                    _stream(device.index))
 
 
 def shared_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
@@ -217,15 +225,17 @@ def shared_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     pages and length of what they share (None: nothing is shared).  ``scale``
     is dim ** -0.5 by default.  Returns ``out`` (like ``q`` unless given);
     ``lse`` [tokens, heads] float32 receives the logarithms of the softmax
-    sums, ``status`` [1] int32 the KVR_DEV_* bits.
+    sums, ``status`` [1] int32 the KVR_DEV_* bits.  There is no gradient.
     """
     where = "shared_attention"
     device = _gpu(where, "q", q)
-    if not _here(device):
+    if device.index != _current():
         with torch.cuda.device(device):
             return shared_attention(q, k_cache, v_cache, row_start, table, length, group_start, prefix_table,
                                     prefix_length, scale=scale, k_scale=k_scale, v_scale=v_scale, out=out, lse=lse,
                                     status=status)
+    if q.requires_grad or k_cache.requires_grad or v_cache.requires_grad:
+        _no_gradient(where)
     cache = _cache_args(where, k_cache, v_cache, k_scale, v_scale, device)
     _, _, kv_heads, dim = k_cache.shape
     if q.dim() != 3 or q.shape[2] != dim:
@@ -248,6 +258,8 @@ def shared_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
     elif out.shape != q.shape or out.dtype != q.dtype or out.device != device:
         _refuse(where, "out must be like q")
+    elif out.requires_grad:
+        _no_gradient(where)
     q0, q1, q2 = q.stride()
     o0, o1, o2 = out.stride()
     if q2 != 1 or o2 != 1:
@@ -265,7 +277,7 @@ def shared_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
                                  _status(where, status, device))
     nbytes = _attention_bytes(DTYPE_CODES[k_cache.dtype], kv_heads, dim, code, tokens, requests, groups, heads)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    kvr_shared_attention(cache, args, ws.data_ptr(), nbytes, _stream(device))
+    kvr_shared_attention(cache, args, ws.data_ptr(), nbytes, _stream(device.index))
     return out
 
 

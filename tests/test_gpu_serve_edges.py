@@ -230,3 +230,40 @@ def test_strides_that_nothing_follows(tokens, pages, page, heads, cache):
     got, odd = both(odd_where_one)
     assert torch.equal(got, want) and all(torch.equal(a, b) for a, b in zip(odd, stored))
     assert torch.isfinite(want).all()
+
+
+def test_a_call_that_would_need_a_gradient_is_refused():
+    p = R.Problem([1, 3], [20, 30], heads=2, kv_heads=2, dim=64, cache=FP8)
+    args, kw = p.args(), p.kwargs()
+    want = K.shared_attention(*args, **kw)
+    k = torch.randn((4, 2, 64), device=DEV).to(BF16)
+    slots = torch.arange(4, dtype=torch.int32, device=DEV)
+    scales = {n: kw[n] for n in ("k_scale", "v_scale")}
+
+    def attention(name, x):
+        return K.shared_attention(*([x] + args[1:] if name == "q" else args), **dict(kw, **{name: x} if name != "q" else {}))
+
+    def store(name, x):
+        kv = {"k": k, "v": k}
+        if name in kv:
+            kv[name] = x
+        K.cache_store(kv["k"], kv["v"], args[1], args[2], slots, **dict(scales, **{name: x} if name in scales else {}))
+
+    for call, name, x in ((attention, "q", args[0]), (attention, "v_scale", kw["v_scale"]),
+                          (attention, "out", torch.empty_like(args[0])), (store, "k", k), (store, "v", k),
+                          (store, "k_scale", kw["k_scale"])):
+        x = x.clone().requires_grad_()
+        before = [c.view(torch.uint8).clone() for c in args[1:3]]
+        with pytest.raises(K.KvrError, match="no gradient") as ei:
+            call(name, x)
+        assert ei.value.status == K.KVR_EINVAL
+        assert all(torch.equal(c.view(torch.uint8), b) for c, b in zip(args[1:3], before))
+        for off in (torch.no_grad(), torch.inference_mode()):
+            with off:
+                call(name, x.detach() if name == "out" else x)
+        call(name, x.detach())
+    q = args[0].clone().requires_grad_()
+    with torch.no_grad():
+        K.cache_store(k, k, args[1], args[2], torch.full_like(slots, -1), **scales)
+        assert torch.equal(K.shared_attention(q, *args[1:], **kw), K.shared_attention(*args, **kw))
+    assert not want.requires_grad
