@@ -80,12 +80,12 @@ constexpr int plan_words(int cap) { return 48 + (cap ? 8 * (cap + 1) : 0); }
 
 // Waves along the rows that `rows` rows take in tiles of kTileRows; `few`: that
 // up to 32 rows take.
-__device__ __forceinline__ int row_waves(int rows, int few) {
+__host__ __device__ __forceinline__ int row_waves(int rows, int few) {
   const int rest = rows % kTileRows;
   return rows / kTileRows * 4 + (rest == 0 ? 0 : rest <= 32 ? few : 4);
 }
 
-__device__ __forceinline__ int steps_of(int keys) { return (keys + kStepKeys - 1) / kStepKeys; }
+__host__ __device__ __forceinline__ int steps_of(int keys) { return (keys + kStepKeys - 1) / kStepKeys; }
 
 // Whether a group takes its prefix for all of its requests at once, in tiles of
 // `together` waves along the rows instead of `apart`, at the price of partial
@@ -94,9 +94,29 @@ __device__ __forceinline__ int steps_of(int keys) { return (keys + kStepKeys - 1
 // from about 200 keys on if the group is large enough (64 requests, 8 key
 // heads: 256 keys 34.3 apart, 33.6 together, 2,048 keys 67.9 and 40.5; 16
 // requests: 512 keys 19.0 and 19.8, 1,024 keys 21.1 and 20.9).
-__device__ __forceinline__ bool worth_sharing(int apart, int together, int steps, int kv_heads) {
+__host__ __device__ __forceinline__ bool worth_sharing(int apart, int together, int steps, int kv_heads) {
   return (int64_t)together * 4 <= (int64_t)apart * 3 && steps >= kMinSharedSteps &&
          (int64_t)(apart - together) * steps * kv_heads >= 256;
+}
+
+// Most cost of an item, where all units cost `total`: the slots' fair share.
+__host__ __device__ __forceinline__ int chunk_of(int64_t total, int slots, int few) {
+  const int64_t fair = (total + slots - 1) / slots;
+  const int least = kMinSplitCost * few;
+  return (int)(fair < least ? least : fair > 0x7fffffff ? 0x7fffffff : fair);
+}
+
+// Items of a unit, and the steps of each.
+struct Cut {
+  int splits, per;
+};
+
+__host__ __device__ __forceinline__ Cut cut_of(int steps, int cost, int chunk) {
+  Cut c;
+  c.splits = max(1, (cost + chunk - 1) / chunk);
+  c.per = max(1, (steps + c.splits - 1) / c.splits);
+  c.splits = max(1, (steps + c.per - 1) / c.per);
+  return c;
 }
 
 // Lengths that are not valid: nothing was computed, every result is NaN.
@@ -286,9 +306,7 @@ __device__ __forceinline__ int make_plan(const AttendArgs& a, int* lds, bool wri
     total += w.cost;
   }
   group_before(total, total, part64);
-  const int64_t fair = (total + a.split_slots - 1) / a.split_slots;
-  const int least = kMinSplitCost * a.few_waves;
-  const int chunk = (int)(fair < least ? least : fair > 0x7fffffff ? 0x7fffffff : fair);
+  const int chunk = chunk_of(total, a.split_slots, a.few_waves);
   int items = 0, rows_acc = 0, joins = 0;
   for (int u0 = 0; u0 < units; u0 += threads) {
     const int u = u0 + tid;
@@ -298,9 +316,9 @@ __device__ __forceinline__ int make_plan(const AttendArgs& a, int* lds, bool wri
         s = last_at_most(z.bounds, segments, u);
         w = unit_work(a, z, s, u);
       }
-      splits = max(1, (w.cost + chunk - 1) / chunk);
-      per = max(1, (w.steps + splits - 1) / splits);
-      splits = max(1, (w.steps + per - 1) / per);
+      const Cut c = cut_of(w.steps, w.cost, chunk);
+      splits = c.splits;
+      per = c.per;
       partial = s < a.groups || w.group >= 0 || splits > 1 ? splits * w.it.rows : 0;
     }
     int all_items, all_rows;

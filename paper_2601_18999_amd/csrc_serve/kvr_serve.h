@@ -52,6 +52,23 @@ constexpr bool lanes_reach(int dim, int64_t stride) {
   return (512 / dim - 1) * stride + 2 * dim <= (int64_t)1 << 32;
 }
 
+// Most partial rows of the attention's plan: a unit of up to kTileRows rows that
+// is split, or whose rows have a shared prefix, has as many as it has rows, for
+// each of its items.
+//  * A unit is split where it costs more than a slot's share of the total, and
+//    into fewer than twice as many items as shares it costs: all such units have
+//    fewer than 2 * slots items.
+//  * A prefix is shared where that leaves at most 3/4 of the requests' own row
+//    waves.  R rows of n requests take at least R / 32 waves together and less
+//    than R / 32 + 4 n apart, so R < 384 n.  They count twice, with the prefix
+//    and with the own tokens.
+// (Never more than all rows, twice with groups, and a tile for each added item.)
+constexpr int64_t most_partial_rows(int64_t rows, int64_t requests, bool groups, int64_t slots) {
+  const int64_t shared = !groups ? 0 : rows < 384 * requests ? 2 * rows : 2 * 384 * requests;
+  const int64_t some = shared + 2 * slots * kTileRows, all = (groups ? 2 : 1) * rows + slots * kTileRows;
+  return some < all ? some : all;
+}
+
 // ---- page tables ----
 struct TablesHdr {
   int64_t head, tail;  // the ring before the call

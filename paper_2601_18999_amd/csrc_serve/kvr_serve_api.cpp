@@ -120,10 +120,9 @@ kvr_status check(const kvr_cache* c, const kvr_attention* a) {
   return KVR_OK;
 }
 
-// Most units, items and partial rows that the plan can make: a request's and
-// a group's rows end in one tile that is not full each, the items of a unit
-// that is split add at most split_slots, and the partial rows are at most all
-// rows twice (own tokens and prefix) and a tile for each added item.
+// Most units and items that the plan can make: a request's and a group's rows
+// end in one tile that is not full each, and the items of the units that are
+// split add at most split_slots.
 kvr_status lay_out(const kvr_cache* c, const kvr_attention* a, AttendLayout* l) {
   const int64_t rows = (int64_t)a->num_tokens * (a->heads / c->kv_heads);
   const int64_t parts = a->num_groups ? 2 : 1;
@@ -134,7 +133,7 @@ kvr_status lay_out(const kvr_cache* c, const kvr_attention* a, AttendLayout* l) 
   if (items * c->kv_heads >= (1ll << 32) / kvr::kAttendThreads)
     return invalid("too many heads and requests for one launch: (num_tokens * heads / kv_heads / 128 * (2 with groups) + "
                    "num_requests + num_groups + 512 / kv_heads) * kv_heads must be below 2^24");
-  const int64_t partial = parts * rows + (int64_t)l->split_slots * kvr::kTileRows;
+  const int64_t partial = kvr::most_partial_rows(rows, a->num_requests, a->num_groups > 0, l->split_slots);
   l->unit_cap = (int32_t)units;
   l->item_cap = (int32_t)items;
   size_t at = 256;

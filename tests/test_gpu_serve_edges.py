@@ -267,3 +267,30 @@ def test_a_call_that_would_need_a_gradient_is_refused():
         K.cache_store(k, k, args[1], args[2], torch.full_like(slots, -1), **scales)
         assert torch.equal(K.shared_attention(q, *args[1:], **kw), K.shared_attention(*args, **kw))
     assert not want.requires_grad
+
+
+@pytest.mark.parametrize("new,own,sizes,prefix,heads,kv", [
+    ([257] * 9, [300] * 9, [9], [3000], 1, 1),          # the most rows a request that share a prefix
+    ([129] * 40, [129 + i for i in range(40)], [30, 10], [2000, 900], 1, 1),
+    ([33] * 64, [40] * 64, [64], [5000], 2, 2),
+    ([1] * 300, [1 + 61 * i % 900 for i in range(300)], [200, 100], [700, 40], 8, 1),
+    ([1], [30000], (), (), 64, 1),                      # split into as many items as there are slots
+    ([1] * 3 + [700], [9000, 50, 20000, 700], (), (), 4, 4),
+    ([2000], [2000], (), (), 16, 1),
+], ids=["257", "129", "33", "ones", "split", "mixed", "prompt"])
+@pytest.mark.parametrize("dim,cache", [(64, None), (256, None), (256, FP8)], ids=["64", "256", "256-8-bit"])
+def test_nothing_is_written_behind_the_workspace(new, own, sizes, prefix, heads, kv, dim, cache, monkeypatch):
+    from paper_2601_18999_amd import serve
+    p = R.Problem(new, own, sizes, prefix, heads=heads, kv_heads=kv, dim=dim, cache=cache)
+    call, buffers = serve.kvr_shared_attention, []
+
+    def guarded(cache, args, ws, nbytes, stream):
+        whole = torch.full((nbytes + (64 << 20),), 0xA5, dtype=torch.uint8, device=DEV)
+        buffers.append((whole, nbytes))
+        call(cache, args, whole.data_ptr(), nbytes, stream)
+
+    monkeypatch.setattr(serve, "kvr_shared_attention", guarded)
+    out, lse = attend(p)
+    (whole, nbytes), = buffers
+    assert bool((whole[nbytes:] == 0xA5).all())
+    R.check(out, lse, p, on_device(p))

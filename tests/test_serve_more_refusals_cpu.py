@@ -22,3 +22,12 @@ def test_more_workgroups_than_a_launch_holds_are_refused():
         big = (cache(kv_heads=kv), attention(num_tokens=most, num_requests=most, num_groups=0, heads=heads))
         _refused(lambda: K.kvr_attention_workspace(*big))
         _refused(lambda: K.kvr_shared_attention(*big, P, 1 << 60))
+
+
+@pytest.mark.parametrize("groups", [0, 1])
+def test_the_workspace_of_one_long_prompt_does_not_grow_with_it(groups):
+    # its rows have partial results only in as many items as the device holds at once
+    def size(tokens):
+        return K.kvr_attention_workspace(cache(kv_heads=8), attention(num_tokens=tokens, num_requests=1,
+                                                                      num_groups=groups, heads=32))
+    assert size(9216) < 80 << 20 and size(131072) < size(9216) + (8 << 20)

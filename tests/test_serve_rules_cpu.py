@@ -43,3 +43,77 @@ int main() {
     assert all(reach == same for reach, same in got), got
     fits = [s <= last for s in strides]
     assert [bool(r) for r, _ in got] == fits
+
+
+def test_partial_rows_fit_their_room(tmp_path):
+    # the plan's own rules over random requests and groups, those of the largest shared and split units among them
+    out = compiled(tmp_path, """
+#include <cstdio>
+#include <random>
+#include <vector>
+#include "kvr_plan.h"
+using namespace kvr;
+
+struct Request { int rows, own, group; };
+
+// partial rows of a plan, counted unit by unit
+static int64_t partial_rows(const std::vector<Request>& reqs, const std::vector<int>& prefix, int slots, int few, int kv) {
+  const int groups = (int)prefix.size();
+  std::vector<int> apart(groups), rows(groups), shared(groups);
+  for (const Request& r : reqs)
+    if (groups) apart[r.group] += row_waves(r.rows, few), rows[r.group] += r.rows;
+  for (int j = 0; j < groups; ++j)
+    shared[j] = worth_sharing(apart[j], row_waves(rows[j], few), steps_of(prefix[j]), kv);
+  struct U { int rows, steps, cost; bool partial; };
+  std::vector<U> units;
+  auto tiles = [&](int n, int steps, bool partial) {
+    for (int at = 0; at < n; at += kTileRows) {
+      const int r = n - at < kTileRows ? n - at : kTileRows;
+      units.push_back({r, steps, steps * row_waves(r, few), partial});
+    }
+  };
+  for (int j = 0; j < groups; ++j)
+    if (shared[j]) tiles(rows[j], steps_of(prefix[j]), true);
+  for (const Request& r : reqs) {
+    const bool s = groups && shared[r.group];
+    tiles(r.rows, steps_of(r.own) + (groups && !s ? steps_of(prefix[r.group]) : 0), s);
+  }
+  int64_t total = 0, sum = 0;
+  for (const U& u : units) total += u.cost;
+  const int chunk = chunk_of(total, slots, few);
+  for (const U& u : units) {
+    const Cut c = cut_of(u.steps, u.cost, chunk);
+    if (u.partial || c.splits > 1) sum += (int64_t)c.splits * u.rows;
+  }
+  return sum;
+}
+
+int main() {
+  std::mt19937 rng(5);
+  auto upto = [&](int n) { return (int)(rng() %% (unsigned)n); };
+  const int sizes[] = {1, 2, 16, 32, 33, 100, 127, 128, 129, 160, 161, 256, 257, 288, 289, 384, 385};
+  int64_t cases = 0, over = 0, shared_near = 0, split_near = 0;
+  for (int i = 0; i < 60000; ++i) {
+    const int few = upto(2) ? 1 : 4, kv = 1 << upto(11), slots = kAttendSlots / kv > 0 ? kAttendSlots / kv : 1;
+    const int n = 1 + upto(upto(2) ? 12 : 200), groups = upto(3) ? 1 + upto(n < 5 ? n : 5) : 0;
+    std::vector<int> prefix(groups);
+    for (int& p : prefix) p = upto(upto(2) ? 400 : 20000);
+    std::vector<Request> reqs(n);
+    const int same = upto(2) ? sizes[upto(17)] : 0, lengths = 1 + upto(upto(2) ? 200 : 30000);
+    int64_t rows = 0;
+    for (int r = 0; r < n; ++r) {
+      reqs[r] = {same ? same : upto(600), 1 + upto(lengths), groups ? r * groups / n : 0};
+      rows += reqs[r].rows;
+    }
+    const int64_t most = most_partial_rows(rows, n, groups > 0, slots), have = partial_rows(reqs, prefix, slots, few, kv);
+    ++cases;
+    over += have > most;
+    if (groups) shared_near += have > 2 * 200 * (int64_t)n;
+    if (!groups) split_near += 2 * have > most;
+  }
+  std::printf("%%lld %%lld %%lld %%lld\\n", (long long)cases, (long long)over, (long long)shared_near, (long long)split_near);
+}
+""".replace("%%", "%"), "-x", "hip", "--offload-arch=gfx950")
+    cases, over, shared_near, split_near = map(int, out)
+    assert cases == 60000 and over == 0
+    assert shared_near > 100 and split_near > 100  # the room is used: more than half of it by many
