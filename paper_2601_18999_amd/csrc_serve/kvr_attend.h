@@ -148,24 +148,25 @@ __device__ const uint32_t kBadRow[4] = {~0u, ~0u, ~0u, ~0u};  // NaN in every ty
 // Loads from memory straight to LDS: lane i's 16 (4) bytes to `to` + 16 i
 // (4 i), `to` the same in all lanes.  The compiler does not see these loads:
 // wait_loads<n> waits until at most n of them are in flight.  (M0 may not be
-// read in the cycle after it is written.)
+// read in the cycle after it is written.  The compiler keeps values of its own
+// there, so it is named as written.)
 __device__ __forceinline__ uint32_t lds_offset(const void* p) {
   return (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(lds_char*)p);
 }
 __device__ __forceinline__ void load16_to_lds(global_bytes from, uint32_t to) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from),
                "s"(__builtin_amdgcn_readfirstlane(to))
-               : "memory");
+               : "memory", "m0");
 }
 __device__ __forceinline__ void load4_to_lds(global_ints from, uint32_t to) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from),
                "s"(__builtin_amdgcn_readfirstlane(to))
-               : "memory");
+               : "memory", "m0");
 }
 // The same with one base for the wave and 32-bit offsets.
 __device__ __forceinline__ void load16_to_lds(uint64_t base, uint32_t offset, uint32_t to) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(__builtin_amdgcn_readfirstlane(to))
-               : "memory");
+               : "memory", "m0");
 }
 template <int N>
 __device__ __forceinline__ void wait_loads() {

@@ -1,6 +1,7 @@
 """The host rules of the serving operators' kernels on the CPU, compiled from
 the headers that the kernels are built from."""
 import os
+import re
 import subprocess
 
 import pytest
@@ -117,3 +118,16 @@ int main() {
     cases, over, shared_near, split_near = map(int, out)
     assert cases == 60000 and over == 0
     assert shared_near > 100 and split_near > 100  # the room is used: more than half of it by many
+
+
+def test_assembler_names_the_registers_that_it_writes():
+    # scalar registers by name: the compiler has to know what it may not keep there
+    statements = 0
+    for name in sorted(os.listdir(SERVE)):
+        text = open(os.path.join(SERVE, name)).read()
+        for asm in re.findall(r"\basm\b(?: volatile)?\s*\((.*?)\);", text, re.S):
+            code, _, operands = asm.partition('"' + ' ::') if '" ::' in asm else asm.partition('" :')
+            for written in re.findall(r"\bs_mov_b(?:32|64) ([a-z_]+[0-9]*),", code):
+                statements += 1
+                assert f'"{written}"' in operands, (name, asm)
+    assert statements == 3
