@@ -90,7 +90,7 @@ def _tables_bytes(rows: int) -> int:
 @functools.lru_cache(maxsize=65536)
 def _attention_bytes(code: int, kv_heads: int, dim: int, q_code: int, tokens: int, requests: int, groups: int,
                      heads: int) -> int:
-    """Workspace of kvr_shared_attention, which these sizes decide (-1: refused)."""
+    """Workspace of kvr_shared_attention, which these sizes decide; raises for what it refuses."""
     return kvr_attention_workspace(
         CACHE_RECORD.pack(CACHE_RECORD.size, code, 1, 1, kv_heads, dim, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0),
         ATTENTION_RECORD.pack(ATTENTION_RECORD.size, q_code, tokens, requests, groups, heads, 0, 0, 1.0, 0, 0, 0, 0, 0,
@@ -108,7 +108,8 @@ def block_tables(held: torch.Tensor, delta: torch.Tensor, table: torch.Tensor, r
     ``num_tokens``: an upper bound of the new tokens, the length of ``slots``
     and ``positions``; ``base`` [rows] int32: position of a row's first token.
     ``table`` and ``ring`` are updated in place, with ``in_place`` also
-    ``held`` and ``state``, else new tensors are returned for these.
+    ``held`` and ``state``, else new tensors are returned for these.  Without
+    any row nothing changes.
     """
     where = "block_tables"
     device = _gpu(where, "held", held)
@@ -125,6 +126,13 @@ def block_tables(held: torch.Tensor, delta: torch.Tensor, table: torch.Tensor, r
     p_table, width, stride = _table(where, "table", table, rows, device)
     if not 0 <= num_tokens < 1 << 31 or not 0 < page_size <= 1024:
         _refuse(where, "num_tokens must be in 0..2^31 - 1, page_size a power of two in 1..1024")
+    if not rows:
+        # the C call takes no empty batch; what it would refuse for one row is refused here too
+        kvr_block_tables_workspace(TABLES_RECORD.pack(TABLES_RECORD.size, 1, max(1, width), page_size, ring.shape[0],
+                                                      num_tokens, max(1, width), *[0] * 11))
+        none = torch.full((2, num_tokens), -1, dtype=i32, device=device)
+        return BlockTables(held if in_place else held.clone(), state if in_place else state.clone(),
+                           torch.zeros(1, dtype=i32, device=device), none[0], none[1])
     nbytes = _tables_bytes(rows)
     # one allocation: the outputs, then the workspace on a 256-byte boundary
     outputs = 2 * rows + 1 + 2 * num_tokens
@@ -226,6 +234,7 @@ def shared_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     is dim ** -0.5 by default.  Returns ``out`` (like ``q`` unless given);
     ``lse`` [tokens, heads] float32 receives the logarithms of the softmax
     sums, ``status`` [1] int32 the KVR_DEV_* bits.  There is no gradient.
+    Without any request nothing is written.
     """
     where = "shared_attention"
     device = _gpu(where, "q", q)
@@ -275,7 +284,12 @@ def shared_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
                                  dim ** -0.5 if scale is None else scale, 0, q.data_ptr(), out.data_ptr(), p_lse, q0,
                                  q1, o0, o1, p_rows, p_length, p_table, p_start, p_prefix, p_plen, stride, pstride,
                                  _status(where, status, device))
-    nbytes = _attention_bytes(DTYPE_CODES[k_cache.dtype], kv_heads, dim, code, tokens, requests, groups, heads)
+    # (the C call takes no batch without requests)
+    nbytes = _attention_bytes(DTYPE_CODES[k_cache.dtype], kv_heads, dim, code, tokens, requests or 1, groups, heads)
+    if not requests:
+        if tokens and not p_rows:
+            _refuse(where, "without row_start there is one token a request")
+        return out
     ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
     kvr_shared_attention(cache, args, ws.data_ptr(), nbytes, _stream(device.index))
     return out

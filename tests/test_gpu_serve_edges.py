@@ -294,3 +294,46 @@ def test_nothing_is_written_behind_the_workspace(new, own, sizes, prefix, heads,
     (whole, nbytes), = buffers
     assert bool((whole[nbytes:] == 0xA5).all())
     R.check(out, lse, p, on_device(p))
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_tables_without_rows_change_nothing(in_place):
+    none = torch.zeros(0, dtype=torch.int32, device=DEV)
+    table = torch.zeros((0, 8), dtype=torch.int32, device=DEV)
+    for tokens in (0, 5):
+        ring, state = K.page_ring(10, DEV)
+        state[0], state[2] = 4, 128
+        r = K.block_tables(none, none.clone(), table, ring, state, 16, tokens, base=none.clone(), in_place=in_place)
+        assert r.held.shape == (0,) and r.row_start.tolist() == [0]
+        assert r.slots.tolist() == r.positions.tolist() == [-1] * tokens
+        assert r.state.tolist() == [4, 10, 128] and ring.tolist() == list(range(10))
+        assert r.held.dtype == r.slots.dtype == r.positions.dtype == r.row_start.dtype == torch.int32
+        assert (r.held is none and r.state is state) == in_place
+    for page, tokens in ((24, 0), (0, 0), (16, -1)):
+        with pytest.raises(K.KvrError):
+            K.block_tables(none, none.clone(), table, ring, state, page, tokens)
+    with pytest.raises(K.KvrError):
+        K.block_tables(none, none.clone(), table[:, :0], ring[:0], state, 16, 0)
+    with pytest.raises(K.KvrError):
+        K.block_tables(none, torch.zeros(1, dtype=torch.int32, device=DEV), table, ring, state, 16, 0)
+
+
+def test_attention_without_requests_writes_nothing():
+    p = R.Problem([1], [20], [1], [9], heads=4, kv_heads=2, dim=64)
+    q, kc, vc, rs, tb, ln, gs, pt, pl = p.args()
+    for groups in ((), (gs[:1], pt[:0], pl[:0]), (torch.zeros_like(gs), pt, pl)):
+        for tokens in (0, 1):
+            out = torch.full_like(q[:tokens], 9.0)
+            lse = torch.full((tokens, 4), 9.0, device=DEV)
+            status = torch.zeros(1, dtype=torch.int32, device=DEV)
+            got = K.shared_attention(q[:tokens], kc, vc, rs[:1], tb[:0], ln[:0], *groups, out=out, lse=lse,
+                                     status=status)
+            assert got is out and (out == 9.0).all() and (lse == 9.0).all() and int(status) == 0
+            if not tokens:
+                assert K.shared_attention(q[:0], kc, vc, None, tb[:0], ln[:0], *groups).shape == (0, 4, 64)
+    for bad in ((q[:, :3], kc, vc, rs[:1], tb[:0], ln[:0]), (q.half(), kc, vc, rs[:1], tb[:0], ln[:0]),
+                (q, kc, vc, rs, tb[:0], ln[:0]), (q, kc, vc, rs[:1], tb, ln[:0]), (q, kc, vc, None, tb[:0], ln[:0])):
+        with pytest.raises(K.KvrError):
+            K.shared_attention(*bad)
+    # and a request again
+    R.check(K.shared_attention(*p.args(), **p.kwargs()), None, p)
