@@ -413,8 +413,10 @@ kvr_status kvr_cache_store(const kvr_cache* c, const kvr_store* s, void* hip_str
  * over the prefix and the own tokens up to t itself; lse[t][i] (optional,
  * [num_tokens][heads]) is the natural logarithm of the softmax's sum.
  * Whatever stands in the cache behind a length or in a later token (an
- * infinity or NaN among them) has no influence on a row; a row that sees no
- * key gets 0 and lse -inf.  Tokens behind d_row_start's last are not written.
+ * infinity or NaN among them) has no influence on a row.  (Every row sees a
+ * key, its own token's.)  A row whose scores are all -inf gets 0 and lse -inf;
+ * a NaN among its scores makes its result and lse NaN.  Tokens behind
+ * d_row_start's last are not written.
  * A prefix is read once for a whole group where its requests have few new
  * tokens each, and the partial results are joined.  The order of the sums
  * depends on the lengths, not on the run: the same call gives the same bits.

@@ -337,3 +337,59 @@ def test_attention_without_requests_writes_nothing():
             K.shared_attention(*bad)
     # and a request again
     R.check(K.shared_attention(*p.args(), **p.kwargs()), None, p)
+
+
+# the last item of the split keys, or a wave's last tile, has keys that only the last rows see
+@pytest.mark.parametrize("new,own", [(64, 513), (100, 577), (128, 705), (20, 1025), (32, 65), (9, 2049)])
+@pytest.mark.parametrize("dim,cache", [(64, None), (256, None), (128, FP8)], ids=["64", "256", "128-8-bit"])
+def test_rows_that_see_nothing_of_an_item(new, own, dim, cache):
+    p = R.Problem([new], [own], heads=1, kv_heads=1, dim=dim, cache=cache).spoil()
+    R.check(*attend(p), p, on_device(p))
+
+
+@pytest.mark.parametrize("new,own,sizes,prefix", [([1, 1], [40, 9], (), ()), ([1, 1], [9000, 9], (), ()),
+                                                  ([1] * 24, [33] * 24, [24], [2100]), ([90, 2], [90, 9], (), ())],
+                         ids=["few", "split", "group", "rows"])
+@pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
+def test_scores_of_minus_infinity(new, own, sizes, prefix, dtype):
+    # all of a request's own keys, and all keys of its prefix too or not: 0 and -inf, or the prefix alone
+    for whole in ((False, True) if sizes else (True,)):
+        p = R.Problem(new, own, sizes, prefix, heads=4, kv_heads=2, dim=64, dtype=dtype)
+        p.q[..., 3] = 1.0
+        rows = [(p.table[0], own[0])] + ([(p.prefix_table[0], prefix[0])] if whole and sizes else [])
+        for row, n in rows:
+            for t in range(n):
+                p.k_cache[row[t // p.page], t % p.page, 1, 3] = -float("inf")
+        ref, size, ref_lse = on_device(p)  # softmax of nothing but -inf is NaN
+        nothing = torch.isnan(ref).any(-1)
+        hidden = torch.zeros_like(nothing)
+        if whole:
+            hidden[:sum(new) if sizes else new[0], 2:] = True
+            if sizes:
+                hidden[1:] = False  # the others have their own tokens
+        assert torch.equal(nothing, hidden)
+        out, lse = attend(p)
+        mask = nothing[..., None]
+        R.check(out, lse, p, [ref.masked_fill(mask, 0.0), size.masked_fill(mask, 0.0), ref_lse])
+        assert (out[nothing.to(DEV)] == 0).all() and (lse[nothing.to(DEV)] == -float("inf")).all()
+
+
+def unit_room(p):
+    """Units that a call has room for: what decides whether its workgroups plan for themselves."""
+    rows = sum(p.new) * p.heads // p.kv_heads
+    return (2 if p.sizes else 1) * (rows // 128) + len(p.new) + len(p.sizes)
+
+
+# every workgroup plans for itself up to 256 units, and up to twice as many units times key heads as the device holds
+# workgroups: 1,024, or 512 with heads of 256
+@pytest.mark.parametrize("requests,groups,kv,dim,room", [
+    (254, 0, 1, 64, 255), (255, 0, 1, 64, 256), (253, 2, 1, 64, 257), (256, 0, 1, 64, 258), (254, 1, 1, 128, 257),
+    (127, 127, 1, 64, 254), (126, 127, 2, 64, 253), (127, 1, 8, 64, 128), (128, 0, 8, 128, 129), (126, 1, 8, 128, 127),
+    (127, 1, 4, 256, 128), (127, 2, 4, 256, 129), (63, 1, 8, 256, 64), (64, 1, 8, 256, 65)])
+@pytest.mark.parametrize("cache", [None, FP8], ids=["16-bit", "8-bit"])
+def test_units_around_the_forms_of_the_plan(requests, groups, kv, dim, room, cache):
+    sizes = [requests // groups] * (groups - 1) + [requests - requests // groups * (groups - 1)] if groups else []
+    p = R.Problem([1] * requests, [1 + 29 * i % 300 for i in range(requests)], sizes,
+                  [300 - i % 250 for i in range(groups)], heads=kv, kv_heads=kv, dim=dim, cache=cache)
+    assert unit_room(p) == room
+    R.check(*attend(p), p, on_device(p))
