@@ -40,7 +40,6 @@ namespace {
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) char lds_char;
@@ -49,7 +48,6 @@ typedef const __attribute__((address_space(1))) char* global_bytes;
 typedef const __attribute__((address_space(1))) i32x4* global_chunk;
 
 struct Bf16 {
-  typedef __bf16 x2 __attribute__((ext_vector_type(2)));
   typedef __bf16 x8 __attribute__((ext_vector_type(8)));
   typedef __bf16 x4 __attribute__((ext_vector_type(4)));
   static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
@@ -66,7 +64,6 @@ struct Bf16 {
 };
 
 struct Fp16 {
-  typedef _Float16 x2 __attribute__((ext_vector_type(2)));
   typedef _Float16 x8 __attribute__((ext_vector_type(8)));
   typedef _Float16 x4 __attribute__((ext_vector_type(4)));
   static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
@@ -261,6 +258,7 @@ struct Widened {
   static constexpr int kRows = kThreads / kChunks;
   static constexpr int kN = S::kKeys / kRows;
   static_assert(kThreads % kChunks == 0 && S::kKeys % kRows == 0, "tile shape");
+  static_assert(kN <= 4, "addresses that are held at once");
 
   i32x4 k[kN], v[kN];
 
@@ -278,28 +276,17 @@ struct Widened {
       else if ((uint32_t)page[i] >= (uint32_t)a.num_pages)
         pk = pv = (global_bytes)kBadRow;
     };
-    if constexpr (kN > 4) {  // too many addresses to hold: one after the other
+    global_bytes pk[kN], pv[kN];
 #pragma unroll
-      for (int i = 0; i < kN; ++i) {
-        global_bytes pk, pv;
-        place(i, pk, pv);
-        check(i, pk, pv);
-        k[i] = *(global_chunk)pk;
-        v[i] = *(global_chunk)pv;
-      }
-    } else {
-      global_bytes pk[kN], pv[kN];
+    for (int i = 0; i < kN; ++i) place(i, pk[i], pv[i]);
+    if (!whole) {
 #pragma unroll
-      for (int i = 0; i < kN; ++i) place(i, pk[i], pv[i]);
-      if (!whole) {
+      for (int i = 0; i < kN; ++i) check(i, pk[i], pv[i]);
+    }
 #pragma unroll
-        for (int i = 0; i < kN; ++i) check(i, pk[i], pv[i]);
-      }
-#pragma unroll
-      for (int i = 0; i < kN; ++i) {
-        k[i] = *(global_chunk)pk[i];
-        v[i] = *(global_chunk)pv[i];
-      }
+    for (int i = 0; i < kN; ++i) {
+      k[i] = *(global_chunk)pk[i];
+      v[i] = *(global_chunk)pv[i];
     }
   }
 

@@ -251,8 +251,7 @@ __global__ void __launch_bounds__(256) store_kernel(StoreArgs a) {
 template <bool SMALL>
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(AttendArgs a) {
   __shared__ int lds[SMALL ? plan_words(kPlanSmall) : plan_words(0)];
-  const int units = make_plan<SMALL ? kPlanSmall : 0>(a, lds, true, [&](int i, const Item& it) { a.items[i] = it; });
-  (void)units;
+  make_plan<SMALL ? kPlanSmall : 0>(a, lds, true, [&](int i, const Item& it) { a.items[i] = it; });
 }
 
 // ---------------------------------------------------------------- attention: the join
@@ -281,7 +280,7 @@ __global__ void __launch_bounds__(256) join_kernel(AttendArgs a) {
     const int row = x.row0 + r;
     float m = -INFINITY, l = 0.0f;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    // n partial results, `step` rows apart; eight are on their way at a time
+    // n partial results, `step` rows apart; four are on their way at a time
     auto add = [&](int first, int step, int n) {
       for (int s0 = 0; s0 < n; s0 += kJoinAtOnce) {
         float2 ml[kJoinAtOnce];

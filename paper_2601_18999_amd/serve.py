@@ -17,7 +17,7 @@ from typing import NamedTuple, Optional
 
 import torch
 
-from . import (KVR_EINVAL, KvrError, _check, kvr_attention_workspace, kvr_block_tables, kvr_block_tables_workspace,
+from . import (KVR_EINVAL, KvrError, kvr_attention_workspace, kvr_block_tables, kvr_block_tables_workspace,
                kvr_cache_store, kvr_shared_attention)
 
 DTYPE_CODES = {torch.bfloat16: 0, torch.float16: 1, torch.float8_e4m3fn: 2}
