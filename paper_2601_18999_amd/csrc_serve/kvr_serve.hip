@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(256) store_kernel(StoreArgs a) {
 // The plan in a launch of its own: the items in memory.
 template <bool SMALL>
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(AttendArgs a) {
-  __shared__ int lds[SMALL ? plan_words(kPlanSmall) : plan_words(0)];
+  __shared__ __attribute__((aligned(8))) int lds[SMALL ? plan_words(kPlanSmall) : plan_words(0)];
   make_plan<SMALL ? kPlanSmall : 0>(a, lds, true, [&](int i, const Item& it) { a.items[i] = it; });
 }
 
