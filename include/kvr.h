@@ -389,7 +389,7 @@ typedef struct kvr_cache {
 typedef struct kvr_store {
   uint32_t struct_size;
   int32_t dtype;
-  int32_t num_tokens; /* >= 0; num_tokens * kv_heads * dim / 8 < 2^31       */
+  int32_t num_tokens; /* >= 0; num_tokens * kv_heads * dim / 8 <= 2^31 - 257 */
   int32_t pad;
   const void *d_k, *d_v;
   int64_t k_token, k_head, v_token, v_head;

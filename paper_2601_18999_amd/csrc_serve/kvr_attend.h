@@ -892,9 +892,11 @@ __device__ __forceinline__ void attend_item(const AttendArgs& a, const Item& it,
 }
 
 // Many rows: bound by the matrix and the vector unit, whose times add up (9,216
-// new tokens of 32 / 8 heads of 128: 710 to 720 us, 970 to 990 TFLOP/s, where a
-// library product reaches 1,264).  Few rows: bound by memory (64 requests in
-// four groups, 243 MB: 50 us, 4.9 TB/s, where a copy reaches 5.1).
+// new tokens of 32 / 8 heads of 128: 695 to 740 us on different devices, 940 to
+// 1,000 TFLOP/s, where a library product reaches 1,230 to 1,264; heads of 256,
+// 6,000 new tokens of 16 / 4 heads: 480 to 491 us, 600 to 614 TFLOP/s).  Few
+// rows: bound by memory (64 requests in four groups, 243 MB: 50 us, 4.9 TB/s,
+// where a copy reaches 5.1; 57 us with the plan in each workgroup).
 template <int D, class T, bool FP8>
 __global__ void __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) attend_kernel(AttendArgs a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];

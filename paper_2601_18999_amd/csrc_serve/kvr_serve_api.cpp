@@ -218,7 +218,7 @@ kvr_status kvr_cache_store(const kvr_cache* c, const kvr_store* s, void* hip_str
   if (c->dtype != KVR_FP8 && c->dtype != s->dtype) return invalid("a 16-bit cache holds the type that is stored");
   const int64_t chunks = (int64_t)c->kv_heads * c->dim / 8;
   if (s->num_tokens < 0 || s->num_tokens * chunks > kInt - 256)
-    return invalid("num_tokens must be >= 0, num_tokens * kv_heads * dim / 8 below 2^31");
+    return invalid("num_tokens must be >= 0, num_tokens * kv_heads * dim / 8 at most 2^31 - 257");
   if (s->num_tokens == 0) return KVR_OK;
   CacheSteps kc, vc;
   st = check_buffers(c, &kc, &vc);

@@ -30,7 +30,12 @@ ATTENTION_RECORD = struct.Struct("<I7ifi3Q4q6Q2qQ")
 
 
 class BlockTables(NamedTuple):
-    """What ``block_tables`` returns; the table and the ring are updated in place."""
+    """What ``block_tables`` returns; the table and the ring are updated in place.
+
+    ``row_start``, ``slots``, ``positions`` and (unless ``in_place``) ``held``
+    are views of one allocation, which lives as long as one of them: clone
+    what is kept beyond the step.
+    """
     held: torch.Tensor       # [rows] int32: tokens of each row
     state: torch.Tensor      # [3] int64: ring head, ring tail, status bits
     row_start: torch.Tensor  # [rows + 1] int32: new tokens of the rows before

@@ -31,3 +31,10 @@ def test_the_workspace_of_one_long_prompt_does_not_grow_with_it(groups):
         return K.kvr_attention_workspace(cache(kv_heads=8), attention(num_tokens=tokens, num_requests=1,
                                                                       num_groups=groups, heads=32))
     assert size(9216) < 80 << 20 and size(131072) < size(9216) + (8 << 20)
+
+
+def test_more_tokens_than_a_store_counts_are_refused():
+    # chunks of 8 elements of all tokens: at most 2^31 - 257
+    for kv, dim, tokens in ((1, 64, (1 << 28) - 32), (8, 128, (1 << 24) - 2), (1024, 256, 1 << 16)):
+        assert tokens * kv * dim // 8 > (1 << 31) - 257
+        _refused(lambda: K.kvr_cache_store(cache(kv_heads=kv, dim=dim), store(num_tokens=tokens)))
