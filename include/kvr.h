@@ -318,7 +318,8 @@ void kvr_destroy(kvr_ctx* ctx);
  * stated at each operator, and or-ed into a status word (KVR_DEV_*).
  * ------------------------------------------------------------------------ */
 
-enum { KVR_BF16 = 0, KVR_FP16 = 1, KVR_FP8 = 2 }; /* element types; KVR_FP8: OCP e4m3 */
+/* element types; KVR_FP8: OCP e4m3; KVR_INT8: two's complement */
+enum { KVR_BF16 = 0, KVR_FP16 = 1, KVR_FP8 = 2, KVR_INT8 = 3, KVR_FP32 = 4 };
 
 /* Pages for rows that gain or lose tokens.  Row r (a request's own tokens, or
  * a group's prefix) holds d_held[r] tokens in the first ceil(held / page_size)
@@ -453,6 +454,118 @@ kvr_status kvr_attention_workspace(const kvr_cache* c, const kvr_attention* a, s
 
 kvr_status kvr_shared_attention(const kvr_cache* c, const kvr_attention* a, void* d_workspace, size_t bytes,
                                 void* hip_stream);
+
+/* What stands around the attention in a worker's layer.  Rows (a token's
+ * values) may have any stride; the elements of a row are neighbours. */
+
+/* The norms behind and before a block, with its gate and the residual.  For
+ * each token, in 32 bits:
+ *   a = x
+ *   a = a * rsqrt(mean(a^2) + eps) * after          (d_after, or left out)
+ *   a = a * act(gate)                               (d_gate, or left out)
+ *   r = residual + residual_scale * a               (d_residual; else r = a)
+ *   n = r * rsqrt(mean(r^2) + eps) * before         (d_before, or left out)
+ * d_residual_out receives r (required with d_residual, which it may be; NULL
+ * without), d_out receives n: rounded to dtype, or as KVR_INT8 with a scale
+ * for each token in d_out_scale, scale = max |n| / 127 and n * (127 / max |n|)
+ * rounded to nearest even.  A row whose largest magnitude is below 2^-100 has
+ * zeros and the scale 0; one that holds an infinity or NaN has zeros and the
+ * scale NaN.  (n is made of the r before it is rounded for d_residual_out.)
+ * d_out may be d_x where the types and strides are the same, else outputs do
+ * not overlap inputs. */
+enum { KVR_ACT_NONE = 0, KVR_ACT_SIGMOID = 1, KVR_ACT_SILU = 2 }; /* z, 1 / (1 + e^-z), z / (1 + e^-z) */
+
+typedef struct kvr_norm {
+  uint32_t struct_size;
+  int32_t dtype;          /* of x, weights, gate: KVR_BF16 or KVR_FP16        */
+  int32_t residual_dtype; /* dtype or KVR_FP32                                */
+  int32_t out_dtype;      /* dtype or KVR_INT8                                */
+  int32_t num_tokens;     /* >= 0                                             */
+  int32_t dim;            /* 1..65536                                         */
+  int32_t activation;     /* KVR_ACT_*, of the gate                           */
+  float eps;              /* finite, > 0                                      */
+  float residual_scale;   /* finite                                           */
+  int32_t pad;
+  const void *d_x, *d_after, *d_gate, *d_residual, *d_before;
+  void *d_residual_out, *d_out;
+  float* d_out_scale;
+  int64_t x_token, gate_token, residual_token, residual_out_token, out_token; /* gate_token may be 0 */
+} kvr_norm;
+
+kvr_status kvr_block_norm(const kvr_norm* n, void* hip_stream);
+
+/* A matrix product in 8-bit integers with scales for each token and channel:
+ *   out[t][c] = float(sum_k x[t][k] w[c][k]) * x_scale[t] * w_scale[c] + bias[c]
+ * (bias optional; one rounding to the type of d_out behind the 32-bit ones).
+ * d_x holds KVR_INT8 with d_x_scale, or KVR_BF16 / KVR_FP16, which are brought
+ * to integers with a scale for each token as kvr_block_norm does it, in the
+ * workspace.  The sum is exact.  Every row of w, and of 8-bit x, starts on a
+ * 16-byte boundary. */
+typedef struct kvr_product {
+  uint32_t struct_size;
+  int32_t dtype;      /* of d_x: KVR_INT8, KVR_BF16 or KVR_FP16               */
+  int32_t out_dtype;  /* KVR_BF16, KVR_FP16 or KVR_FP32                       */
+  int32_t num_tokens; /* >= 0                                                 */
+  int32_t dim;        /* k: a multiple of 16, 16..65536                       */
+  int32_t channels;   /* 1..2^24                                              */
+  const void *d_x, *d_w;
+  void* d_out;
+  const float *d_x_scale, *d_w_scale, *d_bias;
+  int64_t x_token, w_channel, out_token;
+} kvr_product;
+
+/* Bytes of d_workspace that kvr_integer_product needs (0: none).  Pure host
+ * function. */
+kvr_status kvr_product_workspace(const kvr_product* p, size_t* bytes);
+
+kvr_status kvr_integer_product(const kvr_product* p, void* d_workspace, size_t bytes, void* hip_stream);
+
+/* Linear attention with a decay for each key head: in the place of a cache, a
+ * request has a state S of dim x dim values per key head.  For its new tokens
+ * t (ragged requests as in kvr_attention) and a query head i of key head
+ * h = i / (heads / kv_heads)
+ *   S_t = exp(log_decay[h]) S_(t-1) + k_t v_t^T,   out[t][i] = scale * q_t S_t,
+ * element [a][b] of S belongs to element a of the keys and b of the values.
+ * The states stand in the slots of a pool, in 32 bits: the state before
+ * request r's first new token is that of slot d_read[r] (-1: zero), which many
+ * requests may share (the state behind their group's prefix); the one behind
+ * its last new token goes to slot d_write[r] (-1: nowhere; d_write NULL =
+ * d_read).  A request without new tokens copies its state.  A slot that one
+ * request writes is neither written nor read by another one of the call.
+ * log_decay is a natural logarithm, <= 0; -inf forgets all but the own token.
+ * What stands in a later token, or in another request, has no influence on a
+ * row (infinities and NaN among it).  Tokens behind d_row_start's last are
+ * not written.  Where a call's tokens are split differently over calls, the
+ * results differ by roundings; the same call gives the same bits.
+ * row_start that is not valid (negative, decreasing, more than num_tokens)
+ * sets KVR_DEV_BAD_LENGTH in d_status (optional): every result is NaN, no
+ * state is written.  A slot that the pool does not have sets KVR_DEV_BAD_PAGE:
+ * the request's results are NaN, its state is not written. */
+typedef struct kvr_linear {
+  uint32_t struct_size;
+  int32_t dtype;        /* of q, k, v, out: KVR_BF16 or KVR_FP16              */
+  int32_t num_tokens;   /* >= 0; num_tokens * heads < 2^31                    */
+  int32_t num_requests; /* 1..2^20                                            */
+  int32_t heads;        /* a multiple of kv_heads                             */
+  int32_t kv_heads;     /* 1..1024                                            */
+  int32_t dim;          /* 64 or 128                                          */
+  int32_t num_slots;    /* >= 1                                               */
+  float scale;          /* finite                                             */
+  int32_t pad;
+  const void *d_q, *d_k, *d_v;
+  void* d_out;
+  float* d_state;
+  int64_t q_token, q_head, k_token, k_head, v_token, v_head, out_token, out_head;
+  int64_t state_slot, state_head; /* a state's dim * dim values are neighbours  */
+  const float* d_log_decay;       /* [kv_heads]                                 */
+  const int32_t *d_row_start, *d_read, *d_write;
+  uint32_t* d_status;
+} kvr_linear;
+
+/* Bytes of d_workspace that kvr_linear_attention needs.  Pure host function. */
+kvr_status kvr_linear_workspace(const kvr_linear* l, size_t* bytes);
+
+kvr_status kvr_linear_attention(const kvr_linear* l, void* d_workspace, size_t bytes, void* hip_stream);
 
 /* Message for the last failure on this thread ("" if none). */
 const char* kvr_last_error(void);

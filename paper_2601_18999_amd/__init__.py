@@ -31,7 +31,8 @@ PHASE_NAMES = ["route", "stage_wait", "mark", "load", "evict", "finish", "match"
 EXPORTED = ["kvr_config_default", "kvr_workspace_size", "kvr_init_replicas", "kvr_route_batch",
             "kvr_stats", "kvr_stats_noalloc", "kvr_check", "kvr_queries_done", "kvr_destroy", "kvr_last_error",
             "kvr_block_tables_workspace", "kvr_block_tables", "kvr_cache_store", "kvr_attention_workspace",
-            "kvr_shared_attention"]
+            "kvr_shared_attention", "kvr_block_norm", "kvr_product_workspace", "kvr_integer_product",
+            "kvr_linear_workspace", "kvr_linear_attention"]
 
 
 class KvrConfig(ctypes.Structure):
@@ -146,7 +147,12 @@ def load_library() -> ctypes.CDLL:
                        ("kvr_block_tables", [vp, vp, ctypes.c_size_t, vp]),
                        ("kvr_cache_store", [vp, vp, vp]),
                        ("kvr_attention_workspace", [vp, vp, size_p]),
-                       ("kvr_shared_attention", [vp, vp, vp, ctypes.c_size_t, vp])):
+                       ("kvr_shared_attention", [vp, vp, vp, ctypes.c_size_t, vp]),
+                       ("kvr_block_norm", [vp, vp]),
+                       ("kvr_product_workspace", [vp, size_p]),
+                       ("kvr_integer_product", [vp, vp, ctypes.c_size_t, vp]),
+                       ("kvr_linear_workspace", [vp, size_p]),
+                       ("kvr_linear_attention", [vp, vp, ctypes.c_size_t, vp])):
         getattr(lib, name).restype = ctypes.c_int
         getattr(lib, name).argtypes = args
     lib.kvr_last_error.restype = ctypes.c_char_p
@@ -266,7 +272,7 @@ def kvr_destroy(ctx: int) -> None:
 
 
 # Serving operators: the arguments are the packed structs of include/kvr.h (bytes);
-# the functions on tensors that pack them are in serve.py.
+# the functions on tensors that pack them are in serve.py and layer.py.
 
 def kvr_block_tables_workspace(tables: bytes) -> int:
     n = ctypes.c_size_t(0)
@@ -299,6 +305,36 @@ def kvr_shared_attention(cache: bytes, attention: bytes, d_workspace: int, nbyte
         _check(st, "kvr_shared_attention")
 
 
+def kvr_block_norm(norm: bytes, stream: int = 0) -> None:
+    st = (_lib or load_library()).kvr_block_norm(bytes(norm), stream)
+    if st:
+        _check(st, "kvr_block_norm")
+
+
+def kvr_product_workspace(product: bytes) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load_library().kvr_product_workspace(bytes(product), ctypes.byref(n)), "kvr_product_workspace")
+    return n.value
+
+
+def kvr_integer_product(product: bytes, d_workspace: int = 0, nbytes: int = 0, stream: int = 0) -> None:
+    st = (_lib or load_library()).kvr_integer_product(bytes(product), d_workspace, nbytes, stream)
+    if st:
+        _check(st, "kvr_integer_product")
+
+
+def kvr_linear_workspace(linear: bytes) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load_library().kvr_linear_workspace(bytes(linear), ctypes.byref(n)), "kvr_linear_workspace")
+    return n.value
+
+
+def kvr_linear_attention(linear: bytes, d_workspace: int = 0, nbytes: int = 0, stream: int = 0) -> None:
+    st = (_lib or load_library()).kvr_linear_attention(bytes(linear), d_workspace, nbytes, stream)
+    if st:
+        _check(st, "kvr_linear_attention")
+
+
 from .sim import Simulator  # noqa: E402,F401
 
 
@@ -307,5 +343,9 @@ def __getattr__(name: str):
     if name in ("BlockTables", "block_tables", "page_ring", "cache_store", "shared_attention", "check_status"):
         from . import serve
         globals()[name] = getattr(serve, name)
+        return globals()[name]
+    if name in ("BlockNorm", "block_norm", "integer_product", "linear_attention"):
+        from . import layer
+        globals()[name] = getattr(layer, name)
         return globals()[name]
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -15,7 +15,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB = os.path.join(HERE, "libkvr.so")
 # the simulator, and the serving operators
 SOURCES = ["csrc/kvr_device.hip", "csrc/kvr_api.cpp", "csrc_serve/kvr_serve.hip", "csrc_serve/kvr_serve_api.cpp",
-           "csrc_serve/kvr_attend_64.hip", "csrc_serve/kvr_attend_128.hip", "csrc_serve/kvr_attend_256.hip"]
+           "csrc_serve/kvr_attend_64.hip", "csrc_serve/kvr_attend_128.hip", "csrc_serve/kvr_attend_256.hip",
+           "csrc_serve/kvr_layer_api.cpp", "csrc_serve/kvr_norm.hip", "csrc_serve/kvr_product.hip",
+           "csrc_serve/kvr_linear.hip"]
 ARCH = os.environ.get("KVR_OFFLOAD_ARCH", "gfx950")
 
 FLAGS = [

@@ -1,0 +1,70 @@
+// kvr_layer.h - arguments of the kernels around the attention of a worker's
+// layer (norms, 8-bit products) and of linear attention: what the host side
+// fills in and the device side reads.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+#include "../../include/kvr.h"
+#include "kvr_serve.h"
+
+namespace kvr {
+
+// ---- norms ----
+struct NormArgs {
+  const char *x, *after, *gate, *residual, *before;
+  char *residual_out, *out;
+  float* out_scale;
+  int64_t x_tok, gate_tok, res_tok, res_out_tok, out_tok;  // bytes
+  int32_t tokens, dim, activation;
+  int32_t res32, int8;  // 1: 32-bit residual; 8-bit result
+  float eps, residual_scale, inv_dim;
+};
+
+// ---- 8-bit products ----
+struct ProductArgs {
+  const char *x, *w;
+  char* out;
+  const float *x_scale, *w_scale, *bias;
+  int64_t x_tok, w_chan, out_tok;  // bytes
+  int32_t tokens, dim, channels;
+};
+
+// ---- linear attention ----
+// A run of up to LinearArgs::segment tokens of one request.
+struct Segment {
+  int32_t request, row0, rows;
+  int32_t index;  // among its request's
+};
+
+struct LinearHdr {
+  int32_t segments, rejected;
+};
+
+struct LinearArgs {
+  const char *q, *k, *v;
+  char* out;
+  float* state;
+  const float* log_decay;
+  const int32_t *row_start, *read, *write;
+  uint32_t* status;
+  LinearHdr* hdr;
+  Segment* segments;
+  float* added;  // [segment][kv head][dim][dim]
+  int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head, o_tok, o_head;  // bytes
+  int64_t state_slot, state_head;                                     // elements
+  Divisor kv_div;                                                     // by kv_heads
+  int32_t tokens, requests, heads, kv_heads, share, dim, slots;
+  int32_t segment, segment_cap;
+  float scale;
+};
+
+hipError_t launch_norm(const NormArgs& a, bool fp16, hipStream_t st);
+// out: KVR_BF16, KVR_FP16 or KVR_FP32
+hipError_t launch_product(const ProductArgs& a, int out, hipStream_t st);
+hipError_t launch_linear(const LinearArgs& a, bool fp16, hipStream_t st);
+
+}  // namespace kvr

@@ -3,23 +3,20 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
-#include <cstdio>
 
+#include "kvr_checks.h"
 #include "kvr_serve.h"
 
 namespace {
 
+using kvr::aligned;
+using kvr::hip_failed;
+using kvr::invalid;
+using kvr::kInt;
+using kvr::on_chunks;
+using kvr::round_up;
 using kvr::set_error;
-
-constexpr int64_t kInt = 0x7fffffff;
-
-kvr_status invalid(const char* msg) { return set_error(KVR_EINVAL, msg); }
-
-kvr_status hip_failed(hipError_t e, const char* what) {
-  char msg[256];
-  std::snprintf(msg, sizeof(msg), "%s: %s", what, hipGetErrorString(e));
-  return set_error(KVR_EDEVICE, msg);
-}
+using kvr::step;
 
 bool power_of_two(int32_t x) { return x > 0 && (x & (x - 1)) == 0; }
 
@@ -28,10 +25,6 @@ int log2_of(int32_t x) {
   while ((1 << s) < x) ++s;
   return s;
 }
-
-bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
-
-size_t round_up(size_t n) { return (n + 255) & ~size_t(255); }
 
 kvr_status check(const kvr_tables* t) {
   if (!t) return invalid("tables is NULL");
@@ -60,12 +53,6 @@ kvr_status check(const kvr_cache* c) {
   if (c->dtype != KVR_FP8 && (c->d_k_scale || c->d_v_scale)) return invalid("scales are for an 8-bit cache");
   return KVR_OK;
 }
-
-// A stride in bytes; where there is one of a kind there is no next one, and
-// whatever the caller's stride is has no meaning.
-int64_t step(int64_t stride, int64_t n, int size) { return n > 1 ? stride * size : 0; }
-
-bool on_chunks(int64_t a, int64_t b, int64_t c = 0) { return ((a | b | c) & 15) == 0; }
 
 // The strides of a cache in bytes.
 struct CacheSteps {
