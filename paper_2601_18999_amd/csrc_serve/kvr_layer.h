@@ -34,10 +34,17 @@ struct ProductArgs {
 };
 
 // ---- linear attention ----
+// Requests of up to so many tokens take the recurrent form.
+constexpr int kFewTokens = 4;
+// Workgroups of the chunked form that the device holds.
+constexpr int kLinearSlots = 2 * kComputeUnits;
+
 // A run of up to LinearArgs::segment tokens of one request.
 struct Segment {
   int32_t request, row0, rows;
-  int32_t index;  // among its request's
+  int32_t index, parts;  // of its request's segments
+  int32_t slot;          // of LinearArgs::added, of the request's first segment
+  int32_t pad, pad1;
 };
 
 struct LinearHdr {
@@ -53,7 +60,9 @@ struct LinearArgs {
   uint32_t* status;
   LinearHdr* hdr;
   Segment* segments;
-  float* added;  // [segment][kv head][dim][dim]
+  // [slot][kv head][dim][dim], one for each segment of the requests of several:
+  // what the segment before adds to the state, then the state before this one
+  float* added;
   int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head, o_tok, o_head;  // bytes
   int64_t state_slot, state_head;                                     // elements
   Divisor kv_div;                                                     // by kv_heads

@@ -78,18 +78,27 @@ kvr_status check(const kvr_linear* l) {
 }
 
 struct LinearLayout {
-  size_t segments, bytes;
+  size_t segments, added, bytes;
   int32_t segment, segment_cap;
 };
 
+// Segments of equal length, as many as the device holds workgroups (one takes
+// a segment's key head), but not of fewer than 256 tokens.
 kvr_status lay_out(const kvr_linear* l, LinearLayout* o) {
-  o->segment = INT32_MAX;
-  const int64_t cap = l->num_requests;
+  const int64_t tokens = l->num_tokens;
+  const int64_t even = (tokens * l->kv_heads + kvr::kLinearSlots - 1) / kvr::kLinearSlots;
+  const int64_t segment = even > 256 ? (even + 63) / 64 * 64 : 256;
+  const int64_t cap = l->num_requests + (l->d_row_start ? tokens / segment : 0);
+  // (a launch has fewer than 2^32 threads)
   if (cap * l->kv_heads >= 1 << 24)
-    return invalid("too many requests and heads for one launch: num_requests * kv_heads must be below 2^24");
+    return invalid("too many requests and heads for one launch: num_requests * kv_heads must be below 2^24 - 512");
+  o->segment = (int32_t)(segment < kInt ? segment : kInt);
   o->segment_cap = (int32_t)cap;
   o->segments = 256;
-  o->bytes = l->d_row_start ? 256 + round_up((size_t)cap * sizeof(kvr::Segment)) : 0;
+  o->added = 256 + round_up((size_t)cap * sizeof(kvr::Segment));
+  // a request of several segments has at most twice as many as full ones
+  const size_t slots = tokens > segment ? 2 * (size_t)(tokens / segment) : 0;
+  o->bytes = l->d_row_start ? o->added + slots * l->kv_heads * l->dim * l->dim * 4 : 0;
   return KVR_OK;
 }
 
@@ -244,7 +253,7 @@ kvr_status kvr_linear_attention(const kvr_linear* l, void* d_workspace, size_t b
   a.status = l->d_status;
   a.hdr = reinterpret_cast<kvr::LinearHdr*>(ws);
   a.segments = reinterpret_cast<kvr::Segment*>(ws + o.segments);
-  a.added = nullptr;
+  a.added = reinterpret_cast<float*>(ws + o.added);
   a.kv_div = kvr::make_divisor((uint32_t)l->kv_heads);
   a.tokens = l->num_tokens;
   a.requests = l->num_requests;
