@@ -36,6 +36,7 @@ FLAGS = [
 # written, which the compiler would remark upon for each statement.
 EXTRA = {f"csrc_serve/kvr_attend_{d}.hip": ["-mllvm", "-amdgpu-use-amdgpu-trackers=1", "-Wno-inline-asm"]
          for d in (64, 128, 256)}
+EXTRA["csrc_serve/kvr_product.hip"] = ["-Wno-inline-asm"]
 
 
 def hipcc() -> str:

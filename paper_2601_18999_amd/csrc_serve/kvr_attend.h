@@ -32,6 +32,7 @@
 #include <atomic>
 #include <type_traits>
 
+#include "kvr_lds.h"
 #include "kvr_plan.h"
 
 namespace kvr {
@@ -42,9 +43,6 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) char lds_char;
-typedef const __attribute__((address_space(1))) int32_t* global_ints;
-typedef const __attribute__((address_space(1))) char* global_bytes;
 typedef const __attribute__((address_space(1))) i32x4* global_chunk;
 
 struct Bf16 {
@@ -141,40 +139,6 @@ constexpr int attend_lds() {
 // whose page number is none.
 __device__ const uint32_t kNoRow[4] = {0, 0, 0, 0};
 __device__ const uint32_t kBadRow[4] = {~0u, ~0u, ~0u, ~0u};  // NaN in every type
-
-// Loads from memory straight to LDS: lane i's 16 (4) bytes to `to` + 16 i
-// (4 i), `to` the same in all lanes.  The compiler does not see these loads:
-// wait_loads<n> waits until at most n of them are in flight.  (M0 may not be
-// read in the cycle after it is written.  The compiler keeps values of its own
-// there, so it is named as written.)
-__device__ __forceinline__ uint32_t lds_offset(const void* p) {
-  return (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(lds_char*)p);
-}
-__device__ __forceinline__ void load16_to_lds(global_bytes from, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from),
-               "s"(__builtin_amdgcn_readfirstlane(to))
-               : "memory", "m0");
-}
-__device__ __forceinline__ void load4_to_lds(global_ints from, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from),
-               "s"(__builtin_amdgcn_readfirstlane(to))
-               : "memory", "m0");
-}
-// The same with one base for the wave and 32-bit offsets.
-__device__ __forceinline__ void load16_to_lds(uint64_t base, uint32_t offset, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(__builtin_amdgcn_readfirstlane(to))
-               : "memory", "m0");
-}
-template <int N>
-__device__ __forceinline__ void wait_loads() {
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
-// every read of LDS by this wave has been answered
-__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
-// a barrier that does not wait for loads in flight
-__device__ __forceinline__ void barrier() {
-  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-}
 
 // page * page_bytes + slot * slot_bytes behind base (32-bit factors: two multiply-adds)
 __device__ __forceinline__ global_bytes row_address(global_bytes base, int page, int slot, uint32_t page_bytes,
