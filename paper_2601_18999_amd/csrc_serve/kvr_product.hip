@@ -10,6 +10,7 @@
 #include <hip/hip_runtime.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "kvr_layer.h"
 #include "kvr_lds.h"
@@ -19,59 +20,63 @@ namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kStep = 128;  // elements of k that a tile holds
+constexpr int kStep = 64;   // elements of k that a tile holds
 constexpr int kXcds = 8;    // workgroups go to them in turn
 
 // What is read in the place of elements behind the last one.
 __device__ const uint32_t kZeros[4] = {0, 0, 0, 0};
 
-template <class T>
-struct Four {
-  T e[4];
+template <class T, int N>
+struct Some {
+  T e[N];
 };
 
-// Four neighbouring channels of a token.
-template <class T>
-__device__ __forceinline__ void store4(const ProductArgs& a, int token, int channel, f32x4 f) {
-  T* to = reinterpret_cast<T*>(a.out + token * a.out_tok) + channel;
-  if (channel + 4 <= a.channels) {
-    Four<T> x;
+// N neighbouring channels of a token, as many as there are.
+template <class T, int N>
+__device__ __forceinline__ void store(char* row, int channel, int channels, const float (&f)[N]) {
+  T* to = reinterpret_cast<T*>(row) + channel;
+  if (channel + N <= channels) {
+    Some<T, N> x;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x.e[e] = (T)f[e];
+    for (int e = 0; e < N; ++e) x.e[e] = (T)f[e];
     __builtin_memcpy(to, &x, sizeof(x));
   } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (channel + e < a.channels) to[e] = (T)f[e];
+    for (int e = 0; e < N; ++e)
+      if (channel + e < channels) to[e] = (T)f[e];
   }
 }
 
 // A tile of WC * FC * 32 channels and WT * FT * 32 tokens by WC * WT waves,
 // each of which has FC * FT results of 32 x 32.
 //
-// k passes in steps of 128: rows of 128 bytes of both operands go from memory
-// straight to LDS, two steps ahead of their use, into two buffers in turn.
-// 16-byte chunks of a row stand at chunk ^ (row / 2 % 8): the reads of one
-// chunk of 16 rows fall on different banks.
-template <int WC, int WT, int FC, int FT>
+// k passes in steps of 64: rows of 64 bytes of both operands go from memory
+// straight to LDS, into BUFFERS buffers in turn.  16-byte chunks of a row stand
+// at chunk ^ (row / 4 % 4): the reads of one chunk of 16 rows fall on
+// different banks.
+template <int WC, int WT, int FC, int FT, int BUFFERS>
 struct Shape {
   static constexpr int kWaves = WC * WT, kThreads = 64 * kWaves;
   static constexpr int kChannels = WC * FC * 32, kTokens = WT * FT * 32;
   static constexpr int kRows = kChannels + kTokens;
-  static constexpr int kBuffer = kRows * kStep, kBytes = 2 * kBuffer;
-  static constexpr int kLoads = kRows / 8 / kWaves;  // of a wave, for a step
-  static_assert(kLoads * 8 * kWaves == kRows && kWaves % 2 == 0, "tile shape");
+  static constexpr int kBuffer = kRows * kStep, kPitch = 4 * kChannels + 16, kResults = WT * 32 * kPitch;
+  static constexpr int kTiles = BUFFERS * kBuffer > kResults ? BUFFERS * kBuffer : kResults;
+  static constexpr int kBytes = kTiles + (kTokens + 2 * kChannels) * 4;  // and the tile's scales and biases
+  static constexpr int kLoads = kRows / 16 / kWaves;  // of a wave, for a step: 16 rows each
+  static_assert(kLoads * 16 * kWaves == kRows, "tile shape");
 };
 
 __device__ __forceinline__ const i32x4* chunk_at(const char* tile, int row, int chunk) {
-  return (const i32x4*)(tile + row * kStep + ((chunk ^ (row >> 1 & 7)) << 4));
+  return (const i32x4*)(tile + row * kStep + ((chunk ^ (row >> 2 & 3)) << 4));
 }
 
-template <class T, int WC, int WT, int FC, int FT>
-__global__ __launch_bounds__(64 * WC * WT, 2) void product_kernel(ProductArgs a, uint32_t across, uint32_t down) {
-  typedef Shape<WC, WT, FC, FT> S;
+// kinds of instructions for the scheduler
+constexpr int kProducts = 0x8, kReads = 0x100;
+
+template <class T, int WC, int WT, int FC, int FT, int BUFFERS>
+__global__ __launch_bounds__(64 * WC * WT, FC * FT > 8 ? 1 : 2) void product_kernel(ProductArgs a, uint32_t across, uint32_t down) {
+  typedef Shape<WC, WT, FC, FT, BUFFERS> S;
   extern __shared__ __align__(16) char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 31, h = lane >> 5;
@@ -86,13 +91,13 @@ __global__ __launch_bounds__(64 * WC * WT, 2) void product_kernel(ProductArgs a,
   const uint32_t high = min(kBand, down - band * kBand);
   const int t0 = (int)(band * kBand + in_band % high) * S::kTokens, c0 = (int)(in_band / high) * S::kChannels;
 
-  // rows 8 (i * waves + wave) + lane / 8 of both operands, the chunk that
+  // rows 16 (i * waves + wave) + lane / 4 of both operands, the chunk that
   // belongs where the lane writes
-  const int chunk = (lane % 8) ^ ((wave & 1) * 4 + lane / 16);
+  const int chunk = (lane % 4) ^ (lane / 16);
   global_bytes from[S::kLoads];
 #pragma unroll
   for (int i = 0; i < S::kLoads; ++i) {
-    const int row = (i * S::kWaves + wave) * 8 + lane / 8;
+    const int row = (i * S::kWaves + wave) * 16 + lane / 4;
     from[i] = (global_bytes)(row < S::kChannels
                                  ? a.w + min(c0 + row, a.channels - 1) * a.w_chan
                                  : a.x + min(t0 + row - S::kChannels, a.tokens - 1) * a.x_tok) +
@@ -105,7 +110,18 @@ __global__ __launch_bounds__(64 * WC * WT, 2) void product_kernel(ProductArgs a,
 #pragma unroll
     for (int i = 0; i < S::kLoads; ++i)
       load16_to_lds(there ? from[i] + s * kStep : (global_bytes)kZeros,
-                    to + (s & 1) * S::kBuffer + i * S::kWaves * 1024);
+                    to + (s % BUFFERS) * S::kBuffer + i * S::kWaves * 1024);
+  };
+  // waits for step s, where those up to `last` are on their way
+  auto wait_for = [&](int s, int last) {
+    last = min(last, steps - 1);
+    if (last >= s + 2)
+      wait_loads<2 * S::kLoads>();
+    else if (last == s + 1)
+      wait_loads<S::kLoads>();
+    else
+      wait_loads<0>();
+    barrier();
   };
 
   i32x16 sum[FC][FT];
@@ -116,55 +132,165 @@ __global__ __launch_bounds__(64 * WC * WT, 2) void product_kernel(ProductArgs a,
 #pragma unroll
       for (int i = 0; i < 16; ++i) sum[c][t][i] = 0;
 
-  load(0);
-  if (steps > 1) load(1);
   const int c_row = wave % WC * FC * 32 + n, t_row = S::kChannels + wave / WC * FT * 32 + n;
-#pragma unroll 1
-  for (int s = 0; s < steps; ++s) {
-    if (s + 1 < steps)
-      wait_loads<S::kLoads>();
-    else
-      wait_loads<0>();
-    barrier();
-    const char* tile = lds + (s & 1) * S::kBuffer;
+  i32x4 w[2][FC], x[2][FT];
+  auto read = [&](int s, int k) {
+    const char* tile = lds + (s % BUFFERS) * S::kBuffer;
 #pragma unroll
-    for (int k = 0; k < kStep / 32; ++k) {
-      i32x4 w[FC], x[FT];
+    for (int c = 0; c < FC; ++c) w[k][c] = *chunk_at(tile, c_row + c * 32, 2 * k + h);
 #pragma unroll
-      for (int c = 0; c < FC; ++c) w[c] = *chunk_at(tile, c_row + c * 32, 2 * k + h);
-#pragma unroll
-      for (int t = 0; t < FT; ++t) x[t] = *chunk_at(tile, t_row + t * 32, 2 * k + h);
-#pragma unroll
-      for (int c = 0; c < FC; ++c)
-#pragma unroll
-        for (int t = 0; t < FT; ++t) sum[c][t] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[c], x[t], sum[c][t], 0, 0, 0);
-    }
-    if (s + 2 < steps) {
-      barrier();
-      load(s + 2);
-    }
-  }
-
-#pragma unroll
-  for (int t = 0; t < FT; ++t) {
-    const int token = t0 + (wave / WC * FT + t) * 32 + n;
-    if (token >= a.tokens) continue;
-    const float x_scale = a.x_scale[token];
+    for (int t = 0; t < FT; ++t) x[k][t] = *chunk_at(tile, t_row + t * 32, 2 * k + h);
+    __builtin_amdgcn_sched_group_barrier(kReads, FC + FT, 0);
+  };
+  auto multiply = [&](int k) {
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int c = 0; c < FC; ++c)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int channel = c0 + (wave % WC * FC + c) * 32 + 8 * i + 4 * h;
-        if (channel >= a.channels) continue;
-        f32x4 f;
+      for (int t = 0; t < FT; ++t)
+        sum[c][t] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[k][c], x[k][t], sum[c][t], 0, 0, 0);
+    __builtin_amdgcn_s_setprio(0);
+    __builtin_amdgcn_sched_group_barrier(kProducts, FC * FT, 0);
+  };
+  // scales and biases, for the end: 64 values a load
+  float* scales = (float*)(lds + S::kTiles);
+  for (int i = wave; i < (S::kTokens + 2 * S::kChannels) / 64; i += S::kWaves) {
+    const int first = i * 64, of = first < S::kTokens ? 0 : first < S::kTokens + S::kChannels ? 1 : 2;
+    const float* base = of == 0 ? a.x_scale : of == 1 ? a.w_scale : a.bias ? a.bias : a.w_scale;
+    const int at = of == 0 ? min(t0 + first + lane, a.tokens - 1)
+                           : min(c0 + (first - S::kTokens) % S::kChannels + lane, a.channels - 1);
+    load4_to_lds((global_ints)(base + at), lds_offset(scales + first));
+  }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int at = min(channel + e, a.channels - 1);
-          f[e] = (float)sum[c][t][4 * i + e] * x_scale * a.w_scale[at];
-          if (a.bias) f[e] += a.bias[at];
-        }
-        store4<T>(a, token, channel, f);
+  for (int s = 0; s < BUFFERS; ++s)
+    if (s < steps) load(s);
+  wait_for(0, BUFFERS - 1);
+  read(0, 0);
+  // Half of a step's operands are read while the other half is multiplied, and
+  // the barrier stands between: behind it the step before is read by all waves
+  // (its buffer is filled again) and the next one is there, and there are
+  // products left to do while its first operands are on their way.
+#pragma unroll 1
+  for (int s = 0; s < steps; ++s) {
+    read(s, 1);
+    multiply(0);
+    if (s + 1 < steps) {
+      wait_for(s + 1, s + BUFFERS - 1);
+      if (s + BUFFERS < steps) load(s + BUFFERS);
+      read(s + 1, 0);
+    }
+    multiply(1);
+  }
+
+  // The sums go through LDS, WT * 32 tokens at a time, so that a thread has
+  // eight neighbouring channels and a wave whole rows: rows of 32-bit sums, 16
+  // bytes apart beyond their own.
+  constexpr int kAcross = S::kChannels / 8, kDown = S::kThreads / kAcross, kPitch = S::kPitch;
+  const int col = (int)threadIdx.x % kAcross * 8, channel = c0 + col;
+  float w_scale[8], bias[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    w_scale[e] = scales[S::kTokens + col + e];
+    bias[e] = scales[S::kTokens + S::kChannels + col + e];
+  }
+#pragma unroll
+  for (int t = 0; t < FT; ++t) {
+    barrier();
+    char* row = lds + (wave / WC * 32 + n) * kPitch + (wave % WC * FC * 32 + 4 * h) * 4;
+#pragma unroll
+    for (int c = 0; c < FC; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *(i32x4*)(row + (c * 32 + 8 * i) * 4) =
+            i32x4{sum[c][t][4 * i], sum[c][t][4 * i + 1], sum[c][t][4 * i + 2], sum[c][t][4 * i + 3]};
+    barrier();
+#pragma unroll 4
+    for (int r = (int)threadIdx.x / kAcross; r < WT * 32; r += kDown) {
+      const int place = (r / 32 * FT + t) * 32 + r % 32, token = t0 + place;
+      if (token >= a.tokens || channel >= a.channels) continue;
+      const float x_scale = scales[place];
+      const i32x4 lo = *(const i32x4*)(lds + r * kPitch + col * 4), hi = *(const i32x4*)(lds + r * kPitch + col * 4 + 16);
+      float f[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        f[e] = (float)(e < 4 ? lo[e % 4] : hi[e % 4]) * x_scale * w_scale[e];
+        if (a.bias) f[e] += bias[e];
       }
+      store<T, 8>(a.out + token * a.out_tok, channel, a.channels, f);
+    }
+  }
+}
+
+// Few results: a workgroup has CT * 16 channels and TT * 16 tokens, and its
+// waves have k in turn, 256 elements at a time, from memory straight to the
+// registers that the matrix instructions take them from; their sums are added
+// in LDS.  (Lane l of a wave reads 64 neighbouring bytes of row l % 16: a
+// product takes 16 of them, so its slots stand for elements 64 (l / 16) + 16 j
+// .. of both operands.)
+constexpr int kDirectWaves = 8;
+constexpr int kDirectStep = 256;
+
+template <class T, int CT, int TT>
+__global__ __launch_bounds__(64 * kDirectWaves) void product_direct_kernel(ProductArgs a, uint32_t across) {
+  constexpr int kPitch = CT * 64 + 16, kWave = TT * 16 * kPitch;
+  extern __shared__ __align__(16) char lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 15, g = lane >> 4;
+  const int t0 = (int)(blockIdx.x / across) * TT * 16, c0 = (int)(blockIdx.x % across) * CT * 16;
+  const char *w_from[CT], *x_from[TT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c) w_from[c] = a.w + min(c0 + c * 16 + n, a.channels - 1) * a.w_chan;
+#pragma unroll
+  for (int t = 0; t < TT; ++t) x_from[t] = a.x + min(t0 + t * 16 + n, a.tokens - 1) * a.x_tok;
+  i32x4 sum[CT][TT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c)
+#pragma unroll
+    for (int t = 0; t < TT; ++t) sum[c][t] = i32x4{0, 0, 0, 0};
+  auto step = [&](int k0, auto whole) {
+    i32x4 w[CT][4], x[TT][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int k = k0 + g * 64 + j * 16;
+      const bool there = whole.value || k < a.dim;
+#pragma unroll
+      for (int c = 0; c < CT; ++c) w[c][j] = *(const i32x4*)(there ? w_from[c] + k : (const char*)kZeros);
+#pragma unroll
+      for (int t = 0; t < TT; ++t) x[t][j] = *(const i32x4*)(there ? x_from[t] + k : (const char*)kZeros);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+          sum[c][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[c][j], x[t][j], sum[c][t], 0, 0, 0);
+  };
+  int k0 = wave * kDirectStep;
+  for (; k0 + kDirectStep <= a.dim; k0 += kDirectWaves * kDirectStep) step(k0, std::true_type());
+  if (k0 < a.dim) step(k0, std::false_type());
+#pragma unroll
+  for (int c = 0; c < CT; ++c)
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+      *(i32x4*)(lds + wave * kWave + (t * 16 + n) * kPitch + c * 64 + g * 16) = sum[c][t];
+  __syncthreads();
+  for (int i = threadIdx.x; i < TT * 16 * CT * 4; i += 64 * kDirectWaves) {
+    const int token = t0 + i / (CT * 4), channel = c0 + i % (CT * 4) * 4;
+    if (token >= a.tokens || channel >= a.channels) continue;
+    i32x4 all = {0, 0, 0, 0};
+#pragma unroll
+    for (int v = 0; v < kDirectWaves; ++v)
+      all += *(const i32x4*)(lds + v * kWave + i / (CT * 4) * kPitch + i % (CT * 4) * 16);
+    const float x_scale = a.x_scale[token];
+    float f[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int at = min(channel + e, a.channels - 1);
+      f[e] = (float)all[e] * x_scale * a.w_scale[at];
+      if (a.bias) f[e] += a.bias[at];
+    }
+    store<T, 4>(a.out + token * a.out_tok, channel, a.channels, f);
   }
 }
 
@@ -184,21 +310,55 @@ hipError_t allow_lds(int bytes) {
   return hipSuccess;
 }
 
-template <class T, int WC, int WT, int FC, int FT>
+template <class T, int WC, int WT, int FC, int FT, int BUFFERS>
 hipError_t launch_tiles(const ProductArgs& a, hipStream_t st) {
-  typedef Shape<WC, WT, FC, FT> S;
-  const hipError_t e = allow_lds<product_kernel<T, WC, WT, FC, FT>>(S::kBytes);
+  typedef Shape<WC, WT, FC, FT, BUFFERS> S;
+  const hipError_t e = allow_lds<product_kernel<T, WC, WT, FC, FT, BUFFERS>>(S::kBytes);
   if (e != hipSuccess) return e;
   const uint32_t across = (uint32_t)((a.channels + S::kChannels - 1) / S::kChannels);
   const uint32_t down = (uint32_t)((a.tokens + S::kTokens - 1) / S::kTokens);
-  product_kernel<T, WC, WT, FC, FT><<<across * down, S::kThreads, S::kBytes, st>>>(a, across, down);
+  product_kernel<T, WC, WT, FC, FT, BUFFERS><<<across * down, S::kThreads, S::kBytes, st>>>(a, across, down);
   return hipGetLastError();
 }
 
+template <class T, int CT, int TT>
+hipError_t launch_direct(const ProductArgs& a, hipStream_t st) {
+  constexpr int bytes = kDirectWaves * TT * 16 * (CT * 64 + 16);
+  const hipError_t e = allow_lds<product_direct_kernel<T, CT, TT>>(bytes);
+  if (e != hipSuccess) return e;
+  const uint32_t across = (uint32_t)((a.channels + CT * 16 - 1) / (CT * 16));
+  const uint32_t down = (uint32_t)((a.tokens + TT * 16 - 1) / (TT * 16));
+  product_direct_kernel<T, CT, TT><<<across * down, 64 * kDirectWaves, bytes, st>>>(a, across);
+  return hipGetLastError();
+}
+
+// Which kernel, by what they take (bfloat16 results, k = 4,096, us):
+//   tokens x channels    direct 16 x 16   direct 64 x 32   tiles of 64   128   256
+//        8 x  8,192            8.6              8.7            15.8     25.8   56
+//       64 x  8,192           31.6             14.1            16.2     26.6   57
+//      128 x  8,192           60.6             25.2            16.5     27.8   59
+//      512 x  4,096          115               46              19.3     27.9   61
+//      256 x 16,384          274               99              41.7     29.2   62
+//    1,024 x  8,192          465              179              75.8     47.0   63
+//    2,048 x  8,192                                                    102.8   76
+// The direct kernels are taken as long as one round of workgroups does it (up
+// to 16 tokens, which weights bound, always); of the tiles those that are done
+// first, by the time of a step of k where a compute unit has one workgroup, or
+// several.
 template <class T>
 hipError_t launch(const ProductArgs& a, hipStream_t st) {
-  if ((int64_t)a.tokens * a.channels >= 200 * 65536) return launch_tiles<T, 2, 4, 4, 2>(a, st);
-  return launch_tiles<T, 2, 2, 2, 2>(a, st);
+  auto count = [&](int tokens, int channels) {
+    return (int64_t)((a.tokens + tokens - 1) / tokens) * ((a.channels + channels - 1) / channels);
+  };
+  if (a.tokens <= 16) return launch_direct<T, 1, 1>(a, st);
+  if (count(64, 32) <= kComputeUnits) return launch_direct<T, 2, 4>(a, st);
+  auto step_ns = [&](int tile, int alone, int each) {
+    const int64_t rounds = (count(tile, tile) + kComputeUnits - 1) / kComputeUnits;
+    return rounds * each > alone ? rounds * each : alone;
+  };
+  const int64_t t64 = step_ns(64, 235, 150), t128 = step_ns(128, 400, 365), t256 = step_ns(256, 900, 900);
+  if (t64 <= t128 && t64 <= t256) return launch_tiles<T, 2, 2, 1, 1, 4>(a, st);
+  return t128 <= t256 ? launch_tiles<T, 2, 2, 2, 2, 4>(a, st) : launch_tiles<T, 4, 2, 2, 4, 4>(a, st);
 }
 
 }  // namespace
