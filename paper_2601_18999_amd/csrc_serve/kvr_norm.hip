@@ -2,9 +2,9 @@
 // (kvr_block_norm; kvr.h has the formulas).
 //
 // A row is held in registers (32-bit) from its one reading to its one writing,
-// by WAVES waves, V times eight elements a lane; the two means and the largest
-// magnitude are sums and maxima over those lanes.  Memory bounds: every input
-// is read once and every output written once.
+// V times eight elements a lane; the two means and the largest magnitude are
+// sums and maxima over its lanes, and those of its waves over LDS.  Memory
+// bounds long calls: every input is read once and every output written once.
 #include <hip/hip_runtime.h>
 
 #include "kvr_layer.h"
@@ -12,27 +12,67 @@
 namespace kvr {
 namespace {
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kMostWaves = 16;       // of a row
+constexpr int kMostBlocks = 1 << 20; // of a launch; they take the rows in turn
+
 template <class T>
 struct Eight {
   T e[8];
 };
 
-// Eight elements from `at` on, as many as there are of `n` (behind them: 0).
-// Rows start on any element, so the loads may be unaligned, which the memory
-// instructions allow.
-template <class T>
-__device__ __forceinline__ void load8(const char* row, int at, int n, float (&f)[8]) {
-  const T* p = reinterpret_cast<const T*>(row) + at;
-  if (at + 8 <= n) {
-    Eight<T> x;
-    __builtin_memcpy(&x, p, sizeof(x));
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = (float)x.e[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = at + i < n ? (float)p[i] : 0.0f;
-  }
+// 16 bytes from any address on (rows start on any element; the memory
+// instructions allow it).
+__device__ __forceinline__ u32x4 load16(const char* p) {
+  u32x4 x;
+  __builtin_memcpy(&x, p, sizeof(x));
+  return x;
 }
+
+// Eight elements of a row of n from `at` on, as they stand in memory; 0 behind
+// its end.
+template <class T>
+struct Raw {
+  static constexpr int kLoads = sizeof(T) / 2, kEach = 16 / sizeof(T);  // elements of a load
+  u32x4 x[kLoads];
+
+  __device__ __forceinline__ void load(const char* row, int at, int n) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) x[i] = u32x4{0, 0, 0, 0};
+    if (n % 8 == 0) {
+      if (at < n) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) x[i] = load16(row + (at + i * kEach) * (int)sizeof(T));
+      }
+    } else if (n >= 8) {
+      // those that would end behind the row end with it, and are shifted
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int want = at + i * kEach, from = min(want, n - kEach), by = (want - from) * (int)sizeof(T) * 8;
+        x[i] = load16(row + from * (int)sizeof(T));
+        if (by) {
+          uint64_t lo = x[i][0] | (uint64_t)x[i][1] << 32, hi = x[i][2] | (uint64_t)x[i][3] << 32;
+          lo = by >= 128 ? 0 : by >= 64 ? hi >> (by - 64) : lo >> by | hi << (64 - by);
+          hi = by >= 64 ? 0 : hi >> by;
+          x[i] = u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+        }
+      }
+    } else if (at == 0) {
+      Eight<T> e;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) e.e[i] = i < n ? reinterpret_cast<const T*>(row)[i] : (T)0.0f;
+      __builtin_memcpy(x, &e, sizeof(e));
+    }
+  }
+
+  __device__ __forceinline__ void widen(float (&f)[8]) const {
+    Eight<T> y;
+    __builtin_memcpy(&y, x, sizeof(y));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = (float)y.e[i];
+  }
+};
 
 template <class T>
 __device__ __forceinline__ void store8(char* row, int at, int n, const float (&f)[8]) {
@@ -42,40 +82,51 @@ __device__ __forceinline__ void store8(char* row, int at, int n, const float (&f
 #pragma unroll
     for (int i = 0; i < 8; ++i) x.e[i] = (T)f[i];
     __builtin_memcpy(p, &x, sizeof(x));
-  } else {
+  } else if (at < n) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (at + i < n) p[i] = (T)f[i];
   }
 }
 
+// Over the lanes of a wave: within rows of 16 by DPP, then across them.
+template <class Op>
+__device__ __forceinline__ uint32_t over_wave(uint32_t x, Op op) {
+  x = op(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xb1, 0xf, 0xf, false));   // lane ^ 1
+  x = op(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4e, 0xf, 0xf, false));   // lane ^ 2
+  x = op(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xf, 0xf, false));  // mirrored in 8
+  x = op(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xf, 0xf, false));  // mirrored in 16
+  const auto s = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = op(s[0], s[1]);
+  const auto t = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return op(t[0], t[1]);
+}
+
 __device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-  for (int m = 32; m; m >>= 1) x += __shfl_xor(x, m);
-  return x;
+  return __uint_as_float(over_wave(__float_as_uint(x), [](uint32_t a, uint32_t b) {
+    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+  }));
 }
 
 __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
-#pragma unroll
-  for (int m = 32; m; m >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, m));
-  return x;
+  return over_wave(x, [](uint32_t a, uint32_t b) { return max(a, b); });
 }
 
-constexpr int kMostBlocks = 1 << 20;  // of a launch; they take the rows in turn
-
-constexpr int row_threads(int waves) { return waves < 4 ? 256 : 64 * waves; }
-
-template <class T, int WAVES, int V>
-__global__ __launch_bounds__(row_threads(WAVES)) void norm_kernel(NormArgs a) {
-  constexpr int kRows = row_threads(WAVES) / (64 * WAVES);  // of a workgroup
-  __shared__ float sums[2][kRows][WAVES];
-  __shared__ uint32_t tops[kRows][WAVES];
+// One row for each wave (SINGLE: four rows a workgroup), or for a workgroup.
+// T: the type of x, R: of the residual.  Several rows a compute unit are on
+// their way at once, which takes few registers for each: with 180 instead of
+// 64 (eight waves of a row of 4,096, V = 1) 9,216 rows took 144 us.
+template <class T, class R, bool SINGLE, int V>
+__global__ __launch_bounds__(SINGLE ? 256 : 64 * kMostWaves, V == 1 ? 8 : 4) void norm_kernel(NormArgs a) {
+  __shared__ float sums[2][kMostWaves];
+  __shared__ uint32_t tops[kMostWaves];
   const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-  const int mine = wave / WAVES, part = wave % WAVES;
-  const int at0 = (part * 64 + lane) * 8;
-  constexpr int kNext = WAVES * 512;
+  const int waves = SINGLE ? 1 : (int)blockDim.x / 64;
+  const int at0 = (SINGLE ? lane : (int)threadIdx.x) * 8, next = waves * 512;
+  const int64_t first = SINGLE ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
+  const int64_t step = SINGLE ? (int64_t)gridDim.x * 4 : gridDim.x;
 
-  // the sum of f^2 over the row
+  // the mean of f^2 over the row
   auto mean_square = [&](const float(&f)[V][8], int which) {
     float s = 0.0f;
 #pragma unroll
@@ -83,158 +134,140 @@ __global__ __launch_bounds__(row_threads(WAVES)) void norm_kernel(NormArgs a) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) s = __builtin_fmaf(f[v][i], f[v][i], s);
     s = wave_sum(s);
-    if constexpr (WAVES > 1) {
-      if (lane == 0) sums[which][mine][part] = s;
+    if (!SINGLE) {
+      if (lane == 0) sums[which][wave] = s;
       __syncthreads();
-      s = 0.0f;
-#pragma unroll
-      for (int w = 0; w < WAVES; ++w) s += sums[which][mine][w];
+      s = wave_sum(lane < waves ? sums[which][lane % kMostWaves] : 0.0f);
     }
     return s * a.inv_dim;
   };
-
-  for (int64_t row = (int64_t)blockIdx.x * kRows + mine; row < a.tokens; row += (int64_t)gridDim.x * kRows) {
-    float f[V][8];
-    const char* x = a.x + row * a.x_tok;
+  auto weigh = [&](float(&f)[V][8], const char* weight, int which) {
+    Raw<T> raw[V];
+    if (V == 1) raw[0].load(weight, at0, a.dim);
+    const float by = __builtin_amdgcn_rsqf(mean_square(f, which) + a.eps);
 #pragma unroll
-    for (int v = 0; v < V; ++v) load8<T>(x, at0 + v * kNext, a.dim, f[v]);
-    if (a.after) {
-      const float by = __builtin_amdgcn_rsqf(mean_square(f, 0) + a.eps);
+    for (int v = 0; v < V; ++v) {
+      if (V > 1) raw[v].load(weight, at0 + v * next, a.dim);
+      float w[8];
+      raw[v].widen(w);
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        float w[8];
-        load8<T>(a.after, at0 + v * kNext, a.dim, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[v][i] = f[v][i] * by * w[i];
-      }
+      for (int i = 0; i < 8; ++i) f[v][i] = f[v][i] * by * w[i];
     }
+  };
+
+#pragma unroll 1
+  for (int64_t row = first; row < a.tokens; row += step) {
+    // what comes from far is on its way before the first sum is waited for
+    Raw<T> raw_x[V], raw_gate[V];
+    Raw<R> raw_res[V];
+    const char *gate = a.gate + row * a.gate_tok, *res = a.residual + row * a.res_tok;
+#pragma unroll
+    for (int v = 0; v < V; ++v) raw_x[v].load(a.x + row * a.x_tok, at0 + v * next, a.dim);
+    if (V == 1 && a.gate) raw_gate[0].load(gate, at0, a.dim);
+    if (V == 1 && a.residual) raw_res[0].load(res, at0, a.dim);
+    float f[V][8];
+#pragma unroll
+    for (int v = 0; v < V; ++v) raw_x[v].widen(f[v]);
+    if (a.after) weigh(f, a.after, 0);
     if (a.gate) {
-      const char* gate = a.gate + row * a.gate_tok;
 #pragma unroll
       for (int v = 0; v < V; ++v) {
+        if (V > 1) raw_gate[v].load(gate, at0 + v * next, a.dim);
         float g[8];
-        load8<T>(gate, at0 + v * kNext, a.dim, g);
+        raw_gate[v].widen(g);
+        if (a.activation != KVR_ACT_NONE) {
+          // (an error of the exponent's product is one of |g| half steps)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (a.activation != KVR_ACT_NONE)
-            g[i] = (a.activation == KVR_ACT_SILU ? g[i] : 1.0f) / (1.0f + expf(-g[i]));
-          f[v][i] *= g[i];
+          for (int i = 0; i < 8; ++i)
+            g[i] = (a.activation == KVR_ACT_SILU ? g[i] : 1.0f) *
+                   __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g[i] * -1.44269504088896340736f));
         }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[v][i] *= g[i];
       }
     }
     if (a.residual) {
-      const char* from = a.residual + row * a.res_tok;
-      char* to = a.residual_out + row * a.res_out_tok;
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        const int at = at0 + v * kNext;
+        const int at = at0 + v * next;
+        if (V > 1) raw_res[v].load(res, at, a.dim);
         float r[8];
-        if (a.res32)
-          load8<float>(from, at, a.dim, r);
-        else
-          load8<T>(from, at, a.dim, r);
+        raw_res[v].widen(r);
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[v][i] = __builtin_fmaf(a.residual_scale, f[v][i], r[i]);
-        if (at < a.dim) {
-          if (a.res32)
-            store8<float>(to, at, a.dim, f[v]);
-          else
-            store8<T>(to, at, a.dim, f[v]);
-        }
+        store8<R>(a.residual_out + row * a.res_out_tok, at, a.dim, f[v]);
       }
     }
-    if (a.before) {
-      const float by = __builtin_amdgcn_rsqf(mean_square(f, 1) + a.eps);
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        float w[8];
-        load8<T>(a.before, at0 + v * kNext, a.dim, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[v][i] = f[v][i] * by * w[i];
-      }
-    }
+    if (a.before) weigh(f, a.before, 1);
     char* out = a.out + row * a.out_tok;
     if (!a.int8) {
 #pragma unroll
+      for (int v = 0; v < V; ++v) store8<T>(out, at0 + v * next, a.dim, f[v]);
+    } else {
+      // The largest magnitude by its bits: NaN is above infinity, and that above the rest.
+      uint32_t top = 0;
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(f[v][i]) & 0x7fffffffu);
+      top = wave_max(top);
+      if (!SINGLE) {
+        if (lane == 0) tops[wave] = top;
+        __syncthreads();
+        top = wave_max(lane < waves ? tops[lane % kMostWaves] : 0);
+      }
+      const float largest = __uint_as_float(top);
+      const bool usual = top < 0x7f800000u && largest >= 0x1p-100f;
+      const float by = usual ? 127.0f / largest : 0.0f;
+      if (at0 == 0)
+        a.out_scale[row] = usual ? largest / 127.0f : top < 0x7f800000u ? 0.0f : __uint_as_float(0x7fc00000u);
+#pragma unroll
       for (int v = 0; v < V; ++v) {
-        const int at = at0 + v * kNext;
-        if (at < a.dim) store8<T>(out, at, a.dim, f[v]);
-      }
-      if (WAVES > 1) __syncthreads();
-      continue;
-    }
-    // The largest magnitude by its bits: NaN is above infinity, and that above the rest.
-    uint32_t top = 0;
+        const int at = at0 + v * next;
+        Eight<int8_t> q;
 #pragma unroll
-    for (int v = 0; v < V; ++v)
+        for (int i = 0; i < 8; ++i) q.e[i] = usual ? (int8_t)(int)__builtin_rintf(f[v][i] * by) : 0;
+        if (at + 8 <= a.dim) {
+          __builtin_memcpy(out + at, &q, 8);
+        } else if (at < a.dim) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(f[v][i]) & 0x7fffffffu);
-    top = wave_max(top);
-    if constexpr (WAVES > 1) {
-      if (lane == 0) tops[mine][part] = top;
-      __syncthreads();
-#pragma unroll
-      for (int w = 0; w < WAVES; ++w) top = max(top, tops[mine][w]);
-    }
-    const float largest = __uint_as_float(top);
-    const bool usual = top < 0x7f800000u && largest >= 0x1p-100f;
-    const float by = usual ? 127.0f / largest : 0.0f;
-    if (part == 0 && lane == 0)
-      a.out_scale[row] = usual ? largest / 127.0f : top < 0x7f800000u ? 0.0f : __uint_as_float(0x7fc00000u);
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int at = at0 + v * kNext;
-      if (at >= a.dim) continue;
-      Eight<int8_t> q;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) q.e[i] = usual ? (int8_t)(int)__builtin_rintf(f[v][i] * by) : 0;
-      if (at + 8 <= a.dim) {
-        __builtin_memcpy(out + at, &q, 8);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (at + i < a.dim) out[at + i] = (char)q.e[i];
+          for (int i = 0; i < 8; ++i)
+            if (at + i < a.dim) out[at + i] = (char)q.e[i];
+        }
       }
     }
-    if (WAVES > 1) __syncthreads();  // before the next row's sums
+    if (!SINGLE) __syncthreads();  // before the next row's sums
   }
 }
 
-template <class T, int WAVES, int V>
+template <class T, class R, bool SINGLE, int V>
 void launch(const NormArgs& a, hipStream_t st) {
-  constexpr int rows = row_threads(WAVES) / (64 * WAVES);
-  const int64_t groups = ((int64_t)a.tokens + rows - 1) / rows;
-  const uint32_t blocks = (uint32_t)(groups < kMostBlocks ? groups : kMostBlocks);
-  norm_kernel<T, WAVES, V><<<blocks, row_threads(WAVES), 0, st>>>(a);
+  const int64_t rows = SINGLE ? ((int64_t)a.tokens + 3) / 4 : a.tokens;
+  const int threads = SINGLE ? 256 : (a.dim + 512 * V - 1) / (512 * V) * 64;
+  norm_kernel<T, R, SINGLE, V><<<(uint32_t)(rows < kMostBlocks ? rows : kMostBlocks), threads, 0, st>>>(a);
 }
 
-template <class T>
+template <class T, class R>
 void launch_typed(const NormArgs& a, hipStream_t st) {
   if (a.dim <= 512)
-    launch<T, 1, 1>(a, st);
-  else if (a.dim <= 1024)
-    launch<T, 1, 2>(a, st);
-  else if (a.dim <= 2048)
-    launch<T, 4, 1>(a, st);
-  else if (a.dim <= 4096)
-    launch<T, 4, 2>(a, st);
-  else if (a.dim <= 8192)
-    launch<T, 4, 4>(a, st);
-  else if (a.dim <= 16384)
-    launch<T, 16, 2>(a, st);
-  else if (a.dim <= 32768)
-    launch<T, 16, 4>(a, st);
+    launch<T, R, true, 1>(a, st);
+  else if (a.dim <= 512 * kMostWaves)
+    launch<T, R, false, 1>(a, st);
+  else if (a.dim <= 1024 * kMostWaves)
+    launch<T, R, false, 2>(a, st);
+  else if (a.dim <= 2048 * kMostWaves)
+    launch<T, R, false, 4>(a, st);
   else
-    launch<T, 16, 8>(a, st);
+    launch<T, R, false, 8>(a, st);
 }
 
 }  // namespace
 
 hipError_t launch_norm(const NormArgs& a, bool fp16, hipStream_t st) {
   if (fp16)
-    launch_typed<_Float16>(a, st);
+    a.res32 ? launch_typed<_Float16, float>(a, st) : launch_typed<_Float16, _Float16>(a, st);
   else
-    launch_typed<__bf16>(a, st);
+    a.res32 ? launch_typed<__bf16, float>(a, st) : launch_typed<__bf16, __bf16>(a, st);
   return hipGetLastError();
 }
 
