@@ -34,8 +34,11 @@ struct ProductArgs {
 };
 
 // ---- linear attention ----
-// Requests of up to so many tokens take the recurrent form.
+// Requests of up to so many tokens take the recurrent form; where a request has
+// more than kManyTokens on average, all take the chunked one (for which a launch
+// less is done).
 constexpr int kFewTokens = 4;
+constexpr int kManyTokens = 32;
 // Workgroups of the chunked form that the device holds.
 constexpr int kLinearSlots = 2 * kComputeUnits;
 
@@ -68,6 +71,7 @@ struct LinearArgs {
   Divisor kv_div;                                                     // by kv_heads
   int32_t tokens, requests, heads, kv_heads, share, dim, slots;
   int32_t segment, segment_cap;
+  int32_t few;  // requests of up to so many tokens take the recurrent form (-1: none)
   float scale;
 };
 

@@ -266,6 +266,7 @@ kvr_status kvr_linear_attention(const kvr_linear* l, void* d_workspace, size_t b
   a.slots = l->num_slots;
   a.segment = o.segment;
   a.segment_cap = o.segment_cap;
+  a.few = l->d_row_start && l->num_tokens > (int64_t)kvr::kManyTokens * l->num_requests ? -1 : kvr::kFewTokens;
   a.scale = l->scale;
   const hipError_t e = kvr::launch_linear(a, l->dtype == KVR_FP16, static_cast<hipStream_t>(hip_stream));
   return e == hipSuccess ? KVR_OK : hip_failed(e, "linear attention kernels launch");

@@ -58,47 +58,59 @@ __device__ void fill_nan(const LinearArgs& a, int row0, int rows, int head, int 
   }
 }
 
-// Checks row_start and lists the segments: one workgroup.
+// Checks row_start and lists the segments, the longest first (the workgroups
+// that start last then have little to do): one workgroup.
 __global__ __launch_bounds__(kThreads) void linear_plan_kernel(LinearArgs a) {
-  __shared__ uint64_t ahead[2][kThreads];
+  constexpr int kKinds = 64;  // by chunks, the last one all longer ones
+  __shared__ int place[kKinds], slots;
   const int tid = threadIdx.x;
+  if (tid < kKinds) place[tid] = 0;
+  if (tid == 0) slots = 0;
+  __syncthreads();
+  auto kind = [&](int rows) { return kKinds - 1 - min((rows + kChunk - 1) / kChunk, kKinds - 1); };
   int bad = 0;
-  uint64_t base = 0;  // segments of the requests before, and (above 32 bits) slots
-  for (int r0 = 0; r0 < a.requests; r0 += kThreads) {
-    const int r = r0 + tid;
-    int from = 0, rows = 0, parts = 0;
-    if (r < a.requests) {
-      from = a.row_start[r];
-      const int to = a.row_start[r + 1];
-      if (from < 0 || to < from || to > a.tokens) bad = 1;
-      rows = to - from;
-      parts = rows > 0 ? (rows - 1) / a.segment + 1 : 1;
+  // A request's segments: all but the last are full.  Those of a few tokens
+  // are not listed (linear_steps_kernel takes them).
+  auto each = [&](auto found) {
+    for (int r = tid; r < a.requests; r += kThreads) {
+      const int from = a.row_start[r], to = a.row_start[r + 1];
+      if (from < 0 || to < from || to > a.tokens)
+        bad = 1;
+      else if (a.few < 0 || to - from > a.few)
+        found(r, from, to - from, to > from ? (to - from - 1) / a.segment + 1 : 1);
     }
-    // (of valid lengths there are no more segments than the list has room for)
-    if (__syncthreads_or(bad)) break;
-    const uint64_t mine = (uint64_t)(parts > 1 ? parts : 0) << 32 | (uint32_t)parts;
-    uint64_t sum = mine;
-    ahead[0][tid] = sum;
-    __syncthreads();
-    int buffer = 0;
-    for (int d = 1; d < kThreads; d <<= 1) {
-      if (tid >= d) sum += ahead[buffer][tid - d];
-      buffer ^= 1;
-      ahead[buffer][tid] = sum;
-      __syncthreads();
-    }
-    const uint64_t at = base + sum - mine;
-    for (int i = 0; i < parts; ++i)
-      a.segments[(uint32_t)at + i] = {r,     from + i * a.segment, min(a.segment, rows - i * a.segment), i,
-                                      parts, (int)(at >> 32),      0,                                    0};
-    base += ahead[buffer][kThreads - 1];
-    __syncthreads();
-  }
+  };
+  each([&](int, int, int rows, int parts) {
+    if (parts > 1) atomicAdd(&place[kind(a.segment)], parts - 1);
+    atomicAdd(&place[kind(rows - (parts - 1) * a.segment)], 1);
+  });
   bad = __syncthreads_or(bad);
-  if (tid == 0) {
-    *a.hdr = {(int)(uint32_t)base, bad};
+  int all = 0;
+  if (tid < kKinds) {
+    const int mine = place[tid];
+    int sum = mine;
+#pragma unroll
+    for (int d = 1; d < kKinds; d <<= 1) {
+      const int x = __shfl_up(sum, d);
+      if (tid >= d) sum += x;
+    }
+    place[tid] = sum - mine;
+    all = sum;
+  }
+  __syncthreads();
+  if (tid == kKinds - 1) {
+    *a.hdr = {all, bad};
     if (bad && a.status) atomicOr(a.status, (uint32_t)KVR_DEV_BAD_LENGTH);
   }
+  if (bad) return;
+  each([&](int r, int from, int rows, int parts) {
+    const int slot = parts > 1 ? atomicAdd(&slots, parts) : 0;
+    const int full = parts > 1 ? atomicAdd(&place[kind(a.segment)], parts - 1) : 0;
+    for (int i = 0; i < parts - 1; ++i)
+      a.segments[full + i] = {r, from + i * a.segment, a.segment, i, parts, slot, 0, 0};
+    const int rest = rows - (parts - 1) * a.segment;
+    a.segments[atomicAdd(&place[kind(rest)], 1)] = {r, from + rows - rest, rest, parts - 1, parts, slot, 0, 0};
+  });
 }
 
 // The recurrent form: one workgroup for a request's key head, which holds the
@@ -120,7 +132,7 @@ __global__ __launch_bounds__(kThreads) void linear_steps_kernel(LinearArgs a) {
     }
     row0 = a.row_start[at];
     rows = a.row_start[at + 1] - row0;
-    if (rows > kFewTokens) return;
+    if (rows > a.few) return;
   }
   int read, write;
   if (!slots_fit(a, (int)at, read, write)) {
@@ -185,20 +197,29 @@ __global__ __launch_bounds__(kThreads) void linear_steps_kernel(LinearArgs a) {
 // ---- the chunked form ----
 
 // Numbers of 32 bits as sums of bfloat16 ones, which the matrix units multiply
-// exactly: two hold 16 bits of them (results, which are rounded to 8 or 11
-// bits), three all 24 (states).
-__device__ __forceinline__ s16x8 rounded(f32x8 x) {
-  return __builtin_bit_cast(s16x8, __builtin_convertvector(x, bf16x8));
-}
-__device__ __forceinline__ f32x8 widened(s16x8 x) {
-  return __builtin_convertvector(__builtin_bit_cast(bf16x8, x), f32x8);
+// exactly: the first takes the leading 8 bits, the second the next 8, and so
+// three hold all 24 (states); of two the second is rounded, so they hold 16
+// (results, which are rounded to 8 or 11 bits).
+__device__ __forceinline__ float leading(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+__device__ __forceinline__ int packed(float x, float y) {  // their leading halves
+  return (int)__builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
 }
 template <int N>
 __device__ __forceinline__ void split(f32x8 x, s16x8 (&part)[N]) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    part[i] = rounded(x);
-    if (i + 1 < N) x -= widened(part[i]);
+  for (int k = 0; k < N; ++k) {
+    if (N == 2 && k == 1) {
+      part[k] = __builtin_bit_cast(s16x8, __builtin_convertvector(x, bf16x8));
+    } else {
+      i32x4 y;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = packed(x[2 * i], x[2 * i + 1]);
+      part[k] = __builtin_bit_cast(s16x8, y);
+    }
+    if (k + 1 < N) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] -= leading(x[i]);
+    }
   }
 }
 __device__ __forceinline__ f32x16 multiply(s16x8 a, s16x8 b, f32x16 c) {
@@ -215,7 +236,9 @@ struct OfBf16 {
   static constexpr int kParts = 1;
   // the sign bits of a pair's infinities and NaN
   static __device__ __forceinline__ uint32_t odd(uint32_t x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
-  static __device__ __forceinline__ f32x8 wide(s16x8 x) { return widened(x); }
+  static __device__ __forceinline__ f32x8 wide(s16x8 x) {
+    return __builtin_convertvector(__builtin_bit_cast(bf16x8, x), f32x8);
+  }
   static __device__ __forceinline__ void parts(s16x8 x, s16x8 (&part)[1]) { part[0] = x; }
   static __device__ __forceinline__ s16x4 narrow(f32x4 x) {
     return __builtin_bit_cast(s16x4, __builtin_convertvector(x, bf16x4));
@@ -234,89 +257,100 @@ struct OfFp16 {
   }
 };
 
-// 16-byte chunks of a row of D elements in LDS stand at chunk ^ swizzle(row):
-// the reads of one chunk of 16 rows, and those of 64 bytes of four rows, fall
-// on different banks (64 banks of 4 bytes).
+// A tile of 64 tokens in LDS: rows of D elements, 64 bytes apart beyond their
+// own, and 16 more after every four.  The reads of 16 bytes of 16 rows, and
+// those of 64 bytes of four rows, then fall on different banks (64 banks of 4
+// bytes), and every address is one of the lane and a constant.
 template <int D>
-__device__ __forceinline__ int swizzle(int row) {
-  return D == 64 ? ((row << 1) & 4) | ((row >> 2) & 3) : ((row & 3) << 2) | ((row >> 2) & 3);
-}
-template <int D>
-__device__ __forceinline__ int place(int row, int chunk) {
-  return row * 2 * D + ((chunk ^ swizzle<D>(row)) << 4);
-}
+struct Rows {
+  static constexpr int kPitch = 2 * D + 64, kBytes = kChunk * kPitch + kChunk / 4 * 16;
+  static constexpr int of(int rows) { return rows * kPitch + rows / 4 * 16; }  // multiples of four rows
+  static __device__ __forceinline__ int at(int row) { return row * kPitch + row / 4 * 16; }
+};
 
 // Queries and keys stand in LDS in the order in which a state's registers
 // hold its rows: of 16 elements the groups of four 0, 2, 1, 3.  A chunk of 16
 // bytes, which a half wave takes as an operand, then holds elements 4 h .. and
 // 8 + 4 h .. of its 16.
-template <int D>
-__device__ __forceinline__ void put(char* tile, int row, int chunk, s16x8 x) {
-  char* to = tile + (chunk & 1) * 8;
-  *(s16x4*)(to + place<D>(row, chunk & ~1)) = __builtin_shufflevector(x, x, 0, 1, 2, 3);
-  *(s16x4*)(to + place<D>(row, chunk | 1)) = __builtin_shufflevector(x, x, 4, 5, 6, 7);
-}
 
 // Eight rows' elements of one column a lane: rows 16 s + 8 h .., column 32 c +
 // lane % 32.  The transposing read: 16 lanes name four rows of 16 elements,
-// four lanes a row, and lane i of them gets column i.
+// four lanes a row, and lane i of them gets column i.  `at`: column_place.
 template <int D, bool ORDERED>
-__device__ __forceinline__ s16x8 column(const char* tile, int s, int c, int lane) {
-  const int h = lane >> 5, sl = lane & 15, g = 2 * c + ((lane >> 4) & 1);
+__device__ __forceinline__ int column_place(int lane) {
+  const int sl = lane & 15;
+  return Rows<D>::at((lane >> 5) * 8 + sl / 4) + ((lane >> 4) & 1) * 32 +
+         (ORDERED ? (sl & 1) * 16 + (sl & 2) * 4 : (sl & 3) * 8);
+}
+template <int D>
+__device__ __forceinline__ s16x8 column(const char* tile, int at, int s, int c) {
   s16x4 x[2];
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int row = s * 16 + h * 8 + j * 4 + sl / 4;
-    const char* p = ORDERED ? tile + place<D>(row, 2 * g + (sl & 1)) + (sl & 2) * 4
-                            : tile + place<D>(row, 2 * g + (sl & 2) / 2) + (sl & 1) * 8;
-    x[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(lds_char*)p);
-  }
+  for (int j = 0; j < 2; ++j)
+    x[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(
+        lds_char*)(tile + at + Rows<D>::of(16 * s + 4 * j) + c * 64));
   return __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// A lane's share of a tile of 64 tokens on its way to LDS.
+// A lane's share of a tile on its way to LDS: one 16-byte chunk of every
+// kStepRows-th row.
 template <int D>
 struct Tile {
-  static constexpr int kChunks = D / 8, kN = kChunk * kChunks / kThreads;
+  static constexpr int kChunks = D / 8, kStepRows = kThreads / kChunks, kN = kChunk / kStepRows;
   s16x8 x[kN];
 
-  // rows behind `rows`: zeros
+  // `from`: the lane's chunk of its first row; rows behind `rows`: zeros
   __device__ __forceinline__ void fetch(const char* from, int64_t stride, int rows, int thread) {
+    const int64_t next = kStepRows * stride;
+    if (rows >= kChunk) {
 #pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      const int row = (thread + i * kThreads) / kChunks, chunk = thread % kChunks;
-      x[i] = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
-      if (row < rows) x[i] = *(const s16x8*)(from + row * stride + chunk * 16);
+      for (int i = 0; i < kN; ++i, from += next) x[i] = *(const s16x8*)from;
+    } else {
+#pragma unroll
+      for (int i = 0; i < kN; ++i, from += next) {
+        x[i] = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
+        if (thread / kChunks + i * kStepRows < rows) x[i] = *(const s16x8*)from;
+      }
     }
+  }
+  static __device__ __forceinline__ const char* lane(const char* from, int64_t stride, int thread) {
+    return from + thread / kChunks * stride + thread % kChunks * 16;
   }
   template <class T>
   __device__ __forceinline__ void store_ordered(char* tile, int thread) const {
+    const int chunk = thread % kChunks;
+    char* to = tile + Rows<D>::at(thread / kChunks) + chunk / 2 * 32 + (chunk & 1) * 8;
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const int row = (thread + i * kThreads) / kChunks, chunk = thread % kChunks;
       s16x8 part[T::kParts];
       T::parts(x[i], part);
 #pragma unroll
-      for (int k = 0; k < T::kParts; ++k) put<D>(tile + k * kChunk * 2 * D, row, chunk, part[k]);
+      for (int k = 0; k < T::kParts; ++k) {
+        char* p = to + Rows<D>::of(i * kStepRows) + k * Rows<D>::kBytes;
+        *(s16x4*)p = __builtin_shufflevector(part[k], part[k], 0, 1, 2, 3);
+        *(s16x4*)(p + 16) = __builtin_shufflevector(part[k], part[k], 4, 5, 6, 7);
+      }
     }
   }
   __device__ __forceinline__ void store(char* tile, int thread) const {
+    char* to = tile + Rows<D>::at(thread / kChunks) + thread % kChunks * 16;
 #pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      const int row = (thread + i * kThreads) / kChunks, chunk = thread % kChunks;
-      *(s16x8*)(tile + place<D>(row, chunk)) = x[i];
-    }
+    for (int i = 0; i < kN; ++i) *(s16x8*)(to + Rows<D>::of(i * kStepRows)) = x[i];
   }
 };
 
+// The scores of a chunk: rows of 64, 16 bytes apart beyond their own.
+constexpr int kScorePitch = 2 * kChunk + 16, kScores = kChunk * kScorePitch;
+
 template <int D, class T, bool OUT>
 struct ChunkLds {
-  static constexpr int kTile = kChunk * 2 * D;
+  static constexpr int kTile = Rows<D>::kBytes;
   static constexpr int kKeys = T::kParts * kTile;
   static constexpr int kQueries = OUT ? T::kParts * kTile : 0;
-  static constexpr int kWeights = OUT ? 2 * kChunk * 2 * kChunk : 0;
+  static constexpr int kWeights = OUT ? 2 * kScores : 0;
   static constexpr int kBytes = kKeys + kQueries + kTile + kWeights + 2 * kChunk * 4;
 };
+static_assert(2 * ChunkLds<128, OfBf16, true>::kBytes <= 160 * 1024, "two workgroups a compute unit");
 
 // One workgroup for a segment's key head.  Wave w has 32 columns of the state
 // (D / 32 column groups; with two groups two waves hold the same) in registers:
@@ -336,13 +370,16 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
   float* power = left + kChunk;                   // d^(i + 1)
   int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = wave % kGroups, rw = wave / kGroups;
-  if (a.hdr->rejected) return;  // (linear_steps_kernel writes the results)
   const uint32_t at = divide(blockIdx.x, a.kv_div);
-  if ((int)at >= a.hdr->segments) return;
   const int head = (int)(blockIdx.x - at * a.kv_div.d);
+  if (a.hdr->rejected) {  // (with few >= 0 linear_steps_kernel writes the results)
+    if (OUT && a.few < 0)
+      for (int t = (int)at; t < a.tokens; t += a.segment_cap) fill_nan<typename T::Type>(a, t, 1, head, D);
+    return;
+  }
+  if ((int)at >= a.hdr->segments) return;
   const Segment seg = a.segments[at];
   const bool last = seg.index == seg.parts - 1;
-  if (seg.parts == 1 && seg.rows <= kFewTokens) return;
   if (!OUT && last) return;
   int read, write;
   if (!slots_fit(a, seg.request, read, write)) {
@@ -359,36 +396,47 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
     from = a.added + ((int64_t)(seg.slot + seg.index) * a.kv_heads + head) * D * D;
   else if (OUT && read >= 0)
     from = a.state + read * a.state_slot + head * a.state_head;
+  // (a place in the state of this lane's columns: its row 0 of each four)
+  const int mine = 4 * h * D + c * 32 + n;
+  if (from) {
 #pragma unroll
-  for (int t = 0; t < kGroups; ++t)
+    for (int t = 0; t < kGroups; ++t)
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      state[t][i] = from ? from[(t * 32 + 8 * (i / 4) + 4 * h + i % 4) * D + c * 32 + n] : 0.0f;
-
-  const int chunks = (seg.rows + kChunk - 1) / kChunk;
-  const char* k_from = a.k + seg.row0 * a.k_tok + head * a.k_head;
-  const char* v_from = a.v + seg.row0 * a.v_tok + head * a.v_head;
-  const int q_head0 = head * a.share;
-  const char* q_from = a.q + seg.row0 * a.q_tok + q_head0 * a.q_head;
-
-  // d^(i - j) of the scores that this lane computes: queries i = 16 wave +
-  // lane % 16, keys j = 16 t + 4 (lane / 16) + e
-  float apart[4][4];
-  if (OUT) {
+      for (int i = 0; i < 16; ++i) state[t][i] = from[mine + (t * 32 + 8 * (i / 4) + i % 4) * D];
+  } else {
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < kGroups; ++t)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int m = 16 * wave + lane % 16 - (16 * t + 4 * (lane / 16) + e);
-        apart[t][e] = m >= 0 ? decay_by(m) : -1.0f;
-      }
+      for (int i = 0; i < 16; ++i) state[t][i] = 0.0f;
   }
   if (tid < kChunk) power[tid] = decay_by(tid + 1);
+
+  const int chunks = (seg.rows + kChunk - 1) / kChunk;
+  const int q_head0 = head * a.share;
+  const char* k_from = Tile<D>::lane(a.k + seg.row0 * a.k_tok + head * a.k_head, a.k_tok, tid);
+  const char* v_from = Tile<D>::lane(a.v + seg.row0 * a.v_tok + head * a.v_head, a.v_tok, tid);
+  const char* q_from = Tile<D>::lane(a.q + seg.row0 * a.q_tok + q_head0 * a.q_head, a.q_tok, tid);
 
   Tile<D> tk, tv, tq;
   tk.fetch(k_from, a.k_tok, seg.rows, tid);
   tv.fetch(v_from, a.v_tok, seg.rows, tid);
   if (OUT) tq.fetch(q_from, a.q_tok, seg.rows, tid);
+  // scale * d^(i - j) of the scores that this lane computes: queries i = 16
+  // wave + lane % 16, keys j = 16 t + 4 (lane / 16) + e, and of those which are
+  // not later ones (bit 4 t + e)
+  float apart[4][4];
+  int earlier = 0;
+  if (OUT) {
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int m = 16 * wave + lane % 16 - (16 * t + 4 * (lane / 16) + e);
+        apart[t][e] = m > 0 ? power[m - 1] * a.scale : a.scale;
+        earlier |= (m >= 0) << (4 * t + e);
+      }
+  }
 #pragma unroll 1
   for (int chunk = 0; chunk < chunks; ++chunk) {
     const int row0 = chunk * kChunk, rows = min(kChunk, seg.rows - row0);
@@ -398,11 +446,19 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
     tk.template store_ordered<T>(keys, tid);
     tv.store(values, tid);
     if (tid < kChunk && (chunk == 0 || rows < kChunk)) left[tid] = tid < rows ? decay_by(rows - 1 - tid) : 0.0f;
-    const int next = row0 + kChunk;
-    if (chunk + 1 < chunks) {
-      tk.fetch(k_from + next * a.k_tok, a.k_tok, seg.rows - next, tid);
-      tv.fetch(v_from + next * a.v_tok, a.v_tok, seg.rows - next, tid);
-    }
+    // the next chunk's; what is on its way is waited for as a whole, so nothing
+    // is fetched before all that is there is in LDS
+    auto fetch_next = [&]() {
+      if (chunk + 1 == chunks) return;
+      const int behind = seg.rows - row0 - kChunk;
+      k_from += kChunk * a.k_tok;
+      v_from += kChunk * a.v_tok;
+      q_from += kChunk * a.q_tok;
+      tk.fetch(k_from, a.k_tok, behind, tid);
+      tv.fetch(v_from, a.v_tok, behind, tid);
+      if (OUT) tq.fetch(q_from, a.q_tok, behind, tid);
+    };
+    const int v_place = column_place<D, false>(lane) + c * 64;
     if constexpr (OUT) {
 #pragma unroll 1
       for (int s = 0; s < a.share; ++s) {
@@ -413,12 +469,15 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
         asm volatile("" : "+v"(lane), "+v"(n), "+v"(h), "+v"(tid));
         tq.template store_ordered<T>(queries, tid);
         if (s + 1 < a.share)
-          tq.fetch(q_from + row0 * a.q_tok + (s + 1) * a.q_head, a.q_tok, rows, tid);
-        else if (chunk + 1 < chunks)
-          tq.fetch(q_from + next * a.q_tok, a.q_tok, seg.rows - next, tid);
+          tq.fetch(q_from + (s + 1) * a.q_head, a.q_tok, rows, tid);
+        else
+          fetch_next();
         __syncthreads();
         // scores, transposed: keys 16 t .. of the wave's 16 queries; those of later keys are 0, and of a later 32
         // queries' keys are not read
+        const char* k_at = keys + Rows<D>::at(lane % 16) + lane / 16 * 16;
+        const char* q_at = queries + Rows<D>::at(lane % 16) + lane / 16 * 16 + wave * Rows<D>::of(16);
+        char* w_to = weights + (16 * wave + lane % 16) * kScorePitch + lane / 16 * 8;
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           if (t > (wave | 1)) continue;
@@ -429,8 +488,8 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
               s16x8 kp[P], qp[P];
 #pragma unroll
               for (int p = 0; p < P; ++p) {
-                kp[p] = *(const s16x8*)(keys + p * L::kTile + place<D>(16 * t + lane % 16, 4 * k + lane / 16));
-                qp[p] = *(const s16x8*)(queries + p * L::kTile + place<D>(16 * wave + lane % 16, 4 * k + lane / 16));
+                kp[p] = *(const s16x8*)(k_at + p * L::kTile + Rows<D>::of(16 * t) + k * 64);
+                qp[p] = *(const s16x8*)(q_at + p * L::kTile + k * 64);
               }
 #pragma unroll
               for (int p = 0; p < P; ++p)
@@ -440,12 +499,15 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
           }
           f32x4 y;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) y[e] = apart[t][e] < 0.0f ? 0.0f : x[e] * apart[t][e];
-          const bf16x4 hi = __builtin_convertvector(y, bf16x4);
-          const bf16x4 lo = __builtin_convertvector(y - __builtin_convertvector(hi, f32x4), bf16x4);
-          const int to = place<64>(16 * wave + lane % 16, 2 * t + lane / 32) + ((lane >> 4) & 1) * 8;
-          *(bf16x4*)(weights + to) = hi;
-          *(bf16x4*)(weights + 2 * kChunk * kChunk + to) = lo;
+          for (int e = 0; e < 4; ++e) {
+            y[e] = x[e] * apart[t][e];
+            if (t >= wave) y[e] = earlier >> (4 * t + e) & 1 ? y[e] : 0.0f;
+          }
+          f32x4 rest;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) rest[e] = y[e] - leading(y[e]);
+          *(i32x2*)(w_to + t * 32) = i32x2{packed(y[0], y[1]), packed(y[2], y[3])};
+          *(bf16x4*)(w_to + t * 32 + kScores) = __builtin_convertvector(rest, bf16x4);
         }
         // the state's part of the results, transposed: queries 32 (rw * tiles + t) + n, columns as the state's rows
         f32x16 o[kRowTiles];
@@ -453,6 +515,7 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
         for (int t = 0; t < kRowTiles; ++t)
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
+        const char* q_row = queries + Rows<D>::at(n) + h * 16 + rw * kRowTiles * Rows<D>::of(32);
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
           f32x8 x;
@@ -462,10 +525,9 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
           split<2>(x, sp);
 #pragma unroll
           for (int t = 0; t < kRowTiles; ++t) {
-            const int row = 32 * (rw * kRowTiles + t) + n;
             s16x8 qp[P];
 #pragma unroll
-            for (int p = 0; p < P; ++p) qp[p] = *(const s16x8*)(queries + p * L::kTile + place<D>(row, 2 * k + h));
+            for (int p = 0; p < P; ++p) qp[p] = *(const s16x8*)(q_row + p * L::kTile + Rows<D>::of(32 * t) + k * 32);
             o[t] = multiply(sp[0], qp[0], o[t]);
             o[t] = multiply(sp[1], qp[0], o[t]);
             if constexpr (P == 2) o[t] = multiply(sp[0], qp[1], o[t]);
@@ -473,7 +535,7 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
         }
 #pragma unroll
         for (int t = 0; t < kRowTiles; ++t) {
-          const float by = power[32 * (rw * kRowTiles + t) + n];
+          const float by = power[32 * (rw * kRowTiles + t) + n] * a.scale;
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[t][i] *= by;
         }
@@ -483,7 +545,7 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
         uint32_t some = 0;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          v[k] = __builtin_bit_cast(i32x4, column<D, false>(values, k, c, lane));
+          v[k] = __builtin_bit_cast(i32x4, column<D>(values, v_place, k, 0));
 #pragma unroll
           for (int e = 0; e < 4; ++e) some |= T::odd(v[k][e]);
         }
@@ -496,16 +558,16 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[k][e] &= (int)~((T::odd(v[k][e]) >> 15) * 0xffffu);
         }
+        const char* w_row = weights + (rw * kRowTiles * 32 + n) * kScorePitch + h * 16;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           s16x8 vp[P];
           T::parts(__builtin_bit_cast(s16x8, v[k]), vp);
 #pragma unroll
           for (int t = 0; t < kRowTiles; ++t) {
-            const int tile = rw * kRowTiles + t;
-            if (k > 2 * tile + 1) continue;
-            const int p = place<64>(32 * tile + n, 2 * k + h);
-            const s16x8 hi = *(const s16x8*)(weights + p), lo = *(const s16x8*)(weights + 2 * kChunk * kChunk + p);
+            if (k > 2 * (rw * kRowTiles + t) + 1) continue;
+            const char* w = w_row + t * 32 * kScorePitch + k * 32;
+            const s16x8 hi = *(const s16x8*)w, lo = *(const s16x8*)(w + kScores);
             o[t] = multiply(vp[0], hi, o[t]);
             o[t] = multiply(vp[0], lo, o[t]);
             if constexpr (P == 2) o[t] = multiply(vp[1], hi, o[t]);
@@ -514,18 +576,15 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
         if (odd) {
 #pragma unroll 1
           for (int j = 0; j < rows; ++j) {
-            const char* x_at = values + j * 2 * D;
-            const char* w_at = weights + (j % 8) * 2;
-            int sw = swizzle<D>(j) << 4, first = c * 64 + 8 * h, chunk_at = (j / 8) << 4;
-            asm volatile("" : "+v"(sw), "+v"(first), "+v"(chunk_at));
+            const char* x_at = values + Rows<D>::at(j) + c * 64 + h * 8;
 #pragma unroll
             for (int t = 0; t < kRowTiles; ++t) {
               const int row = 32 * (rw * kRowTiles + t) + n;
-              const char* p = w_at + row * 2 * kChunk + (chunk_at ^ swizzle<64>(row) << 4);
-              const float w = j <= row ? (float)*(const __bf16*)p + (float)*(const __bf16*)(p + 2 * kChunk * kChunk) : 0.0f;
+              const char* p = weights + row * kScorePitch + j * 2;
+              const float w = j <= row ? (float)*(const __bf16*)p + (float)*(const __bf16*)(p + kScores) : 0.0f;
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                const s16x4 x = *(const s16x4*)(x_at + (((first & ~15) + i * 16) ^ sw) + (first & 8));
+                const s16x4 x = *(const s16x4*)(x_at + i * 16);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                   const bool here = T::odd(x[e] & 0xffff) && j <= row;
@@ -542,25 +601,25 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
             char* to = a.out + (seg.row0 + row0 + row) * a.o_tok + (q_head0 + s) * a.o_head + (c * 32 + 4 * h) * 2;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const f32x4 x = {o[t][4 * i] * a.scale, o[t][4 * i + 1] * a.scale, o[t][4 * i + 2] * a.scale,
-                               o[t][4 * i + 3] * a.scale};
-              *(s16x4*)(to + i * 16) = T::narrow(x);
+              *(s16x4*)(to + i * 16) = T::narrow(f32x4{o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]});
             }
           }
         }
       }
     } else {
+      fetch_next();
       __syncthreads();
     }
     // the state behind the chunk
-    const float by = rows == kChunk ? power[kChunk - 1] : power[rows - 1];
+    const float by = power[rows - 1];
 #pragma unroll
     for (int t = 0; t < kGroups; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) state[t][i] *= by;
+    const int k_place = column_place<D, true>(lane);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      f32x8 x = T::wide(column<D, false>(values, k, c, lane));
+      f32x8 x = T::wide(column<D>(values, v_place, k, 0));
       const f32x4 w0 = *(const f32x4*)(left + 16 * k + 8 * h), w1 = *(const f32x4*)(left + 16 * k + 8 * h + 4);
       x *= __builtin_shufflevector(w0, w1, 0, 1, 2, 3, 4, 5, 6, 7);
       s16x8 vp[3];
@@ -569,7 +628,7 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
       for (int t = 0; t < kGroups; ++t) {
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-          const s16x8 kp = column<D, true>(keys + p * L::kTile, k, t, lane);
+          const s16x8 kp = column<D>(keys + p * L::kTile, k_place, k, t);
 #pragma unroll
           for (int r = 0; r + p < 3; ++r) state[t] = multiply(kp, vp[r], state[t]);
         }
@@ -580,13 +639,13 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
   float* to = nullptr;
   if (!OUT)
     to = a.added + ((int64_t)(seg.slot + seg.index + 1) * a.kv_heads + head) * D * D;
-  else if (last && write >= 0)
+  else if (last && write >= 0 && (seg.rows || write != read))
     to = a.state + write * a.state_slot + head * a.state_head;
   if (to && rw == 0) {
 #pragma unroll
     for (int t = 0; t < kGroups; ++t)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) to[(t * 32 + 8 * (i / 4) + 4 * h + i % 4) * D + c * 32 + n] = state[t][i];
+      for (int i = 0; i < 16; ++i) to[mine + (t * 32 + 8 * (i / 4) + i % 4) * D] = state[t][i];
   }
 }
 
@@ -647,7 +706,7 @@ hipError_t launch_chunks(const LinearArgs& a, hipStream_t st) {
 template <int D, class T>
 hipError_t launch(const LinearArgs& a, hipStream_t st) {
   hipError_t e = hipSuccess;
-  if (a.row_start && a.tokens > kFewTokens) {
+  if (a.row_start && a.tokens > a.few) {
     if (a.tokens > a.segment) {
       e = launch_chunks<D, T, false>(a, st);
       if (e != hipSuccess) return e;
@@ -658,6 +717,7 @@ hipError_t launch(const LinearArgs& a, hipStream_t st) {
     e = launch_chunks<D, T, true>(a, st);
     if (e != hipSuccess) return e;
   }
+  if (a.few < 0) return hipSuccess;
   linear_steps_kernel<D, typename T::Type><<<(uint32_t)a.requests * (uint32_t)a.kv_heads, kThreads, 0, st>>>(a);
   return hipGetLastError();
 }
