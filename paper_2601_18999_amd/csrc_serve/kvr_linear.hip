@@ -268,19 +268,17 @@ struct Rows {
   static __device__ __forceinline__ int at(int row) { return row * kPitch + row / 4 * 16; }
 };
 
-// Queries and keys stand in LDS in the order in which a state's registers
-// hold its rows: of 16 elements the groups of four 0, 2, 1, 3.  A chunk of 16
-// bytes, which a half wave takes as an operand, then holds elements 4 h .. and
-// 8 + 4 h .. of its 16.
-
 // Eight rows' elements of one column a lane: rows 16 s + 8 h .., column 32 c +
 // lane % 32.  The transposing read: 16 lanes name four rows of 16 elements,
 // four lanes a row, and lane i of them gets column i.  `at`: column_place.
-template <int D, bool ORDERED>
+// STATE: of 16 columns the groups of four 0, 2, 1, 3, so that of the products'
+// results, whose rows those columns are, a lane holds rows 16 s + 8 h .. + 7 in
+// registers 8 s .., as an operand has them.
+template <int D, bool STATE>
 __device__ __forceinline__ int column_place(int lane) {
   const int sl = lane & 15;
   return Rows<D>::at((lane >> 5) * 8 + sl / 4) + ((lane >> 4) & 1) * 32 +
-         (ORDERED ? (sl & 1) * 16 + (sl & 2) * 4 : (sl & 3) * 8);
+         (STATE ? (sl & 1) * 16 + (sl & 2) * 4 : (sl & 3) * 8);
 }
 template <int D>
 __device__ __forceinline__ s16x8 column(const char* tile, int at, int s, int c) {
@@ -316,20 +314,16 @@ struct Tile {
   static __device__ __forceinline__ const char* lane(const char* from, int64_t stride, int thread) {
     return from + thread / kChunks * stride + thread % kChunks * 16;
   }
+  // in as many parts as the products take (one tile behind the other)
   template <class T>
-  __device__ __forceinline__ void store_ordered(char* tile, int thread) const {
-    const int chunk = thread % kChunks;
-    char* to = tile + Rows<D>::at(thread / kChunks) + chunk / 2 * 32 + (chunk & 1) * 8;
+  __device__ __forceinline__ void store_parts(char* tile, int thread) const {
+    char* to = tile + Rows<D>::at(thread / kChunks) + thread % kChunks * 16;
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       s16x8 part[T::kParts];
       T::parts(x[i], part);
 #pragma unroll
-      for (int k = 0; k < T::kParts; ++k) {
-        char* p = to + Rows<D>::of(i * kStepRows) + k * Rows<D>::kBytes;
-        *(s16x4*)p = __builtin_shufflevector(part[k], part[k], 0, 1, 2, 3);
-        *(s16x4*)(p + 16) = __builtin_shufflevector(part[k], part[k], 4, 5, 6, 7);
-      }
+      for (int k = 0; k < T::kParts; ++k) *(s16x8*)(to + Rows<D>::of(i * kStepRows) + k * Rows<D>::kBytes) = part[k];
     }
   }
   __device__ __forceinline__ void store(char* tile, int thread) const {
@@ -354,7 +348,7 @@ static_assert(2 * ChunkLds<128, OfBf16, true>::kBytes <= 160 * 1024, "two workgr
 
 // One workgroup for a segment's key head.  Wave w has 32 columns of the state
 // (D / 32 column groups; with two groups two waves hold the same) in registers:
-// lane n column n, register i row 8 (i / 4) + 4 h + i % 4 of each 32, which is
+// lane n column n, register i row 16 (i / 8) + 8 h + i % 8 of each 32, which is
 // an operand of the products with queries as it stands.  OUT: computes the
 // results from the state before the segment; else what the segment adds to it.
 template <int D, class T, bool OUT>
@@ -396,13 +390,12 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
     from = a.added + ((int64_t)(seg.slot + seg.index) * a.kv_heads + head) * D * D;
   else if (OUT && read >= 0)
     from = a.state + read * a.state_slot + head * a.state_head;
-  // (a place in the state of this lane's columns: its row 0 of each four)
-  const int mine = 4 * h * D + c * 32 + n;
+  const int mine = 8 * h * D + c * 32 + n;  // the lane's first value
   if (from) {
 #pragma unroll
     for (int t = 0; t < kGroups; ++t)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) state[t][i] = from[mine + (t * 32 + 8 * (i / 4) + i % 4) * D];
+      for (int i = 0; i < 16; ++i) state[t][i] = from[mine + (t * 32 + 16 * (i / 8) + i % 8) * D];
   } else {
 #pragma unroll
     for (int t = 0; t < kGroups; ++t)
@@ -443,7 +436,7 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
     // (places in LDS are computed where they are used: kept over the loop, they take more registers than there are)
     asm volatile("" : "+v"(lane), "+v"(n), "+v"(h), "+v"(tid));
     __syncthreads();  // the tiles of the chunk before are read
-    tk.template store_ordered<T>(keys, tid);
+    tk.template store_parts<T>(keys, tid);
     tv.store(values, tid);
     if (tid < kChunk && (chunk == 0 || rows < kChunk)) left[tid] = tid < rows ? decay_by(rows - 1 - tid) : 0.0f;
     // the next chunk's; what is on its way is waited for as a whole, so nothing
@@ -467,7 +460,7 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
 #pragma unroll
         for (int t = 0; t < kGroups; ++t) asm volatile("" : "+v"(state[t]));
         asm volatile("" : "+v"(lane), "+v"(n), "+v"(h), "+v"(tid));
-        tq.template store_ordered<T>(queries, tid);
+        tq.template store_parts<T>(queries, tid);
         if (s + 1 < a.share)
           tq.fetch(q_from + (s + 1) * a.q_head, a.q_tok, rows, tid);
         else
@@ -645,7 +638,7 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
 #pragma unroll
     for (int t = 0; t < kGroups; ++t)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) to[mine + (t * 32 + 8 * (i / 4) + i % 4) * D] = state[t][i];
+      for (int i = 0; i < 16; ++i) to[mine + (t * 32 + 16 * (i / 8) + i % 8) * D] = state[t][i];
   }
 }
 
