@@ -346,6 +346,11 @@ struct ChunkLds {
 };
 static_assert(2 * ChunkLds<128, OfBf16, true>::kBytes <= 160 * 1024, "two workgroups a compute unit");
 
+// What is read from LDS above is on its way before anything below begins: a
+// read takes as long as several products, and left to itself the compiler puts
+// it right before its use.
+__device__ __forceinline__ void ahead() { __builtin_amdgcn_sched_barrier(0); }
+
 // One workgroup for a segment's key head.  Wave w has 32 columns of the state
 // (D / 32 column groups; with two groups two waves hold the same) in registers:
 // lane n column n, register i row 16 (i / 8) + 8 h + i % 8 of each 32, which is
@@ -354,6 +359,7 @@ static_assert(2 * ChunkLds<128, OfBf16, true>::kBytes <= 160 * 1024, "two workgr
 template <int D, class T, bool OUT>
 __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a) {
   typedef ChunkLds<D, T, OUT> L;
+  constexpr bool kEarly = D == 64;  // (heads of 128 leave no registers for it)
   constexpr int kGroups = D / 32, kRowWaves = 4 / kGroups, kRowTiles = 2 / kRowWaves, kSteps = D / 16, P = T::kParts;
   extern __shared__ __align__(16) char lds[];
   char* keys = lds;
@@ -471,24 +477,33 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
         const char* k_at = keys + Rows<D>::at(lane % 16) + lane / 16 * 16;
         const char* q_at = queries + Rows<D>::at(lane % 16) + lane / 16 * 16 + wave * Rows<D>::of(16);
         char* w_to = weights + (16 * wave + lane % 16) * kScorePitch + lane / 16 * 8;
+        s16x8 qp[D / 32][P], kp[2][D / 32][P];
+        auto read_keys = [&](int t) {
+#pragma unroll
+          for (int k = 0; k < D / 32; ++k)
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+              kp[t & 1][k][p] = *(const s16x8*)(k_at + p * L::kTile + Rows<D>::of(16 * t) + k * 64);
+        };
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k)
+#pragma unroll
+          for (int p = 0; p < P; ++p) qp[k][p] = *(const s16x8*)(q_at + p * L::kTile + k * 64);
+        if (kEarly) read_keys(0);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           if (t > (wave | 1)) continue;
           f32x4 x = {0, 0, 0, 0};
+          if (kEarly && t < wave) read_keys((t + 1) & 3);
+          if (kEarly) ahead();
+          if (!kEarly && t <= wave) read_keys(t);
           if (t <= wave) {
 #pragma unroll
-            for (int k = 0; k < D / 32; ++k) {
-              s16x8 kp[P], qp[P];
-#pragma unroll
-              for (int p = 0; p < P; ++p) {
-                kp[p] = *(const s16x8*)(k_at + p * L::kTile + Rows<D>::of(16 * t) + k * 64);
-                qp[p] = *(const s16x8*)(q_at + p * L::kTile + k * 64);
-              }
+            for (int k = 0; k < D / 32; ++k)
 #pragma unroll
               for (int p = 0; p < P; ++p)
 #pragma unroll
-                for (int r = 0; r + p < P; ++r) x = multiply(kp[p], qp[r], x);
-            }
+                for (int r = 0; r + p < P; ++r) x = multiply(kp[t & 1][k][p], qp[k][r], x);
           }
           f32x4 y;
 #pragma unroll
@@ -509,8 +524,19 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
         const char* q_row = queries + Rows<D>::at(n) + h * 16 + rw * kRowTiles * Rows<D>::of(32);
+        s16x8 qs[2][kRowTiles][P];
+        auto read_queries = [&](int k) {
+#pragma unroll
+          for (int t = 0; t < kRowTiles; ++t)
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+              qs[k & 1][t][p] = *(const s16x8*)(q_row + p * L::kTile + Rows<D>::of(32 * t) + k * 32);
+        };
+        read_queries(0);
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
+          if (k + 1 < kSteps) read_queries(k + 1);
+          ahead();
           f32x8 x;
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[e] = state[k / 2][8 * (k % 2) + e];
@@ -518,12 +544,9 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
           split<2>(x, sp);
 #pragma unroll
           for (int t = 0; t < kRowTiles; ++t) {
-            s16x8 qp[P];
-#pragma unroll
-            for (int p = 0; p < P; ++p) qp[p] = *(const s16x8*)(q_row + p * L::kTile + Rows<D>::of(32 * t) + k * 32);
-            o[t] = multiply(sp[0], qp[0], o[t]);
-            o[t] = multiply(sp[1], qp[0], o[t]);
-            if constexpr (P == 2) o[t] = multiply(sp[0], qp[1], o[t]);
+            o[t] = multiply(sp[0], qs[k & 1][t][0], o[t]);
+            o[t] = multiply(sp[1], qs[k & 1][t][0], o[t]);
+            if constexpr (P == 2) o[t] = multiply(sp[0], qs[k & 1][t][1], o[t]);
           }
         }
 #pragma unroll
@@ -535,13 +558,26 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
         __syncthreads();
         // the chunk's own part
         i32x4 v[4];
+        s16x8 wp[2][kRowTiles][2];
+        const char* w_row = weights + (rw * kRowTiles * 32 + n) * kScorePitch + h * 16;
+        auto read_weights = [&](int k) {
+#pragma unroll
+          for (int t = 0; t < kRowTiles; ++t) {
+            if (k > 2 * (rw * kRowTiles + t) + 1) continue;
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+              wp[k & 1][t][p] = *(const s16x8*)(w_row + t * 32 * kScorePitch + k * 32 + p * kScores);
+          }
+        };
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = __builtin_bit_cast(i32x4, column<D>(values, v_place, k, 0));
+        read_weights(0);
+        ahead();
         uint32_t some = 0;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          v[k] = __builtin_bit_cast(i32x4, column<D>(values, v_place, k, 0));
+        for (int k = 0; k < 4; ++k)
 #pragma unroll
           for (int e = 0; e < 4; ++e) some |= T::odd(v[k][e]);
-        }
         // An infinity or NaN does not go into the products, where 0 * inf would
         // reach the rows before it.
         const bool odd = __any(some != 0);
@@ -551,19 +587,18 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[k][e] &= (int)~((T::odd(v[k][e]) >> 15) * 0xffffu);
         }
-        const char* w_row = weights + (rw * kRowTiles * 32 + n) * kScorePitch + h * 16;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
+          if (k + 1 < 4) read_weights(k + 1);
+          ahead();
           s16x8 vp[P];
           T::parts(__builtin_bit_cast(s16x8, v[k]), vp);
 #pragma unroll
           for (int t = 0; t < kRowTiles; ++t) {
             if (k > 2 * (rw * kRowTiles + t) + 1) continue;
-            const char* w = w_row + t * 32 * kScorePitch + k * 32;
-            const s16x8 hi = *(const s16x8*)w, lo = *(const s16x8*)(w + kScores);
-            o[t] = multiply(vp[0], hi, o[t]);
-            o[t] = multiply(vp[0], lo, o[t]);
-            if constexpr (P == 2) o[t] = multiply(vp[1], hi, o[t]);
+            o[t] = multiply(vp[0], wp[k & 1][t][0], o[t]);
+            o[t] = multiply(vp[0], wp[k & 1][t][1], o[t]);
+            if constexpr (P == 2) o[t] = multiply(vp[1], wp[k & 1][t][0], o[t]);
           }
         }
         if (odd) {
@@ -604,28 +639,39 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
       __syncthreads();
     }
     // the state behind the chunk
+    const int k_place = column_place<D, true>(lane);
+    s16x8 vs[2], ks[2][kGroups][P];
+    f32x4 ws[2];
+    auto read_update = [&](int k) {
+      vs[k & 1] = column<D>(values, v_place, k, 0);
+      ws[0] = *(const f32x4*)(left + 16 * k + 8 * h);
+      ws[1] = *(const f32x4*)(left + 16 * k + 8 * h + 4);
+#pragma unroll
+      for (int t = 0; t < kGroups; ++t)
+#pragma unroll
+        for (int p = 0; p < P; ++p) ks[k & 1][t][p] = column<D>(keys + p * L::kTile, k_place, k, t);
+    };
+    read_update(0);
     const float by = power[rows - 1];
 #pragma unroll
     for (int t = 0; t < kGroups; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) state[t][i] *= by;
-    const int k_place = column_place<D, true>(lane);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      f32x8 x = T::wide(column<D>(values, v_place, k, 0));
-      const f32x4 w0 = *(const f32x4*)(left + 16 * k + 8 * h), w1 = *(const f32x4*)(left + 16 * k + 8 * h + 4);
-      x *= __builtin_shufflevector(w0, w1, 0, 1, 2, 3, 4, 5, 6, 7);
+      f32x8 x = T::wide(vs[k & 1]);
+      x *= __builtin_shufflevector(ws[0], ws[1], 0, 1, 2, 3, 4, 5, 6, 7);
+      if (k + 1 < 4) read_update(k + 1);
+      ahead();
       s16x8 vp[3];
       split<3>(x, vp);
 #pragma unroll
-      for (int t = 0; t < kGroups; ++t) {
+      for (int r = 0; r < 3; ++r)
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-          const s16x8 kp = column<D>(keys + p * L::kTile, k_place, k, t);
+        for (int t = 0; t < kGroups; ++t)
 #pragma unroll
-          for (int r = 0; r + p < 3; ++r) state[t] = multiply(kp, vp[r], state[t]);
-        }
-      }
+          for (int p = 0; p < P; ++p)
+            if (r + p < 3) state[t] = multiply(ks[k & 1][t][p], vp[r], state[t]);
     }
   }
 
