@@ -622,16 +622,22 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
             }
           }
         }
+        // A wave's results, 64 bytes of each row, go through the queries' place
+        // (which all waves have read), so that four lanes write a row's.
+        const int first = rw * kRowTiles * 32;
+        char* r_to = queries + Rows<D>::at(n) + rw * kRowTiles * Rows<D>::of(32) + c * 64 + h * 8;
 #pragma unroll
-        for (int t = 0; t < kRowTiles; ++t) {
-          const int row = 32 * (rw * kRowTiles + t) + n;
-          if (row < rows) {
-            char* to = a.out + (seg.row0 + row0 + row) * a.o_tok + (q_head0 + s) * a.o_head + (c * 32 + 4 * h) * 2;
+        for (int t = 0; t < kRowTiles; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              *(s16x4*)(to + i * 16) = T::narrow(f32x4{o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]});
-            }
-          }
+          for (int i = 0; i < 4; ++i)
+            *(s16x4*)(r_to + Rows<D>::of(32 * t) + i * 16) =
+                T::narrow(f32x4{o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]});
+        const char* r_from = queries + Rows<D>::at(lane / 4) + rw * kRowTiles * Rows<D>::of(32) + c * 64 + lane % 4 * 16;
+        char* to = a.out + (seg.row0 + row0 + first + lane / 4) * a.o_tok + (q_head0 + s) * a.o_head + c * 64 + lane % 4 * 16;
+#pragma unroll
+        for (int i = 0; i < 2 * kRowTiles; ++i, to += 16 * a.o_tok) {
+          const s16x8 x = *(const s16x8*)(r_from + Rows<D>::of(16 * i));
+          if (first + 16 * i + lane / 4 < rows) __builtin_memcpy(to, &x, sizeof(x));
         }
       }
     } else {
