@@ -31,7 +31,12 @@ struct ProductArgs {
   const float *x_scale, *w_scale, *bias;
   int64_t x_tok, w_chan, out_tok;  // bytes
   int32_t tokens, dim, channels;
+  int32_t dtype;  // of x: KVR_INT8, or of few tokens that are not brought to integers yet
 };
+
+// So few elements of 16 bits are brought to integers by every workgroup of the
+// product for itself, of at most 16 tokens.
+constexpr int kFewElements = 1 << 16;
 
 // ---- linear attention ----
 // Requests of up to so many tokens take the recurrent form; where a request has

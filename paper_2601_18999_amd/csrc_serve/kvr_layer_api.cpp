@@ -58,8 +58,13 @@ kvr_status check(const kvr_product* p) {
   return KVR_OK;
 }
 
+// Whether 16-bit tokens go through the workspace, as integers.
+bool quantised_first(const kvr_product* p) {
+  return p->dtype != KVR_INT8 && (p->num_tokens > 16 || (int64_t)p->num_tokens * p->dim > kvr::kFewElements);
+}
+
 size_t product_bytes(const kvr_product* p) {
-  return p->dtype == KVR_INT8 ? 0 : round_up((size_t)p->num_tokens * 4) + round_up((size_t)p->num_tokens * p->dim);
+  return !quantised_first(p) ? 0 : round_up((size_t)p->num_tokens * 4) + round_up((size_t)p->num_tokens * p->dim);
 }
 
 kvr_status check(const kvr_linear* l) {
@@ -182,8 +187,9 @@ kvr_status kvr_integer_product(const kvr_product* p, void* d_workspace, size_t b
   a.tokens = p->num_tokens;
   a.dim = p->dim;
   a.channels = p->channels;
+  a.dtype = p->dtype;
   hipError_t e = hipSuccess;
-  if (!int8) {
+  if (need) {
     kvr::NormArgs n = {};
     n.x = a.x;
     n.x_tok = a.x_tok;
@@ -197,6 +203,7 @@ kvr_status kvr_integer_product(const kvr_product* p, void* d_workspace, size_t b
     a.x = n.out;
     a.x_tok = n.out_tok;
     a.x_scale = n.out_scale;
+    a.dtype = KVR_INT8;
   }
   if (e == hipSuccess) e = kvr::launch_product(a, p->out_dtype, stream);
   return e == hipSuccess ? KVR_OK : hip_failed(e, "product kernels launch");

@@ -8,6 +8,7 @@
 #include <hip/hip_runtime.h>
 
 #include "kvr_layer.h"
+#include "kvr_wave.h"
 
 namespace kvr {
 namespace {
@@ -87,29 +88,6 @@ __device__ __forceinline__ void store8(char* row, int at, int n, const float (&f
     for (int i = 0; i < 8; ++i)
       if (at + i < n) p[i] = (T)f[i];
   }
-}
-
-// Over the lanes of a wave: within rows of 16 by DPP, then across them.
-template <class Op>
-__device__ __forceinline__ uint32_t over_wave(uint32_t x, Op op) {
-  x = op(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xb1, 0xf, 0xf, false));   // lane ^ 1
-  x = op(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4e, 0xf, 0xf, false));   // lane ^ 2
-  x = op(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xf, 0xf, false));  // mirrored in 8
-  x = op(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xf, 0xf, false));  // mirrored in 16
-  const auto s = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-  x = op(s[0], s[1]);
-  const auto t = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-  return op(t[0], t[1]);
-}
-
-__device__ __forceinline__ float wave_sum(float x) {
-  return __uint_as_float(over_wave(__float_as_uint(x), [](uint32_t a, uint32_t b) {
-    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
-  }));
-}
-
-__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
-  return over_wave(x, [](uint32_t a, uint32_t b) { return max(a, b); });
 }
 
 // One row for each wave (SINGLE: four rows a workgroup), or for a workgroup.
@@ -204,7 +182,6 @@ __global__ __launch_bounds__(SINGLE ? 256 : 64 * kMostWaves, V == 1 ? 8 : 4) voi
 #pragma unroll
       for (int v = 0; v < V; ++v) store8<T>(out, at0 + v * next, a.dim, f[v]);
     } else {
-      // The largest magnitude by its bits: NaN is above infinity, and that above the rest.
       uint32_t top = 0;
 #pragma unroll
       for (int v = 0; v < V; ++v)
@@ -216,17 +193,14 @@ __global__ __launch_bounds__(SINGLE ? 256 : 64 * kMostWaves, V == 1 ? 8 : 4) voi
         __syncthreads();
         top = wave_max(lane < waves ? tops[lane % kMostWaves] : 0);
       }
-      const float largest = __uint_as_float(top);
-      const bool usual = top < 0x7f800000u && largest >= 0x1p-100f;
-      const float by = usual ? 127.0f / largest : 0.0f;
-      if (at0 == 0)
-        a.out_scale[row] = usual ? largest / 127.0f : top < 0x7f800000u ? 0.0f : __uint_as_float(0x7fc00000u);
+      const Quantiser by(top);
+      if (at0 == 0) a.out_scale[row] = by.scale;
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const int at = at0 + v * next;
         Eight<int8_t> q;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) q.e[i] = usual ? (int8_t)(int)__builtin_rintf(f[v][i] * by) : 0;
+        for (int i = 0; i < 8; ++i) q.e[i] = Quantiser::integer(f[v][i], by.by);
         if (at + 8 <= a.dim) {
           __builtin_memcpy(out + at, &q, 8);
         } else if (at < a.dim) {

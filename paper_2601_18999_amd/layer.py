@@ -23,6 +23,7 @@ from .serve import _current, _gpu, _no_gradient, _refuse, _status, _stream, _vec
 DTYPE_CODES = {torch.bfloat16: 0, torch.float16: 1, torch.int8: 3, torch.float32: 4}
 ACTIVATIONS = {"none": 0, "sigmoid": 1, "silu": 2}
 HALVES = (torch.bfloat16, torch.float16)
+PRODUCT_TYPES = (torch.int8, *HALVES)
 
 # the structs of include/kvr.h, as struct packs them (tests compare the layouts)
 NORM_RECORD = struct.Struct("<I6i2fi8Q5q")
@@ -37,15 +38,17 @@ class BlockNorm(NamedTuple):
     scale: Optional[torch.Tensor]     # [tokens] float32 of an 8-bit result, else None
 
 
-def _matrix(where: str, name: str, t, dtypes, rows, dim, device) -> int:
-    """data_ptr of a [rows, dim] tensor (None: of any number) whose rows are contiguous."""
-    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or t.device != device or t.dim() != 2 or \
-            (rows is not None and t.shape[0] != rows) or (dim is not None and t.shape[1] != dim):
-        _refuse(where, f"{name} must be [{'rows' if rows is None else rows}, {'dim' if dim is None else dim}] of "
-                       f"{' or '.join(map(str, dtypes))} on {device}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
-        _refuse(where, f"the elements of a row of {name} must be contiguous")
-    return t.data_ptr()
+def _matrix(where: str, name: str, t, dtypes, rows, dim, device):
+    """data_ptr and row stride of a [rows, dim] tensor (None: of any number) whose rows are contiguous."""
+    if isinstance(t, torch.Tensor) and t.dtype in dtypes and t.device == device:
+        shape = t.shape
+        if len(shape) == 2 and (rows is None or shape[0] == rows) and (dim is None or shape[1] == dim):
+            stride, one = t.stride()
+            if one == 1 or shape[1] <= 1:
+                return t.data_ptr(), stride
+            _refuse(where, f"the elements of a row of {name} must be contiguous")
+    _refuse(where, f"{name} must be [{'rows' if rows is None else rows}, {'dim' if dim is None else dim}] of "
+                   f"{' or '.join(map(str, dtypes))} on {device}")
 
 
 def _apart(where: str, name: str, t) -> None:
@@ -76,42 +79,49 @@ def block_norm(x: torch.Tensor, *, after: Optional[torch.Tensor] = None, gate: O
             return block_norm(x, after=after, gate=gate, activation=activation, residual=residual,
                               residual_scale=residual_scale, before=before, eps=eps, int8=int8, in_place=in_place,
                               out=out)
-    kind = (x.dtype,)
-    if x.dtype not in HALVES:
-        _refuse(where, f"x of {x.dtype} is not supported (bfloat16, float16)")
-    p_x = _matrix(where, "x", x, kind, None, None, device)
+    dtype = x.dtype
+    code = DTYPE_CODES.get(dtype, 3)
+    if code > 1:
+        _refuse(where, f"x of {dtype} is not supported (bfloat16, float16)")
+    p_x, x0 = _matrix(where, "x", x, HALVES, None, None, device)
     tokens, dim = x.shape
-    p_after = 0 if after is None else _vector(where, "after", after, x.dtype, dim, device)
-    p_before = 0 if before is None else _vector(where, "before", before, x.dtype, dim, device)
-    p_gate = 0 if gate is None else _matrix(where, "gate", gate, kind, tokens, dim, device)
+    p_after = 0 if after is None else _vector(where, "after", after, dtype, dim, device)
+    p_before = 0 if before is None else _vector(where, "before", before, dtype, dim, device)
+    p_gate, g0 = (0, 0) if gate is None else _matrix(where, "gate", gate, (dtype,), tokens, dim, device)
     if activation not in ACTIVATIONS:
         _refuse(where, f"activation must be one of {', '.join(ACTIVATIONS)}")
-    p_res = p_new = code = r0 = n0 = 0
+    p_res = p_new = p_scale = res_code = r0 = n0 = 0
     new = scale = None
     if residual is not None:
-        p_res = _matrix(where, "residual", residual, (x.dtype, torch.float32), tokens, dim, device)
+        p_res, r0 = _matrix(where, "residual", residual, (dtype, torch.float32), tokens, dim, device)
+        res_code = code if residual.dtype is dtype else 4
         if in_place:
             _apart(where, "residual", residual)
-        new = residual if in_place else torch.empty_like(residual, memory_format=torch.contiguous_format)
-        p_new, code, r0, n0 = new.data_ptr(), DTYPE_CODES[residual.dtype], residual.stride(0), new.stride(0)
+            new, p_new, n0 = residual, p_res, r0
+        else:
+            new = torch.empty_like(residual, memory_format=torch.contiguous_format)
+            p_new, n0 = new.data_ptr(), dim
     elif in_place:
         _refuse(where, "in_place is for a residual")
-    for t in (x, after, gate, residual, before, out):
-        if t is not None and t.requires_grad:
-            _no_gradient(where)
+    if x.requires_grad or (after is not None and after.requires_grad) or (gate is not None and gate.requires_grad) or \
+            (residual is not None and residual.requires_grad) or (before is not None and before.requires_grad) or \
+            (out is not None and out.requires_grad):
+        _no_gradient(where)
+    kind = torch.int8 if int8 else dtype
     if out is None:
-        out = torch.empty((tokens, dim), dtype=torch.int8 if int8 else x.dtype, device=device)
+        out = torch.empty((tokens, dim), dtype=kind, device=device)
+        p_out, o0 = out.data_ptr(), dim
     else:
-        _matrix(where, "out", out, (torch.int8 if int8 else x.dtype,), tokens, dim, device)
+        p_out, o0 = _matrix(where, "out", out, (kind,), tokens, dim, device)
         _apart(where, "out", out)
     if int8:
         scale = torch.empty(tokens, dtype=torch.float32, device=device)
+        p_scale = scale.data_ptr()
     if tokens and dim:
         kvr_block_norm(
-            NORM_RECORD.pack(NORM_RECORD.size, DTYPE_CODES[x.dtype], code, DTYPE_CODES[out.dtype], tokens, dim,
+            NORM_RECORD.pack(NORM_RECORD.size, code, res_code, 3 if int8 else code, tokens, dim,
                              ACTIVATIONS[activation], eps, residual_scale, 0, p_x, p_after, p_gate, p_res, p_before,
-                             p_new, out.data_ptr(), scale.data_ptr() if int8 else 0, x.stride(0),
-                             gate.stride(0) if p_gate else 0, r0, n0, out.stride(0)),
+                             p_new, p_out, p_scale, x0, g0, r0, n0, o0),
             _stream(device.index))
     return BlockNorm(out, new, scale)
 
@@ -142,9 +152,9 @@ def integer_product(x: torch.Tensor, weight: torch.Tensor, weight_scale: torch.T
         with torch.cuda.device(device):
             return integer_product(x, weight, weight_scale, x_scale=x_scale, bias=bias, dtype=dtype, out=out)
     int8 = x.dtype is torch.int8
-    p_x = _matrix(where, "x", x, (torch.int8, *HALVES), None, None, device)
+    p_x, x0 = _matrix(where, "x", x, PRODUCT_TYPES, None, None, device)
     tokens, dim = x.shape
-    p_w = _matrix(where, "weight", weight, (torch.int8,), None, dim, device)
+    p_w, w0 = _matrix(where, "weight", weight, (torch.int8,), None, dim, device)
     channels = weight.shape[0]
     if int8 != (x_scale is not None):
         _refuse(where, "x_scale goes with x of torch.int8")
@@ -152,26 +162,30 @@ def integer_product(x: torch.Tensor, weight: torch.Tensor, weight_scale: torch.T
     p_xs = _vector(where, "x_scale", x_scale, f32, tokens, device) if int8 else 0
     p_ws = _vector(where, "weight_scale", weight_scale, f32, channels, device)
     p_bias = 0 if bias is None else _vector(where, "bias", bias, f32, channels, device)
-    for t in (x, weight_scale, x_scale, bias, out):
-        if t is not None and t.requires_grad:
-            _no_gradient(where)
+    if x.requires_grad or weight_scale.requires_grad or (int8 and x_scale.requires_grad) or \
+            (bias is not None and bias.requires_grad) or (out is not None and out.requires_grad):
+        _no_gradient(where)
     if dtype is None:
         dtype = out.dtype if out is not None else torch.bfloat16 if int8 else x.dtype
-    if dtype not in HALVES and dtype is not f32:
+    code, to = DTYPE_CODES[x.dtype], DTYPE_CODES.get(dtype, 3)
+    if to == 3:
         _refuse(where, f"a result of {dtype} is not supported (bfloat16, float16, float32)")
     if out is None:
         out = torch.empty((tokens, channels), dtype=dtype, device=device)
+        p_out, o0 = out.data_ptr(), channels
     else:
-        _matrix(where, "out", out, (dtype,), tokens, channels, device)
+        p_out, o0 = _matrix(where, "out", out, (dtype,), tokens, channels, device)
         _apart(where, "out", out)
-    code, to = DTYPE_CODES[x.dtype], DTYPE_CODES[dtype]
     nbytes = _product_bytes(code, to, tokens, dim, channels)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    p_work = 0
+    if nbytes:
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        p_work = ws.data_ptr()
     if tokens:
         kvr_integer_product(
-            PRODUCT_RECORD.pack(PRODUCT_RECORD.size, code, to, tokens, dim, channels, p_x, p_w, out.data_ptr(), p_xs,
-                                p_ws, p_bias, x.stride(0), weight.stride(0), out.stride(0)),
-            ws.data_ptr() if nbytes else 0, nbytes, _stream(device.index))
+            PRODUCT_RECORD.pack(PRODUCT_RECORD.size, code, to, tokens, dim, channels, p_x, p_w, p_out, p_xs, p_ws,
+                                p_bias, x0, w0, o0),
+            p_work, nbytes, _stream(device.index))
     return out
 
 

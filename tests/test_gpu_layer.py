@@ -192,6 +192,13 @@ def test_product_types(dtype, out, tokens):
     check_product(product_problem(tokens, 336, 260, dtype, bias=tokens == 9), out)
 
 
+@pytest.mark.parametrize("tokens,dim", [(1, 16), (7, 65536), (1, 65536), (2, 32784), (16, 4096), (16, 4112), (17, 64),
+                                        (15, 1040)])
+@pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
+def test_product_of_few_tokens(tokens, dim, dtype):
+    check_product(product_problem(tokens, dim, 67, dtype, bias=True), F32)
+
+
 def test_product_of_the_largest_sums():
     # 65,536 times (-128)^2 = 2^30, and both signs
     w = torch.full((40, 65536), -128, dtype=torch.int8)
@@ -232,6 +239,8 @@ def test_product_of_odd_tokens():
     ws[5] = NAN
     got = check_product((x, None, w, ws, None), BF16)
     assert (got[0, :5] == 0).all() and got[1].isnan().all() and got[69].isnan().all() and got[:, 5].isnan().all()
+    got = check_product((x[:9], None, w, ws, None), BF16)
+    assert (got[0, :5] == 0).all() and got[1].isnan().all() and got[2:, :5].isfinite().all()
 
 
 def test_product_of_no_token():

@@ -154,9 +154,12 @@ def test_linear_buffers_refused(bad):
 
 
 def test_small_or_missing_workspaces_refused():
-    halves = dict(dtype=0, d_x_scale=0)
+    halves = dict(dtype=0, d_x_scale=0, num_tokens=20)
     assert K.kvr_product_workspace(product()) == 0
-    assert K.kvr_product_workspace(product(**halves)) >= 5 * 64 + 20
+    assert K.kvr_product_workspace(product(**halves)) >= 20 * 64 + 80
+    few = dict(halves, num_tokens=16)  # every workgroup brings these to integers itself
+    assert K.kvr_product_workspace(product(**few)) == 0
+    assert K.kvr_product_workspace(product(**few, dim=8192)) >= 16 * 8192 + 64
     _refused(lambda: K.kvr_integer_product(product(**halves), 0, 1 << 20))
     _refused(lambda: K.kvr_integer_product(product(**halves), P + 8, 1 << 20))
     _refused(lambda: K.kvr_integer_product(product(**halves), P, 64), K.KVR_ENOMEM)
