@@ -25,8 +25,8 @@ typedef int i32x16 __attribute__((ext_vector_type(16)));
 constexpr int kStep = 64;   // elements of k that a tile holds
 constexpr int kXcds = 8;    // workgroups go to them in turn
 
-// What is read in the place of elements behind the last one.
-__device__ const uint32_t kZeros[4] = {0, 0, 0, 0};
+// What is read in the place of (16) elements behind the last one.
+__device__ const uint32_t kZeros[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 
 template <class T, int N>
 struct Some {
@@ -273,20 +273,6 @@ __global__ __launch_bounds__(64 * kDirectWaves) void product_direct_kernel(Produ
     }
     __syncthreads();
   }
-  // 16 elements of a token, as integers
-  auto integers = [&](int t, int k) {
-    if constexpr (kInts) {
-      return *(const i32x4*)(x_from[t] + k);
-    } else {
-      Some<X, 16> x;
-      __builtin_memcpy(&x, x_from[t] + k * 2, sizeof(x));
-      const float b = by[min(t * 16 + n, a.tokens - t0 - 1)];
-      Some<int8_t, 16> q;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) q.e[e] = Quantiser::integer((float)x.e[e], b);
-      return __builtin_bit_cast(i32x4, q);
-    }
-  };
   auto step = [&](int k0, auto whole) {
     i32x4 w[CT][4], x[TT][4];
 #pragma unroll
@@ -295,12 +281,26 @@ __global__ __launch_bounds__(64 * kDirectWaves) void product_direct_kernel(Produ
       const bool there = whole.value || k < a.dim;
 #pragma unroll
       for (int c = 0; c < CT; ++c) w[c][j] = *(const i32x4*)(there ? w_from[c] + k : (const char*)kZeros);
+      if constexpr (kInts) {
+#pragma unroll
+        for (int t = 0; t < TT; ++t) x[t][j] = *(const i32x4*)(there ? x_from[t] + k : (const char*)kZeros);
+      }
     }
+    if constexpr (!kInts) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int k = k0 + g * 64 + j * 16;
+      for (int j = 0; j < 4; ++j) {
+        const int k = k0 + g * 64 + j * 16;
 #pragma unroll
-      for (int t = 0; t < TT; ++t) x[t][j] = whole.value || k < a.dim ? integers(t, k) : i32x4{0, 0, 0, 0};
+        for (int t = 0; t < TT; ++t) {
+          Some<X, 16> y;
+          __builtin_memcpy(&y, whole.value || k < a.dim ? x_from[t] + k * 2 : (const char*)kZeros, sizeof(y));
+          const float b = by[min(t * 16 + n, a.tokens - t0 - 1)];
+          Some<int8_t, 16> q;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) q.e[e] = Quantiser::integer((float)y.e[e], b);
+          x[t][j] = __builtin_bit_cast(i32x4, q);
+        }
+      }
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j)
