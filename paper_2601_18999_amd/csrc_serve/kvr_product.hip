@@ -225,18 +225,16 @@ __global__ __launch_bounds__(64 * WC * WT, FC * FT > 8 ? 1 : 2) void product_ker
 // Few results: a workgroup has CT * 16 channels and TT * 16 tokens, and its
 // waves have k in turn, 256 elements at a time, from memory straight to the
 // registers that the matrix instructions take them from; their sums are added
-// in LDS.  (Lane l of a wave reads 64 neighbouring bytes of row l % 16: a
-// product takes 16 of them, so its slots stand for elements 64 (l / 16) + 16 j
-// .. of both operands.)
+// in LDS.  Four lanes read 64 neighbouring bytes of a row in one load (16 bytes
+// of each 64 a lane, all four in loads of their own, took 27 instead of 14.6 us
+// for 8 tokens x 16,384 channels, k = 4,096).
 //
 // X: int8_t, or the type of few tokens of 16 bits, which each workgroup brings
-// to integers for itself: its waves take the rows' largest magnitudes first
-// (8 tokens x 8,192 channels, k = 4,096: 15.4 us with a launch for that).
-constexpr int kDirectWaves = 8;
+// to integers for itself: its waves take the rows' largest magnitudes first.
 constexpr int kDirectStep = 256;
 
-template <class T, class X, int CT, int TT>
-__global__ __launch_bounds__(64 * kDirectWaves) void product_direct_kernel(ProductArgs a, uint32_t across) {
+template <class T, class X, int CT, int TT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void product_direct_kernel(ProductArgs a, uint32_t across) {
   constexpr int kPitch = CT * 64 + 16, kWave = TT * 16 * kPitch;
   constexpr bool kInts = sizeof(X) == 1;
   extern __shared__ __align__(16) char lds[];
@@ -255,7 +253,7 @@ __global__ __launch_bounds__(64 * kDirectWaves) void product_direct_kernel(Produ
 #pragma unroll
     for (int t = 0; t < TT; ++t) sum[c][t] = i32x4{0, 0, 0, 0};
   if constexpr (!kInts) {
-    for (int t = wave; t < min(TT * 16, a.tokens - t0); t += kDirectWaves) {
+    for (int t = wave; t < min(TT * 16, a.tokens - t0); t += WAVES) {
       const char* row = a.x + (t0 + t) * a.x_tok;
       uint32_t top = 0;
 #pragma unroll 4
@@ -277,7 +275,7 @@ __global__ __launch_bounds__(64 * kDirectWaves) void product_direct_kernel(Produ
     i32x4 w[CT][4], x[TT][4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int k = k0 + g * 64 + j * 16;
+      const int k = k0 + j * 64 + g * 16;
       const bool there = whole.value || k < a.dim;
 #pragma unroll
       for (int c = 0; c < CT; ++c) w[c][j] = *(const i32x4*)(there ? w_from[c] + k : (const char*)kZeros);
@@ -289,7 +287,7 @@ __global__ __launch_bounds__(64 * kDirectWaves) void product_direct_kernel(Produ
     if constexpr (!kInts) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int k = k0 + g * 64 + j * 16;
+        const int k = k0 + j * 64 + g * 16;
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
           Some<X, 16> y;
@@ -311,7 +309,7 @@ __global__ __launch_bounds__(64 * kDirectWaves) void product_direct_kernel(Produ
           sum[c][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[c][j], x[t][j], sum[c][t], 0, 0, 0);
   };
   int k0 = wave * kDirectStep;
-  for (; k0 + kDirectStep <= a.dim; k0 += kDirectWaves * kDirectStep) step(k0, std::true_type());
+  for (; k0 + kDirectStep <= a.dim; k0 += WAVES * kDirectStep) step(k0, std::true_type());
   if (k0 < a.dim) step(k0, std::false_type());
 #pragma unroll
   for (int c = 0; c < CT; ++c)
@@ -319,12 +317,12 @@ __global__ __launch_bounds__(64 * kDirectWaves) void product_direct_kernel(Produ
     for (int t = 0; t < TT; ++t)
       *(i32x4*)(lds + wave * kWave + (t * 16 + n) * kPitch + c * 64 + g * 16) = sum[c][t];
   __syncthreads();
-  for (int i = threadIdx.x; i < TT * 16 * CT * 4; i += 64 * kDirectWaves) {
+  for (int i = threadIdx.x; i < TT * 16 * CT * 4; i += 64 * WAVES) {
     const int token = t0 + i / (CT * 4), channel = c0 + i % (CT * 4) * 4;
     if (token >= a.tokens || channel >= a.channels) continue;
     i32x4 all = {0, 0, 0, 0};
 #pragma unroll
-    for (int v = 0; v < kDirectWaves; ++v)
+    for (int v = 0; v < WAVES; ++v)
       all += *(const i32x4*)(lds + v * kWave + i / (CT * 4) * kPitch + i % (CT * 4) * 16);
     const float x_scale = kInts ? a.x_scale[token] : scales[token - t0];
     float f[4];
@@ -365,26 +363,38 @@ hipError_t launch_tiles(const ProductArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <class T, class X, int CT, int TT>
+template <class T, class X, int CT, int TT, int WAVES>
 hipError_t launch_direct(const ProductArgs& a, hipStream_t st) {
-  constexpr int bytes = kDirectWaves * TT * 16 * (CT * 64 + 16);
-  const hipError_t e = allow_lds<product_direct_kernel<T, X, CT, TT>>(bytes);
+  constexpr int bytes = WAVES * TT * 16 * (CT * 64 + 16);
+  const hipError_t e = allow_lds<product_direct_kernel<T, X, CT, TT, WAVES>>(bytes);
   if (e != hipSuccess) return e;
   const uint32_t across = (uint32_t)((a.channels + CT * 16 - 1) / (CT * 16));
   const uint32_t down = (uint32_t)((a.tokens + TT * 16 - 1) / (TT * 16));
-  product_direct_kernel<T, X, CT, TT><<<across * down, 64 * kDirectWaves, bytes, st>>>(a, across);
+  product_direct_kernel<T, X, CT, TT, WAVES><<<across * down, 64 * WAVES, bytes, st>>>(a, across);
   return hipGetLastError();
 }
 
-// Which kernel, by what they take (bfloat16 results, k = 4,096, us):
-//   tokens x channels    direct 16 x 16   direct 64 x 32   tiles of 64   128   256
-//        8 x  8,192            8.6              8.7            15.8     25.8   56
-//       64 x  8,192           31.6             14.1            16.2     26.6   57
-//      128 x  8,192           60.6             25.2            16.5     27.8   59
-//      512 x  4,096          115               46              19.3     27.9   61
-//      256 x 16,384          274               99              41.7     29.2   62
-//    1,024 x  8,192          465              179              75.8     47.0   63
-//    2,048 x  8,192                                                    102.8   76
+// Few tokens: twice 16 channels a workgroup where there are enough for the
+// device.
+template <class T, class X>
+hipError_t launch_few(const ProductArgs& a, hipStream_t st) {
+  if (a.channels > 32 * (kComputeUnits - 1)) return launch_direct<T, X, 2, 1, 16>(a, st);
+  return launch_direct<T, X, 1, 1, 8>(a, st);
+}
+
+// Which kernel, by what they take (8-bit tokens, bfloat16 results, us; direct
+// kernels by tokens x channels of a workgroup):
+//   tokens x k x channels    direct 16x16  16x32  64x16  64x32   tiles of 64   128   256
+//        8 x  4,096 x  4,096      7.4       9.6    7.5    8.7        15.4
+//        8 x  4,096 x 16,384     18.4      14.6   22.5   15.1        15.8
+//       16 x 16,384 x  8,192     35.1      31.6   43.7   34.6        54.5
+//       40 x  4,096 x  4,096     12.3      12.3    9.6   11.4        15.6
+//       64 x  4,096 x  8,192     30.7      24.3   21.7   13.6        16.0   26.6    57
+//      333 x  5,008 x  1,001     23.1      16.2   22.8   11.9        18.9
+//      512 x  4,096 x  4,096                             46          19.3   27.9    61
+//      256 x  4,096 x 16,384                             99          41.7   29.2    62
+//    1,024 x  4,096 x  8,192                            179          75.8   47.0    63
+//    2,048 x  4,096 x  8,192                                               102.8    76
 // The direct kernels are taken as long as one round of workgroups does it (up
 // to 16 tokens, which weights bound, always); of the tiles those that are done
 // first, by the time of a step of k where a compute unit has one workgroup, or
@@ -394,10 +404,11 @@ hipError_t launch(const ProductArgs& a, hipStream_t st) {
   auto count = [&](int tokens, int channels) {
     return (int64_t)((a.tokens + tokens - 1) / tokens) * ((a.channels + channels - 1) / channels);
   };
-  if (a.dtype == KVR_BF16) return launch_direct<T, __bf16, 1, 1>(a, st);
-  if (a.dtype == KVR_FP16) return launch_direct<T, _Float16, 1, 1>(a, st);
-  if (a.tokens <= 16) return launch_direct<T, int8_t, 1, 1>(a, st);
-  if (count(64, 32) <= kComputeUnits) return launch_direct<T, int8_t, 2, 4>(a, st);
+  if (a.dtype == KVR_BF16) return launch_few<T, __bf16>(a, st);
+  if (a.dtype == KVR_FP16) return launch_few<T, _Float16>(a, st);
+  if (a.tokens <= 16) return launch_few<T, int8_t>(a, st);
+  if (count(64, 16) <= kComputeUnits) return launch_direct<T, int8_t, 1, 4, 16>(a, st);
+  if (count(64, 32) <= kComputeUnits) return launch_direct<T, int8_t, 2, 4, 8>(a, st);
   auto step_ns = [&](int tile, int alone, int each) {
     const int64_t rounds = (count(tile, tile) + kComputeUnits - 1) / kComputeUnits;
     return rounds * each > alone ? rounds * each : alone;
