@@ -56,7 +56,8 @@ struct Segment {
 };
 
 struct LinearHdr {
-  int32_t segments, rejected;
+  int32_t segments, followed;  // in all, and such that another one follows
+  int32_t rejected;
 };
 
 struct LinearArgs {

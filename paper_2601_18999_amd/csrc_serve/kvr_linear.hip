@@ -58,19 +58,19 @@ __device__ void fill_nan(const LinearArgs& a, int row0, int rows, int head, int 
   }
 }
 
-// Checks row_start and lists the segments, the longest first (the workgroups
-// that start last then have little to do): one workgroup.
+// Checks row_start and lists the segments: those that others follow, which are
+// full, then the last ones, the longest first (the workgroups that start last
+// then have little to do).  One workgroup.
 __global__ __launch_bounds__(kThreads) void linear_plan_kernel(LinearArgs a) {
   constexpr int kKinds = 64;  // by chunks, the last one all longer ones
-  __shared__ int place[kKinds], slots;
+  __shared__ int place[kKinds], followed, slots;
   const int tid = threadIdx.x;
   if (tid < kKinds) place[tid] = 0;
-  if (tid == 0) slots = 0;
+  if (tid == 0) followed = slots = 0;
   __syncthreads();
   auto kind = [&](int rows) { return kKinds - 1 - min((rows + kChunk - 1) / kChunk, kKinds - 1); };
   int bad = 0;
-  // A request's segments: all but the last are full.  Those of a few tokens
-  // are not listed (linear_steps_kernel takes them).
+  // (requests of a few tokens are not listed: linear_steps_kernel takes them)
   auto each = [&](auto found) {
     for (int r = tid; r < a.requests; r += kThreads) {
       const int from = a.row_start[r], to = a.row_start[r + 1];
@@ -81,11 +81,14 @@ __global__ __launch_bounds__(kThreads) void linear_plan_kernel(LinearArgs a) {
     }
   };
   each([&](int, int, int rows, int parts) {
-    if (parts > 1) atomicAdd(&place[kind(a.segment)], parts - 1);
+    if (parts > 1) atomicAdd(&followed, parts - 1);
     atomicAdd(&place[kind(rows - (parts - 1) * a.segment)], 1);
   });
   bad = __syncthreads_or(bad);
   int all = 0;
+  const int first = followed;
+  __syncthreads();
+  if (tid == 0) followed = 0;
   if (tid < kKinds) {
     const int mine = place[tid];
     int sum = mine;
@@ -94,18 +97,18 @@ __global__ __launch_bounds__(kThreads) void linear_plan_kernel(LinearArgs a) {
       const int x = __shfl_up(sum, d);
       if (tid >= d) sum += x;
     }
-    place[tid] = sum - mine;
-    all = sum;
+    place[tid] = first + sum - mine;
+    all = first + sum;
   }
   __syncthreads();
   if (tid == kKinds - 1) {
-    *a.hdr = {all, bad};
+    *a.hdr = {all, first, bad};
     if (bad && a.status) atomicOr(a.status, (uint32_t)KVR_DEV_BAD_LENGTH);
   }
   if (bad) return;
   each([&](int r, int from, int rows, int parts) {
     const int slot = parts > 1 ? atomicAdd(&slots, parts) : 0;
-    const int full = parts > 1 ? atomicAdd(&place[kind(a.segment)], parts - 1) : 0;
+    const int full = parts > 1 ? atomicAdd(&followed, parts - 1) : 0;
     for (int i = 0; i < parts - 1; ++i)
       a.segments[full + i] = {r, from + i * a.segment, a.segment, i, parts, slot, 0, 0};
     const int rest = rows - (parts - 1) * a.segment;
@@ -377,10 +380,9 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
       for (int t = (int)at; t < a.tokens; t += a.segment_cap) fill_nan<typename T::Type>(a, t, 1, head, D);
     return;
   }
-  if ((int)at >= a.hdr->segments) return;
+  if ((int)at >= (OUT ? a.hdr->segments : a.hdr->followed)) return;
   const Segment seg = a.segments[at];
   const bool last = seg.index == seg.parts - 1;
-  if (!OUT && last) return;
   int read, write;
   if (!slots_fit(a, seg.request, read, write)) {
     if (OUT) fill_nan<typename T::Type>(a, seg.row0, seg.rows, head, D);
@@ -701,10 +703,10 @@ template <int D>
 __global__ __launch_bounds__(kThreads) void linear_states_kernel(LinearArgs a) {
   if (a.hdr->rejected) return;
   const uint32_t at = divide(blockIdx.x, a.kv_div);
-  if ((int)at >= a.hdr->segments) return;
+  if ((int)at >= a.hdr->followed) return;
   const int head = (int)(blockIdx.x - at * a.kv_div.d);
   const Segment seg = a.segments[at];
-  if (seg.index || seg.parts == 1) return;
+  if (seg.index) return;
   const int read = a.read[seg.request];
   if (read < -1 || read >= a.slots) return;  // (reported by linear_chunks_kernel)
   const int64_t place = ((int64_t)blockIdx.y * kThreads + threadIdx.x) * 4;
@@ -740,11 +742,11 @@ hipError_t allow_lds(int bytes) {
 }
 
 template <int D, class T, bool OUT>
-hipError_t launch_chunks(const LinearArgs& a, hipStream_t st) {
+hipError_t launch_chunks(const LinearArgs& a, int segments, hipStream_t st) {
   constexpr int bytes = ChunkLds<D, T, OUT>::kBytes;
   const hipError_t e = allow_lds<linear_chunks_kernel<D, T, OUT>>(bytes);
   if (e != hipSuccess) return e;
-  linear_chunks_kernel<D, T, OUT><<<(uint32_t)a.segment_cap * (uint32_t)a.kv_heads, kThreads, bytes, st>>>(a);
+  linear_chunks_kernel<D, T, OUT><<<(uint32_t)segments * (uint32_t)a.kv_heads, kThreads, bytes, st>>>(a);
   return hipGetLastError();
 }
 
@@ -753,13 +755,14 @@ hipError_t launch(const LinearArgs& a, hipStream_t st) {
   hipError_t e = hipSuccess;
   if (a.row_start && a.tokens > a.few) {
     if (a.tokens > a.segment) {
-      e = launch_chunks<D, T, false>(a, st);
+      const int most = a.tokens / a.segment;  // segments that others follow
+      e = launch_chunks<D, T, false>(a, most, st);
       if (e != hipSuccess) return e;
-      linear_states_kernel<D><<<dim3((uint32_t)a.segment_cap * (uint32_t)a.kv_heads, D * D / 4 / kThreads), kThreads, 0, st>>>(a);
+      linear_states_kernel<D><<<dim3((uint32_t)most * (uint32_t)a.kv_heads, D * D / 4 / kThreads), kThreads, 0, st>>>(a);
       e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
-    e = launch_chunks<D, T, true>(a, st);
+    e = launch_chunks<D, T, true>(a, a.segment_cap, st);
     if (e != hipSuccess) return e;
   }
   if (a.few < 0) return hipSuccess;
