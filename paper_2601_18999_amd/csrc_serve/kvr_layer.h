@@ -77,6 +77,7 @@ struct LinearArgs {
   Divisor kv_div;                                                     // by kv_heads
   int32_t tokens, requests, heads, kv_heads, share, dim, slots;
   int32_t segment, segment_cap;
+  int32_t teams;  // of a segment's key head, which share its queries' heads: 1 or share
   int32_t few;  // requests of up to so many tokens take the recurrent form (-1: none)
   float scale;
 };

@@ -376,7 +376,7 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
   const uint32_t at = divide(blockIdx.x, a.kv_div);
   const int head = (int)(blockIdx.x - at * a.kv_div.d);
   if (a.hdr->rejected) {  // (with few >= 0 linear_steps_kernel writes the results)
-    if (OUT && a.few < 0)
+    if (OUT && a.few < 0 && blockIdx.y == 0)
       for (int t = (int)at; t < a.tokens; t += a.segment_cap) fill_nan<typename T::Type>(a, t, 1, head, D);
     return;
   }
@@ -384,10 +384,18 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
   const Segment seg = a.segments[at];
   const bool last = seg.index == seg.parts - 1;
   int read, write;
+  const int team = OUT ? (int)blockIdx.y : 0;
   if (!slots_fit(a, seg.request, read, write)) {
-    if (OUT) fill_nan<typename T::Type>(a, seg.row0, seg.rows, head, D);
+    if (OUT && team == 0) fill_nan<typename T::Type>(a, seg.row0, seg.rows, head, D);
     return;
   }
+  // The queries' heads of the key head; with several teams each has its share
+  // of them, and all keep the state.  (Where a request's state is read and
+  // written in one place, one team has all heads: it could be written before
+  // another has read it.)
+  const int teams = seg.parts == 1 && read == write ? 1 : OUT ? a.teams : 1;
+  if (team >= teams) return;
+  const int s0 = a.share / teams * team, s1 = s0 + a.share / teams;
   const float g = a.log_decay[head];
   // d^m; a decay of 0 has d^0 = 1
   auto decay_by = [&](int m) { return m ? expf(g * (float)m) : 1.0f; };
@@ -413,7 +421,7 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
   if (tid < kChunk) power[tid] = decay_by(tid + 1);
 
   const int chunks = (seg.rows + kChunk - 1) / kChunk;
-  const int q_head0 = head * a.share;
+  const int q_head0 = head * a.share + s0;
   const char* k_from = Tile<D>::lane(a.k + seg.row0 * a.k_tok + head * a.k_head, a.k_tok, tid);
   const char* v_from = Tile<D>::lane(a.v + seg.row0 * a.v_tok + head * a.v_head, a.v_tok, tid);
   const char* q_from = Tile<D>::lane(a.q + seg.row0 * a.q_tok + q_head0 * a.q_head, a.q_tok, tid);
@@ -462,14 +470,14 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
     const int v_place = column_place<D, false>(lane) + c * 64;
     if constexpr (OUT) {
 #pragma unroll 1
-      for (int s = 0; s < a.share; ++s) {
+      for (int s = 0; s < s1 - s0; ++s) {
         if (s) __syncthreads();
         // (nor are the state's parts kept over this loop)
 #pragma unroll
         for (int t = 0; t < kGroups; ++t) asm volatile("" : "+v"(state[t]));
         asm volatile("" : "+v"(lane), "+v"(n), "+v"(h), "+v"(tid));
         tq.template store_parts<T>(queries, tid);
-        if (s + 1 < a.share)
+        if (s + 1 < s1 - s0)
           tq.fetch(q_from + (s + 1) * a.q_head, a.q_tok, rows, tid);
         else
           fetch_next();
@@ -686,7 +694,7 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
   float* to = nullptr;
   if (!OUT)
     to = a.added + ((int64_t)(seg.slot + seg.index + 1) * a.kv_heads + head) * D * D;
-  else if (last && write >= 0 && (seg.rows || write != read))
+  else if (team == 0 && last && write >= 0 && (seg.rows || write != read))
     to = a.state + write * a.state_slot + head * a.state_head;
   if (to && rw == 0) {
 #pragma unroll
@@ -746,7 +754,7 @@ hipError_t launch_chunks(const LinearArgs& a, int segments, hipStream_t st) {
   constexpr int bytes = ChunkLds<D, T, OUT>::kBytes;
   const hipError_t e = allow_lds<linear_chunks_kernel<D, T, OUT>>(bytes);
   if (e != hipSuccess) return e;
-  linear_chunks_kernel<D, T, OUT><<<(uint32_t)segments * (uint32_t)a.kv_heads, kThreads, bytes, st>>>(a);
+  linear_chunks_kernel<D, T, OUT><<<dim3((uint32_t)segments * (uint32_t)a.kv_heads, OUT ? a.teams : 1), kThreads, bytes, st>>>(a);
   return hipGetLastError();
 }
 
