@@ -144,13 +144,11 @@ __global__ __launch_bounds__(64 * WC * WT, FC * FT > 8 ? 1 : 2) void product_ker
     __builtin_amdgcn_sched_group_barrier(kReads, FC + FT, 0);
   };
   auto multiply = [&](int k) {
-    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int c = 0; c < FC; ++c)
 #pragma unroll
       for (int t = 0; t < FT; ++t)
         sum[c][t] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[k][c], x[k][t], sum[c][t], 0, 0, 0);
-    __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_group_barrier(kProducts, FC * FT, 0);
   };
   // scales and biases, for the end: 64 values a load
