@@ -34,9 +34,18 @@ struct ProductArgs {
   int32_t dtype;  // of x: KVR_INT8, or of few tokens that are not brought to integers yet
 };
 
-// So few elements of 16 bits are brought to integers by every workgroup of the
-// product for itself, of at most 16 tokens.
-constexpr int kFewElements = 1 << 16;
+// Tiles of so many tokens and channels.
+inline int64_t product_tiles(int64_t tokens, int64_t channels, int tile_tokens, int tile_channels) {
+  return (tokens + tile_tokens - 1) / tile_tokens * ((channels + tile_channels - 1) / tile_channels);
+}
+
+// Whether tokens of 16 bits are brought to integers by every workgroup of the
+// product for itself: where they are few elements, and the product is of one
+// round of workgroups or of up to 16 tokens (25 tokens x 128 x 1,408: 12.8 us
+// with a launch for that, which the host takes).
+inline bool quantised_within(int tokens, int dim, int channels) {
+  return (int64_t)tokens * dim <= 1 << 16 && (tokens <= 16 || product_tiles(tokens, channels, 64, 32) <= kComputeUnits);
+}
 
 // ---- linear attention ----
 // Requests of up to so many tokens take the recurrent form; where a request has
@@ -44,6 +53,9 @@ constexpr int kFewElements = 1 << 16;
 // less is done).
 constexpr int kFewTokens = 4;
 constexpr int kManyTokens = 32;
+// So many requests of which none is cut are not planned for: every workgroup
+// checks row_start.
+constexpr int kUnplanned = 256;
 // Workgroups of the chunked form that the device holds.
 constexpr int kLinearSlots = 2 * kComputeUnits;
 
@@ -78,6 +90,7 @@ struct LinearArgs {
   int32_t tokens, requests, heads, kv_heads, share, dim, slots;
   int32_t segment, segment_cap;
   int32_t teams;  // of a segment's key head, which share its queries' heads: 1 or share
+  int32_t planned;
   int32_t few;  // requests of up to so many tokens take the recurrent form (-1: none)
   float scale;
 };

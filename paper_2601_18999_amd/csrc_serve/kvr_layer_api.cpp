@@ -60,7 +60,7 @@ kvr_status check(const kvr_product* p) {
 
 // Whether 16-bit tokens go through the workspace, as integers.
 bool quantised_first(const kvr_product* p) {
-  return p->dtype != KVR_INT8 && (p->num_tokens > 16 || (int64_t)p->num_tokens * p->dim > kvr::kFewElements);
+  return p->dtype != KVR_INT8 && !kvr::quantised_within(p->num_tokens, p->dim, p->channels);
 }
 
 size_t product_bytes(const kvr_product* p) {
@@ -87,6 +87,7 @@ kvr_status check(const kvr_linear* l) {
 struct LinearLayout {
   size_t segments, added, bytes;
   int32_t segment, segment_cap;
+  bool planned;
 };
 
 // Segments of equal length, as many as the device holds workgroups (one takes
@@ -99,7 +100,8 @@ kvr_status lay_out(const kvr_linear* l, LinearLayout* o) {
   const int64_t slots = (int64_t)l->num_requests * l->kv_heads < kvr::kLinearSlots ? kvr::kLinearSlots : kvr::kLinearSlots / 2;
   const int64_t even = (tokens * l->kv_heads + slots - 1) / slots;
   const int64_t segment = even > 256 ? (even + 63) / 64 * 64 : 256;
-  const int64_t cap = l->num_requests + (l->d_row_start ? tokens / segment : 0);
+  const bool cut = l->d_row_start && tokens > segment;  // whether there can be a request of several segments
+  const int64_t cap = l->num_requests + (cut ? tokens / segment : 0);
   // (a launch has fewer than 2^32 threads)
   if (cap * l->kv_heads >= 1 << 24)
     return invalid("too many requests and heads for one launch: num_requests * kv_heads must be below 2^24 - 512");
@@ -108,8 +110,10 @@ kvr_status lay_out(const kvr_linear* l, LinearLayout* o) {
   o->segments = 256;
   o->added = 256 + round_up((size_t)cap * sizeof(kvr::Segment));
   // a request of several segments has at most twice as many as full ones
-  const size_t states = tokens > segment ? 2 * (size_t)(tokens / segment) : 0;
-  o->bytes = l->d_row_start ? o->added + states * l->kv_heads * l->dim * l->dim * 4 : 0;
+  const size_t states = cut ? 2 * (size_t)(tokens / segment) : 0;
+  // (without a plan a request has one segment: as many workgroups for a key head as requests)
+  o->planned = cut || (l->d_row_start && l->num_requests > kvr::kUnplanned);
+  o->bytes = o->planned ? o->added + states * l->kv_heads * l->dim * l->dim * 4 : 0;
   return KVR_OK;
 }
 
@@ -277,6 +281,7 @@ kvr_status kvr_linear_attention(const kvr_linear* l, void* d_workspace, size_t b
   a.slots = l->num_slots;
   a.segment = o.segment;
   a.segment_cap = o.segment_cap;
+  a.planned = o.planned;
   // a device that would be half empty takes the queries' heads side by side,
   // though each keeps the state (33 requests of up to 77 tokens, 15 / 5 heads:
   // 27.7 -> 22 us)

@@ -58,6 +58,20 @@ __device__ void fill_nan(const LinearArgs& a, int row0, int rows, int head, int 
   }
 }
 
+// Whether row_start is not valid: of the plan, or, where there is none (few
+// requests, none of which is cut), checked by every workgroup.
+__device__ __forceinline__ bool rejected(const LinearArgs& a) {
+  if (a.planned) return a.hdr->rejected;
+  int bad = 0;
+  for (int r = threadIdx.x; r < a.requests; r += kThreads) {
+    const int from = a.row_start[r], to = a.row_start[r + 1];
+    bad |= from < 0 || to < from || to > a.tokens;
+  }
+  bad = __syncthreads_or(bad);
+  if (bad && a.status && threadIdx.x == 0) atomicOr(a.status, (uint32_t)KVR_DEV_BAD_LENGTH);
+  return bad;
+}
+
 // Checks row_start and lists the segments: those that others follow, which are
 // full, then the last ones, the longest first (the workgroups that start last
 // then have little to do).  One workgroup.
@@ -129,7 +143,7 @@ __global__ __launch_bounds__(kThreads) void linear_steps_kernel(LinearArgs a) {
   const int head = (int)(blockIdx.x - at * a.kv_div.d);
   int row0 = (int)at, rows = 1;
   if (a.row_start) {
-    if (a.hdr->rejected) {
+    if (rejected(a)) {
       for (int t = (int)at; t < a.tokens; t += a.requests) fill_nan<T>(a, t, 1, head, D);
       return;
     }
@@ -375,14 +389,20 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = wave % kGroups, rw = wave / kGroups;
   const uint32_t at = divide(blockIdx.x, a.kv_div);
   const int head = (int)(blockIdx.x - at * a.kv_div.d);
-  if (a.hdr->rejected) {  // (with few >= 0 linear_steps_kernel writes the results)
+  if (rejected(a)) {  // (with few >= 0 linear_steps_kernel writes the results)
     if (OUT && a.few < 0 && blockIdx.y == 0)
       for (int t = (int)at; t < a.tokens; t += a.segment_cap) fill_nan<typename T::Type>(a, t, 1, head, D);
     return;
   }
-  if ((int)at >= (OUT ? a.hdr->segments : a.hdr->followed)) return;
-  const Segment seg = a.segments[at];
-  const bool last = seg.index == seg.parts - 1;
+  Segment seg;
+  if (!OUT || a.planned) {
+    if ((int)at >= (OUT ? a.hdr->segments : a.hdr->followed)) return;
+    seg = a.segments[at];
+  } else {
+    const int row0 = a.row_start[at];
+    seg = {(int)at, row0, a.row_start[at + 1] - row0, 0, 1, 0, 0, 0};
+    if (a.few >= 0 && seg.rows <= a.few) return;
+  }
   int read, write;
   const int team = OUT ? (int)blockIdx.y : 0;
   if (!slots_fit(a, seg.request, read, write)) {
@@ -691,11 +711,18 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
     }
   }
 
+  // (read again: kept over the loop, they are more than the scalar registers hold)
+  typedef const __attribute__((address_space(4))) LinearArgs Args;
+  const Args* late = (const Args*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(late));
+  const Args& z = *late;
   float* to = nullptr;
-  if (!OUT)
-    to = a.added + ((int64_t)(seg.slot + seg.index + 1) * a.kv_heads + head) * D * D;
-  else if (team == 0 && last && write >= 0 && (seg.rows || write != read))
-    to = a.state + write * a.state_slot + head * a.state_head;
+  if (!OUT) {
+    to = z.added + ((int64_t)(seg.slot + seg.index + 1) * z.kv_heads + head) * D * D;
+  } else if (team == 0 && seg.index == seg.parts - 1) {
+    const int into = z.write[seg.request];
+    if (into >= 0 && (seg.rows || into != z.read[seg.request])) to = z.state + into * z.state_slot + head * z.state_head;
+  }
   if (to && rw == 0) {
 #pragma unroll
     for (int t = 0; t < kGroups; ++t)
@@ -781,7 +808,7 @@ hipError_t launch(const LinearArgs& a, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_linear(const LinearArgs& a, bool fp16, hipStream_t st) {
-  if (a.row_start) {
+  if (a.planned) {
     linear_plan_kernel<<<1, kThreads, 0, st>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

@@ -397,18 +397,21 @@ hipError_t launch_few(const ProductArgs& a, hipStream_t st) {
 // to 16 tokens, which weights bound, always); of the tiles those that are done
 // first, by the time of a step of k where a compute unit has one workgroup, or
 // several.
+template <class T, class X>
+hipError_t launch_one_round(const ProductArgs& a, hipStream_t st) {
+  if (a.tokens <= 16) return launch_few<T, X>(a, st);
+  if (product_tiles(a.tokens, a.channels, 64, 16) <= kComputeUnits) return launch_direct<T, X, 1, 4, 16>(a, st);
+  return launch_direct<T, X, 2, 4, 8>(a, st);
+}
+
 template <class T>
 hipError_t launch(const ProductArgs& a, hipStream_t st) {
-  auto count = [&](int tokens, int channels) {
-    return (int64_t)((a.tokens + tokens - 1) / tokens) * ((a.channels + channels - 1) / channels);
-  };
-  if (a.dtype == KVR_BF16) return launch_few<T, __bf16>(a, st);
-  if (a.dtype == KVR_FP16) return launch_few<T, _Float16>(a, st);
-  if (a.tokens <= 16) return launch_few<T, int8_t>(a, st);
-  if (count(64, 16) <= kComputeUnits) return launch_direct<T, int8_t, 1, 4, 16>(a, st);
-  if (count(64, 32) <= kComputeUnits) return launch_direct<T, int8_t, 2, 4, 8>(a, st);
+  if (a.dtype == KVR_BF16) return launch_one_round<T, __bf16>(a, st);
+  if (a.dtype == KVR_FP16) return launch_one_round<T, _Float16>(a, st);
+  if (a.tokens <= 16 || product_tiles(a.tokens, a.channels, 64, 32) <= kComputeUnits)
+    return launch_one_round<T, int8_t>(a, st);
   auto step_ns = [&](int tile, int alone, int each) {
-    const int64_t rounds = (count(tile, tile) + kComputeUnits - 1) / kComputeUnits;
+    const int64_t rounds = (product_tiles(a.tokens, a.channels, tile, tile) + kComputeUnits - 1) / kComputeUnits;
     return rounds * each > alone ? rounds * each : alone;
   };
   const int64_t t64 = step_ns(64, 235, 150), t128 = step_ns(128, 400, 365), t256 = step_ns(256, 900, 900);

@@ -193,7 +193,7 @@ def test_product_types(dtype, out, tokens):
 
 
 @pytest.mark.parametrize("tokens,dim", [(1, 16), (7, 65536), (1, 65536), (2, 32784), (16, 4096), (16, 4112), (17, 64),
-                                        (15, 1040)])
+                                        (15, 1040), (25, 128), (64, 1024), (65, 1008), (100, 640), (1000, 64)])
 @pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
 def test_product_of_few_tokens(tokens, dim, dtype):
     check_product(product_problem(tokens, dim, 67, dtype, bias=True), F32)
@@ -321,6 +321,22 @@ def test_linear_decays(decay, dtype):
 
 
 @TYPES
+def test_linear_many_requests(dtype):
+    # more than go without a plan: singles, drafts and prompts among them
+    p = R.Linear([1, 0, 2, 4, 5, 1, 1, 20] * 34, heads=2, kv_heads=1, dtype=dtype, read=[i % 7 for i in range(272)],
+                 decay=[-0.1])
+    check_linear(p)
+
+
+@TYPES
+def test_linear_cut_requests_in_place(dtype):
+    # cut ones whose last segment writes what the first begins with, teams of query heads beside each other
+    check_linear(R.Linear([700, 300, 0, 5], heads=6, kv_heads=2, dtype=dtype, write=None))
+    check_linear(R.Linear([130, 64], heads=8, kv_heads=2, dim=128, dtype=dtype, write=None))
+    check_linear(R.Linear([130, 64], heads=8, kv_heads=2, dim=128, dtype=dtype))
+
+
+@TYPES
 def test_linear_long_prompts(dtype):
     check_linear(R.Linear([2500, 0, 1300], heads=2, kv_heads=1, dim=64, dtype=dtype))
     check_linear(R.Linear([1800], heads=1, kv_heads=1, dim=128, dtype=dtype, read=[-1]))
@@ -417,11 +433,17 @@ def test_linear_tokens_behind_the_last_request_are_left():
     R.check_linear(out[:75], args[3], p, w)
 
 
-@pytest.mark.parametrize("rows", [[0, 3, 2, 6], [-1, 2, 3, 6], [0, 2, 3, 7]])
-def test_linear_invalid_lengths(rows):
-    p = R.Linear([2, 1, 3])
+# few requests, as many as are planned for, long ones that are cut
+@pytest.mark.parametrize("new", [[2, 1, 3], [1] * 300 + [2, 1, 3], [200, 1, 300]], ids=["few", "many", "long"])
+@pytest.mark.parametrize("at,by", [(-2, -400), (-3, -1000), (-1, 1), (1, -1)])
+def test_linear_invalid_lengths(new, at, by):
+    p = R.Linear(new)
     args = p.args()
-    args[7] = p.i32(rows)
+    rows = p.row_start.clone()
+    rows[at] += by
+    if at == 1:
+        rows[0] = -1
+    args[7] = rows.to(DEV)
     status = torch.zeros(1, dtype=torch.int32, device=DEV)
     out = K.linear_attention(*args, status=status)
     assert int(status) == 1 and out.isnan().all() and torch.equal(args[3].cpu(), p.state)
@@ -429,7 +451,7 @@ def test_linear_invalid_lengths(rows):
 
 @pytest.mark.parametrize("which", ["read", "write"])
 @pytest.mark.parametrize("slot", [-2, 8, 1 << 30])
-@pytest.mark.parametrize("new", [[2, 1, 70], [1, 1, 1], [1, 70, 5]])
+@pytest.mark.parametrize("new", [[2, 1, 70], [1, 1, 1], [1, 70, 5], [40, 700, 3]])
 def test_linear_invalid_slots(which, slot, new):
     p = R.Linear(new)
     want = p.want()

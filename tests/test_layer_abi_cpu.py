@@ -154,19 +154,27 @@ def test_linear_buffers_refused(bad):
 
 
 def test_small_or_missing_workspaces_refused():
-    halves = dict(dtype=0, d_x_scale=0, num_tokens=20)
+    halves = dict(dtype=0, d_x_scale=0, num_tokens=2000)
     assert K.kvr_product_workspace(product()) == 0
-    assert K.kvr_product_workspace(product(**halves)) >= 20 * 64 + 80
-    few = dict(halves, num_tokens=16)  # every workgroup brings these to integers itself
-    assert K.kvr_product_workspace(product(**few)) == 0
-    assert K.kvr_product_workspace(product(**few, dim=8192)) >= 16 * 8192 + 64
+    assert K.kvr_product_workspace(product(**halves)) >= 2000 * 64 + 8000
+    # few tokens are brought to integers by every workgroup: as long as there is one round of these
+    few = dict(halves, num_tokens=64)
+    assert K.kvr_product_workspace(product(**few, dim=1024, channels=8192)) == 0
+    assert K.kvr_product_workspace(product(**few, dim=1040, channels=8192)) >= 64 * 1040 + 256
+    assert K.kvr_product_workspace(product(**few, dim=1024, channels=8193)) >= 64 * 1024 + 256
+    assert K.kvr_product_workspace(product(**dict(few, num_tokens=16), dim=4096, channels=1 << 20)) == 0
     _refused(lambda: K.kvr_integer_product(product(**halves), 0, 1 << 20))
     _refused(lambda: K.kvr_integer_product(product(**halves), P + 8, 1 << 20))
     _refused(lambda: K.kvr_integer_product(product(**halves), P, 64), K.KVR_ENOMEM)
-    assert K.kvr_linear_workspace(linear()) > 0
-    _refused(lambda: K.kvr_linear_attention(linear(), 0, 1 << 40))
-    _refused(lambda: K.kvr_linear_attention(linear(), P + 16, 1 << 40))
-    _refused(lambda: K.kvr_linear_attention(linear(), P, 16), K.KVR_ENOMEM)
+    # few requests that are not cut take no workspace
+    assert K.kvr_linear_workspace(linear()) == 0 and K.kvr_linear_workspace(linear(num_requests=256)) == 0
+    assert K.kvr_linear_workspace(linear(num_requests=257)) > 0
+    assert K.kvr_linear_workspace(linear(num_tokens=256)) == 0
+    cut = dict(num_tokens=257)
+    assert K.kvr_linear_workspace(linear(**cut)) >= 2 * 2 * 64 * 64 * 4
+    _refused(lambda: K.kvr_linear_attention(linear(**cut), 0, 1 << 40))
+    _refused(lambda: K.kvr_linear_attention(linear(**cut), P + 16, 1 << 40))
+    _refused(lambda: K.kvr_linear_attention(linear(**cut), P, 16), K.KVR_ENOMEM)
 
 
 def test_nothing_to_do_is_no_error_and_no_launch():
