@@ -579,3 +579,18 @@ def test_captured_layers_replay():
         for o, e in zip(outs, eager):
             assert all(torch.equal(a, b) for a, b in zip(o, e))
         assert all(torch.equal(a, b) for a, b in zip(again, eager[1]))
+
+
+def test_the_example_runs():
+    import os
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    sys.path.insert(0, os.path.join(root, "examples"))
+    try:
+        import state_worker
+        worst = state_worker.main(DEV)
+    finally:
+        sys.path.remove(os.path.join(root, "examples"))
+    # results are rounded once (2^-8 of themselves), and so are two factors of each of their parts at most; parts
+    # that cancel may be some times larger than the largest result
+    assert worst < 8 * 2.0 ** -8
