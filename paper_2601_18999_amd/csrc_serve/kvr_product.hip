@@ -56,16 +56,20 @@ __device__ __forceinline__ void store(char* row, int channel, int channels, cons
 // straight to LDS, into BUFFERS buffers in turn.  16-byte chunks of a row stand
 // at chunk ^ (row / 4 % 4): the reads of one chunk of 16 rows fall on
 // different banks.
-template <int WC, int WT, int FC, int FT, int BUFFERS>
+//
+// KS such groups of waves have the steps in turn, and their sums are added at
+// the end: the waves that a compute unit needs, where there is one workgroup for
+// each.
+template <int WC, int WT, int FC, int FT, int BUFFERS, int KS>
 struct Shape {
-  static constexpr int kWaves = WC * WT, kThreads = 64 * kWaves;
+  static constexpr int kGroup = WC * WT, kWaves = kGroup * KS, kThreads = 64 * kWaves;
   static constexpr int kChannels = WC * FC * 32, kTokens = WT * FT * 32;
   static constexpr int kRows = kChannels + kTokens;
   static constexpr int kBuffer = kRows * kStep, kPitch = 4 * kChannels + 16, kResults = WT * 32 * kPitch;
-  static constexpr int kTiles = BUFFERS * kBuffer > kResults ? BUFFERS * kBuffer : kResults;
+  static constexpr int kTiles = KS * (BUFFERS * kBuffer > kResults ? BUFFERS * kBuffer : kResults);
   static constexpr int kBytes = kTiles + (kTokens + 2 * kChannels) * 4;  // and the tile's scales and biases
-  static constexpr int kLoads = kRows / 16 / kWaves;  // of a wave, for a step: 16 rows each
-  static_assert(kLoads * 16 * kWaves == kRows, "tile shape");
+  static constexpr int kLoads = kRows / 16 / kGroup;  // of a wave, for a step: 16 rows each
+  static_assert(kLoads * 16 * kGroup == kRows && kThreads <= 1024 && kBytes <= 160 * 1024, "tile shape");
 };
 
 __device__ __forceinline__ const i32x4* chunk_at(const char* tile, int row, int chunk) {
@@ -75,12 +79,13 @@ __device__ __forceinline__ const i32x4* chunk_at(const char* tile, int row, int 
 // kinds of instructions for the scheduler
 constexpr int kProducts = 0x8, kReads = 0x100;
 
-template <class T, int WC, int WT, int FC, int FT, int BUFFERS>
-__global__ __launch_bounds__(64 * WC * WT, FC * FT > 8 ? 1 : 2) void product_kernel(ProductArgs a, uint32_t across, uint32_t down) {
-  typedef Shape<WC, WT, FC, FT, BUFFERS> S;
+template <class T, int WC, int WT, int FC, int FT, int BUFFERS, int KS>
+__global__ __launch_bounds__(64 * WC * WT * KS, FC * FT > 8 ? 1 : 2) void product_kernel(ProductArgs a, uint32_t across,
+                                                                                  uint32_t down) {
+  typedef Shape<WC, WT, FC, FT, BUFFERS, KS> S;
   extern __shared__ __align__(16) char lds[];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n = lane & 31, h = lane >> 5;
+  const int lane = threadIdx.x & 63, all_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 31, h = lane >> 5, part = KS == 1 ? 0 : all_wave / S::kGroup, wave = all_wave - part * S::kGroup;
 
   // neighbouring tiles on one XCD, whose cache they share: each takes a run of
   // the tiles, which go through bands of eight token tiles channel by channel
@@ -92,26 +97,29 @@ __global__ __launch_bounds__(64 * WC * WT, FC * FT > 8 ? 1 : 2) void product_ker
   const uint32_t high = min(kBand, down - band * kBand);
   const int t0 = (int)(band * kBand + in_band % high) * S::kTokens, c0 = (int)(in_band / high) * S::kChannels;
 
-  // rows 16 (i * waves + wave) + lane / 4 of both operands, the chunk that
+  // rows 16 (i * group + wave) + lane / 4 of both operands, the chunk that
   // belongs where the lane writes
   const int chunk = (lane % 4) ^ (lane / 16);
   global_bytes from[S::kLoads];
 #pragma unroll
   for (int i = 0; i < S::kLoads; ++i) {
-    const int row = (i * S::kWaves + wave) * 16 + lane / 4;
+    const int row = (i * S::kGroup + wave) * 16 + lane / 4;
     from[i] = (global_bytes)(row < S::kChannels
                                  ? a.w + min(c0 + row, a.channels - 1) * a.w_chan
                                  : a.x + min(t0 + row - S::kChannels, a.tokens - 1) * a.x_tok) +
               chunk * 16;
   }
-  const uint32_t to = lds_offset(lds) + wave * 1024;
-  const int steps = (a.dim + kStep - 1) / kStep;
+  char* buffers = lds + part * BUFFERS * S::kBuffer;
+  const uint32_t to = lds_offset(buffers) + wave * 1024;
+  // of each group (behind k's end there are zeros)
+  const int steps = (a.dim + KS * kStep - 1) / (KS * kStep);
   auto load = [&](int s) {
-    const bool there = s * kStep + chunk * 16 < a.dim;
+    const int k = (s * KS + part) * kStep;
+    const bool there = k + chunk * 16 < a.dim;
 #pragma unroll
     for (int i = 0; i < S::kLoads; ++i)
-      load16_to_lds(there ? from[i] + s * kStep : (global_bytes)kZeros,
-                    to + (s % BUFFERS) * S::kBuffer + i * S::kWaves * 1024);
+      load16_to_lds(there ? from[i] + k : (global_bytes)kZeros,
+                    to + (s % BUFFERS) * S::kBuffer + i * S::kGroup * 1024);
   };
   // waits for step s, where those up to `last` are on their way
   auto wait_for = [&](int s, int last) {
@@ -136,7 +144,7 @@ __global__ __launch_bounds__(64 * WC * WT, FC * FT > 8 ? 1 : 2) void product_ker
   const int c_row = wave % WC * FC * 32 + n, t_row = S::kChannels + wave / WC * FT * 32 + n;
   i32x4 w[2][FC], x[2][FT];
   auto read = [&](int s, int k) {
-    const char* tile = lds + (s % BUFFERS) * S::kBuffer;
+    const char* tile = buffers + (s % BUFFERS) * S::kBuffer;
 #pragma unroll
     for (int c = 0; c < FC; ++c) w[k][c] = *chunk_at(tile, c_row + c * 32, 2 * k + h);
 #pragma unroll
@@ -153,7 +161,7 @@ __global__ __launch_bounds__(64 * WC * WT, FC * FT > 8 ? 1 : 2) void product_ker
   };
   // scales and biases, for the end: 64 values a load
   float* scales = (float*)(lds + S::kTiles);
-  for (int i = wave; i < (S::kTokens + 2 * S::kChannels) / 64; i += S::kWaves) {
+  for (int i = all_wave; i < (S::kTokens + 2 * S::kChannels) / 64; i += S::kWaves) {
     const int first = i * 64, of = first < S::kTokens ? 0 : first < S::kTokens + S::kChannels ? 1 : 2;
     const float* base = of == 0 ? a.x_scale : of == 1 ? a.w_scale : a.bias ? a.bias : a.w_scale;
     const int at = of == 0 ? min(t0 + first + lane, a.tokens - 1)
@@ -195,7 +203,7 @@ __global__ __launch_bounds__(64 * WC * WT, FC * FT > 8 ? 1 : 2) void product_ker
 #pragma unroll
   for (int t = 0; t < FT; ++t) {
     barrier();
-    char* row = lds + (wave / WC * 32 + n) * kPitch + (wave % WC * FC * 32 + 4 * h) * 4;
+    char* row = lds + part * S::kResults + (wave / WC * 32 + n) * kPitch + (wave % WC * FC * 32 + 4 * h) * 4;
 #pragma unroll
     for (int c = 0; c < FC; ++c)
 #pragma unroll
@@ -208,7 +216,12 @@ __global__ __launch_bounds__(64 * WC * WT, FC * FT > 8 ? 1 : 2) void product_ker
       const int place = (r / 32 * FT + t) * 32 + r % 32, token = t0 + place;
       if (token >= a.tokens || channel >= a.channels) continue;
       const float x_scale = scales[place];
-      const i32x4 lo = *(const i32x4*)(lds + r * kPitch + col * 4), hi = *(const i32x4*)(lds + r * kPitch + col * 4 + 16);
+      i32x4 lo = {0, 0, 0, 0}, hi = lo;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        lo += *(const i32x4*)(lds + k * S::kResults + r * kPitch + col * 4);
+        hi += *(const i32x4*)(lds + k * S::kResults + r * kPitch + col * 4 + 16);
+      }
       float f[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -350,14 +363,14 @@ hipError_t allow_lds(int bytes) {
   return hipSuccess;
 }
 
-template <class T, int WC, int WT, int FC, int FT, int BUFFERS>
+template <class T, int WC, int WT, int FC, int FT, int BUFFERS, int KS>
 hipError_t launch_tiles(const ProductArgs& a, hipStream_t st) {
-  typedef Shape<WC, WT, FC, FT, BUFFERS> S;
-  const hipError_t e = allow_lds<product_kernel<T, WC, WT, FC, FT, BUFFERS>>(S::kBytes);
+  typedef Shape<WC, WT, FC, FT, BUFFERS, KS> S;
+  const hipError_t e = allow_lds<product_kernel<T, WC, WT, FC, FT, BUFFERS, KS>>(S::kBytes);
   if (e != hipSuccess) return e;
   const uint32_t across = (uint32_t)((a.channels + S::kChannels - 1) / S::kChannels);
   const uint32_t down = (uint32_t)((a.tokens + S::kTokens - 1) / S::kTokens);
-  product_kernel<T, WC, WT, FC, FT, BUFFERS><<<across * down, S::kThreads, S::kBytes, st>>>(a, across, down);
+  product_kernel<T, WC, WT, FC, FT, BUFFERS, KS><<<across * down, S::kThreads, S::kBytes, st>>>(a, across, down);
   return hipGetLastError();
 }
 
@@ -380,23 +393,27 @@ hipError_t launch_few(const ProductArgs& a, hipStream_t st) {
   return launch_direct<T, X, 1, 1, 8>(a, st);
 }
 
-// Which kernel, by what they take (8-bit tokens, bfloat16 results, us; direct
-// kernels by tokens x channels of a workgroup):
-//   tokens x k x channels    direct 16x16  16x32  64x16  64x32   tiles of 64   128   256
-//        8 x  4,096 x  4,096      7.4       9.6    7.5    8.7        15.4
-//        8 x  4,096 x 16,384     18.4      14.6   22.5   15.1        15.8
-//       16 x 16,384 x  8,192     35.1      31.6   43.7   34.6        54.5
-//       40 x  4,096 x  4,096     12.3      12.3    9.6   11.4        15.6
-//       64 x  4,096 x  8,192     30.7      24.3   21.7   13.6        16.0   26.6    57
-//      333 x  5,008 x  1,001     23.1      16.2   22.8   11.9        18.9
-//      512 x  4,096 x  4,096                             46          19.3   27.9    61
-//      256 x  4,096 x 16,384                             99          41.7   29.2    62
-//    1,024 x  4,096 x  8,192                            179          75.8   47.0    63
-//    2,048 x  4,096 x  8,192                                               102.8    76
+// Which kernel, by what they take (8-bit tokens, bfloat16 results, weights that
+// no cache holds, us; direct kernels by tokens x channels of a workgroup, tiles
+// by channels x tokens and the groups of waves that have k in turn):
+//   tokens x k x channels    direct 16x16  16x32  64x16  64x32   tiles 64x64/2  128x64/2  128x128/1  /2  256x256
+//        8 x  4,096 x  4,096      8.0       8.2    7.9    9.8         12.3         18         25      22     57
+//        8 x  4,096 x 16,384     19.7      16.5   24.9   18.3         16.9         22         26      24     59
+//       16 x 16,384 x  8,192     40.1      35.4   48.1   37.6         41           66         90      77    212
+//       17 x  4,096 x  4,096     10.1       8.4    8.5   10.5         12.5         19         26      23     58
+//       33 x  4,096 x  8,192     23.8      22.1   18.2   12.2         13.6         22         26      24     59
+//      333 x  5,008 x  1,001     24.6      18.6   24.0   13.2         15.3         30         45      42     83
+//      128 x  4,096 x  8,192     62        50     44     25.1         14.8         22         29      28     62
+//      512 x  4,096 x  4,096    117        92     81     47           23.2         20.7       28      27     64
+//      256 x  4,096 x 16,384    243       197    163     92           45           44         31.0    31.1   68
+//    1,024 x  4,096 x  8,192    456       365    315    178           75           74         53.0    56.1   65
+//    2,048 x  4,096 x  8,192    904       727    625    354          143          145        100     109     80
 // The direct kernels are taken as long as one round of workgroups does it (up
 // to 16 tokens, which weights bound, always); of the tiles those that are done
-// first, by the time of a step of k where a compute unit has one workgroup, or
-// several.
+// first, by the time of a round of one workgroup a compute unit (0.1 us, k =
+// 4,096; those of 128 x 128 without groups are two a compute unit where there
+// are as many).  64 x 64 without groups took 18.7 instead of 14.8 us for 128
+// tokens x 8,192 channels, with four of them 15.8.
 template <class T, class X>
 hipError_t launch_one_round(const ProductArgs& a, hipStream_t st) {
   if (a.tokens <= 16) return launch_few<T, X>(a, st);
@@ -410,13 +427,16 @@ hipError_t launch(const ProductArgs& a, hipStream_t st) {
   if (a.dtype == KVR_FP16) return launch_one_round<T, _Float16>(a, st);
   if (a.tokens <= 16 || product_tiles(a.tokens, a.channels, 64, 32) <= kComputeUnits)
     return launch_one_round<T, int8_t>(a, st);
-  auto step_ns = [&](int tile, int alone, int each) {
-    const int64_t rounds = (product_tiles(a.tokens, a.channels, tile, tile) + kComputeUnits - 1) / kComputeUnits;
-    return rounds * each > alone ? rounds * each : alone;
+  auto rounds = [&](int channels, int tokens) {
+    return (product_tiles(a.tokens, a.channels, tokens, channels) + kComputeUnits - 1) / kComputeUnits;
   };
-  const int64_t t64 = step_ns(64, 235, 150), t128 = step_ns(128, 400, 365), t256 = step_ns(256, 900, 900);
-  if (t64 <= t128 && t64 <= t256) return launch_tiles<T, 2, 2, 1, 1, 4>(a, st);
-  return t128 <= t256 ? launch_tiles<T, 2, 2, 2, 2, 4>(a, st) : launch_tiles<T, 4, 2, 2, 4, 4>(a, st);
+  const int64_t r128 = rounds(128, 128);
+  const int64_t t64 = 115 * rounds(64, 64), t12864 = 175 * rounds(128, 64), t128 = r128 == 1 ? 270 : 245 * r128,
+                t256 = 620 * rounds(256, 256);
+  if (t64 <= t12864 && t64 <= t128 && t64 <= t256) return launch_tiles<T, 2, 2, 1, 1, 4, 2>(a, st);
+  if (t12864 <= t128 && t12864 <= t256) return launch_tiles<T, 2, 2, 2, 1, 4, 2>(a, st);
+  if (t256 < t128) return launch_tiles<T, 4, 2, 2, 4, 4, 1>(a, st);
+  return r128 == 1 ? launch_tiles<T, 2, 2, 2, 2, 4, 2>(a, st) : launch_tiles<T, 2, 2, 2, 2, 4, 1>(a, st);
 }
 
 }  // namespace
