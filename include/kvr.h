@@ -500,7 +500,7 @@ kvr_status kvr_block_norm(const kvr_norm* n, void* hip_stream);
  * d_x holds KVR_INT8 with d_x_scale, or KVR_BF16 / KVR_FP16, which are brought
  * to integers with a scale for each token as kvr_block_norm does it, in the
  * workspace.  The sum is exact.  Every row of w, and of 8-bit x, starts on a
- * 16-byte boundary. */
+ * 16-byte boundary.  d_out does not overlap inputs. */
 typedef struct kvr_product {
   uint32_t struct_size;
   int32_t dtype;      /* of d_x: KVR_INT8, KVR_BF16 or KVR_FP16               */
@@ -534,8 +534,9 @@ kvr_status kvr_integer_product(const kvr_product* p, void* d_workspace, size_t b
  * request writes is neither written nor read by another one of the call.
  * log_decay is a natural logarithm, <= 0; -inf forgets all but the own token.
  * What stands in a later token, or in another request, has no influence on a
- * row (infinities and NaN among it).  Tokens behind d_row_start's last are
- * not written.  Where a call's tokens are split differently over calls, the
+ * row (infinities and NaN among it).  Where an infinity has an influence, the
+ * value can be NaN in its place.  d_out does not overlap inputs.  Tokens behind
+ * d_row_start's last are not written.  Where a call's tokens are split differently over calls, the
  * results differ by roundings; the same call gives the same bits.
  * row_start that is not valid (negative, decreasing, more than num_tokens)
  * sets KVR_DEV_BAD_LENGTH in d_status (optional): every result is NaN, no

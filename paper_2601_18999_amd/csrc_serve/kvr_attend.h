@@ -29,7 +29,6 @@
 // the rounded result; the sum l adds the unrounded p.
 #pragma once
 
-#include <atomic>
 #include <type_traits>
 
 #include "kvr_lds.h"
@@ -902,17 +901,8 @@ template <int D, class T, bool FP8>
 hipError_t launch_attend_as(const AttendArgs& a, hipStream_t st) {
   constexpr int lds = attend_lds<D>();
   static_assert(lds * (D == 256 ? 1 : 2) <= 160 * 1024, "LDS of a compute unit");
-  // once a device: LDS beyond the default limit
-  static std::atomic<uint64_t> allowed{0};
-  int device = 0;
-  hipError_t e = hipGetDevice(&device);
+  const hipError_t e = allow_lds<attend_kernel<D, T, FP8>>(lds);
   if (e != hipSuccess) return e;
-  const uint64_t bit = device < 64 ? 1ull << device : 0;
-  if (!(allowed.load(std::memory_order_relaxed) & bit)) {
-    e = hipFuncSetAttribute((const void*)attend_kernel<D, T, FP8>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (e != hipSuccess) return e;
-    allowed.fetch_or(bit, std::memory_order_relaxed);
-  }
   attend_kernel<D, T, FP8><<<dim3((uint32_t)a.item_cap * (uint32_t)a.kv_heads), dim3(kAttendThreads), lds, st>>>(a);
   return hipGetLastError();
 }

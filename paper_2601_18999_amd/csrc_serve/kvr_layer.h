@@ -60,11 +60,10 @@ constexpr int kUnplanned = 256;
 constexpr int kLinearSlots = 2 * kComputeUnits;
 
 // A run of up to LinearArgs::segment tokens of one request.
-struct Segment {
+struct alignas(32) Segment {
   int32_t request, row0, rows;
   int32_t index, parts;  // of its request's segments
   int32_t slot;          // of LinearArgs::added, of the request's first segment
-  int32_t pad, pad1;
 };
 
 struct LinearHdr {

@@ -1,8 +1,10 @@
-// kvr_lds.h - loads from memory straight to LDS, and the waits for them.
+// kvr_lds.h - loads from memory straight to LDS, and the waits for them; LDS
+// beyond a kernel's default limit.
 #pragma once
 
 #include <hip/hip_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 
 namespace kvr {
@@ -44,6 +46,22 @@ __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)"
 // a barrier that does not wait for loads in flight
 __device__ __forceinline__ void barrier() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// Once a device: LDS beyond the default limit.
+template <auto Kernel>
+hipError_t allow_lds(int bytes) {
+  static std::atomic<uint64_t> allowed{0};
+  int device = 0;
+  hipError_t e = hipGetDevice(&device);
+  if (e != hipSuccess) return e;
+  const uint64_t bit = device < 64 ? 1ull << device : 0;
+  if (!(allowed.load(std::memory_order_relaxed) & bit)) {
+    e = hipFuncSetAttribute((const void*)Kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+    allowed.fetch_or(bit, std::memory_order_relaxed);
+  }
+  return hipSuccess;
 }
 
 }  // namespace

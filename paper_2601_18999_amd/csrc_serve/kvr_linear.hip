@@ -15,9 +15,8 @@
 // one computes the results of all segments side by side.
 #include <hip/hip_runtime.h>
 
-#include <atomic>
-
 #include "kvr_layer.h"
+#include "kvr_lds.h"
 
 namespace kvr {
 namespace {
@@ -33,7 +32,6 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef __attribute__((address_space(3))) char lds_char;
 
 constexpr int kThreads = 256;
 constexpr int kChunk = 64;  // tokens
@@ -124,9 +122,9 @@ __global__ __launch_bounds__(kThreads) void linear_plan_kernel(LinearArgs a) {
     const int slot = parts > 1 ? atomicAdd(&slots, parts) : 0;
     const int full = parts > 1 ? atomicAdd(&followed, parts - 1) : 0;
     for (int i = 0; i < parts - 1; ++i)
-      a.segments[full + i] = {r, from + i * a.segment, a.segment, i, parts, slot, 0, 0};
+      a.segments[full + i] = {r, from + i * a.segment, a.segment, i, parts, slot};
     const int rest = rows - (parts - 1) * a.segment;
-    a.segments[atomicAdd(&place[kind(rest)], 1)] = {r, from + rows - rest, rest, parts - 1, parts, slot, 0, 0};
+    a.segments[atomicAdd(&place[kind(rest)], 1)] = {r, from + rows - rest, rest, parts - 1, parts, slot};
   });
 }
 
@@ -209,7 +207,6 @@ __global__ __launch_bounds__(kThreads) void linear_steps_kernel(LinearArgs a) {
     for (int i = 0; i < kRows; ++i) *reinterpret_cast<f32x4*>(to + (down + i * kDown) * D) = state[i];
   }
 }
-
 
 // ---- the chunked form ----
 
@@ -400,7 +397,7 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
     seg = a.segments[at];
   } else {
     const int row0 = a.row_start[at];
-    seg = {(int)at, row0, a.row_start[at + 1] - row0, 0, 1, 0, 0, 0};
+    seg = {(int)at, row0, a.row_start[at + 1] - row0, 0, 1, 0};
     if (a.few >= 0 && seg.rows <= a.few) return;
   }
   int read, write;
@@ -760,28 +757,13 @@ __global__ __launch_bounds__(kThreads) void linear_states_kernel(LinearArgs a) {
   }
 }
 
-// Once a device: LDS beyond the default limit.
-template <auto Kernel>
-hipError_t allow_lds(int bytes) {
-  static std::atomic<uint64_t> allowed{0};
-  int device = 0;
-  hipError_t e = hipGetDevice(&device);
-  if (e != hipSuccess) return e;
-  const uint64_t bit = device < 64 ? 1ull << device : 0;
-  if (!(allowed.load(std::memory_order_relaxed) & bit)) {
-    e = hipFuncSetAttribute((const void*)Kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e != hipSuccess) return e;
-    allowed.fetch_or(bit, std::memory_order_relaxed);
-  }
-  return hipSuccess;
-}
-
 template <int D, class T, bool OUT>
 hipError_t launch_chunks(const LinearArgs& a, int segments, hipStream_t st) {
   constexpr int bytes = ChunkLds<D, T, OUT>::kBytes;
   const hipError_t e = allow_lds<linear_chunks_kernel<D, T, OUT>>(bytes);
   if (e != hipSuccess) return e;
-  linear_chunks_kernel<D, T, OUT><<<dim3((uint32_t)segments * (uint32_t)a.kv_heads, OUT ? a.teams : 1), kThreads, bytes, st>>>(a);
+  const dim3 grid((uint32_t)segments * (uint32_t)a.kv_heads, OUT ? a.teams : 1);
+  linear_chunks_kernel<D, T, OUT><<<grid, kThreads, bytes, st>>>(a);
   return hipGetLastError();
 }
 

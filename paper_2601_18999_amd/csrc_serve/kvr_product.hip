@@ -9,7 +9,6 @@
 // four neighbouring channels of one token at a time.
 #include <hip/hip_runtime.h>
 
-#include <atomic>
 #include <type_traits>
 
 #include "kvr_layer.h"
@@ -345,22 +344,6 @@ __global__ __launch_bounds__(64 * WAVES) void product_direct_kernel(ProductArgs 
     }
     store<T, 4>(a.out + token * a.out_tok, channel, a.channels, f);
   }
-}
-
-// Once a device: LDS beyond the default limit.
-template <auto Kernel>
-hipError_t allow_lds(int bytes) {
-  static std::atomic<uint64_t> allowed{0};
-  int device = 0;
-  hipError_t e = hipGetDevice(&device);
-  if (e != hipSuccess) return e;
-  const uint64_t bit = device < 64 ? 1ull << device : 0;
-  if (!(allowed.load(std::memory_order_relaxed) & bit)) {
-    e = hipFuncSetAttribute((const void*)Kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e != hipSuccess) return e;
-    allowed.fetch_or(bit, std::memory_order_relaxed);
-  }
-  return hipSuccess;
 }
 
 template <class T, int WC, int WT, int FC, int FT, int BUFFERS, int KS>

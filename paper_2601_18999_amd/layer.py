@@ -44,6 +44,8 @@ def _matrix(where: str, name: str, t, dtypes, rows, dim, device):
         shape = t.shape
         if len(shape) == 2 and (rows is None or shape[0] == rows) and (dim is None or shape[1] == dim):
             stride, one = t.stride()
+            if shape[0] >> 31:
+                _refuse(where, f"{name} has {shape[0]} rows (fewer than 2^31)")
             if one == 1 or shape[1] <= 1:
                 return t.data_ptr(), stride
             _refuse(where, f"the elements of a row of {name} must be contiguous")
@@ -55,6 +57,15 @@ def _apart(where: str, name: str, t) -> None:
     """Refuses an output whose rows overlap."""
     if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
         _refuse(where, f"the rows of {name} overlap")
+
+
+def _overlap(n: int, step: int, m: int, each: int, size: int) -> bool:
+    """Whether of n times m pieces of ``size`` elements, ``step`` and ``each`` apart, some overlap."""
+    if m <= 1 or n <= 1:
+        return (n > 1 and m == 1 and step < size) or (m > 1 and n == 1 and each < size)
+    if step < each:
+        n, step, m, each = m, each, n, step
+    return each < size or step < (m - 1) * each + size
 
 
 def block_norm(x: torch.Tensor, *, after: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
@@ -226,6 +237,8 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, state: t
     if q.dtype not in HALVES or q.dim() != 3:
         _refuse(where, "q must be [tokens, heads, dim] of torch.bfloat16 or torch.float16")
     tokens, heads, dim = q.shape
+    if tokens * heads >> 31:
+        _refuse(where, "tokens * heads must be below 2^31")
     for name, t in (("k", k), ("v", v)):
         if t.dtype is not q.dtype or t.device != device or t.dim() != 3 or t.shape != (tokens, k.shape[1], dim):
             _refuse(where, f"{name} must be [{tokens}, kv_heads, {dim}] of {q.dtype} on {device}, k like v")
@@ -236,7 +249,7 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, state: t
                        "state contiguous")
     slots, i32 = state.shape[0], torch.int32
     s0, s1 = state.stride()[:2]
-    if (kv_heads > 1 and s1 < dim * dim) or (slots > 1 and s0 < dim * dim):
+    if _overlap(slots, s0, kv_heads, s1, dim * dim):
         _refuse(where, "the states overlap")
     p_decay = _vector(where, "log_decay", log_decay, torch.float32, kv_heads, device)
     p_read = _vector(where, "read", read, i32, None, device)
@@ -253,6 +266,8 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, state: t
     k0, k1, k2 = k.stride()
     v0, v1, v2 = v.stride()
     o0, o1, o2 = out.stride()
+    if _overlap(tokens, o0, heads, o1, dim):
+        _refuse(where, "the heads of out overlap")
     if q2 != 1 or k2 != 1 or v2 != 1 or o2 != 1:
         _refuse(where, "the elements of a head must be contiguous")
     code = DTYPE_CODES[q.dtype]

@@ -497,6 +497,135 @@ def test_linear_states_past_32_bits():
     R.check_linear(out, pool[n - 4:], p, [want[0], want[1][:4], want[2], want[3][:4]])
 
 
+# ---------------------------------------------------------------- refusals of tensors
+
+
+def z(*shape, dtype=BF16):
+    return torch.zeros(shape, dtype=dtype, device=DEV)
+
+
+def far_rows(rows, *rest, dtype=BF16):
+    """So many rows of one row's memory."""
+    return z(1, *rest, dtype=dtype).expand(rows, *rest)
+
+
+I32, I8 = torch.int32, torch.int8
+NORMS = {
+    "one dimension": lambda: dict(x=z(8)),
+    "type": lambda: dict(x=z(4, 8, dtype=F32)),
+    "columns": lambda: dict(x=z(8, 4).t()),
+    "2^31 rows": lambda: dict(x=far_rows(1 << 31, 8)),
+    "eps": lambda: dict(x=z(4, 8), eps=0.0),
+    "weight": lambda: dict(x=z(4, 8), before=z(9)),
+    "weight's type": lambda: dict(x=z(4, 8), before=z(8, dtype=F32)),
+    "weight's place": lambda: dict(x=z(4, 8), before=torch.zeros(8, dtype=BF16)),
+    "gate": lambda: dict(x=z(4, 8), gate=z(3, 8)),
+    "activation": lambda: dict(x=z(4, 8), gate=z(4, 8), activation="tanh"),
+    "residual": lambda: dict(x=z(4, 8), residual=z(4, 8, dtype=FP16)),
+    "in place of nothing": lambda: dict(x=z(4, 8), in_place=True),
+    "overlapping residual": lambda: dict(x=z(4, 8), residual=far_rows(4, 8), in_place=True),
+    "overlapping result": lambda: dict(x=z(4, 8), out=far_rows(4, 8)),
+    "result's type": lambda: dict(x=z(4, 8), out=z(4, 8), int8=True),
+    "gradient": lambda: dict(x=z(4, 8).requires_grad_()),
+}
+PRODUCTS = {
+    "no scale": lambda: ((z(4, 32, dtype=I8), z(8, 32, dtype=I8), z(8, dtype=F32)), {}),
+    "scale of 16 bits": lambda: ((z(4, 32), z(8, 32, dtype=I8), z(8, dtype=F32)), dict(x_scale=z(4, dtype=F32))),
+    "weight's type": lambda: ((z(4, 32), z(8, 32), z(8, dtype=F32)), {}),
+    "weight's rows": lambda: ((z(4, 32), z(8, 48, dtype=I8), z(8, dtype=F32)), {}),
+    "weight_scale": lambda: ((z(4, 32), z(8, 32, dtype=I8), z(7, dtype=F32)), {}),
+    "bias": lambda: ((z(4, 32), z(8, 32, dtype=I8), z(8, dtype=F32)), dict(bias=z(8))),
+    "dim": lambda: ((z(4, 24), z(8, 24, dtype=I8), z(8, dtype=F32)), {}),
+    "stride": lambda: ((z(4, 32), z(8, 40, dtype=I8)[:, :32], z(8, dtype=F32)), {}),
+    "2^31 rows": lambda: ((far_rows(1 << 31, 32), z(8, 32, dtype=I8), z(8, dtype=F32)), dict(out=z(1, 8))),
+    "result's type": lambda: ((z(4, 32), z(8, 32, dtype=I8), z(8, dtype=F32)), dict(dtype=torch.float64)),
+    "overlapping result": lambda: ((z(4, 32), z(8, 32, dtype=I8), z(8, dtype=F32)), dict(out=far_rows(4, 8))),
+    "gradient": lambda: ((z(4, 32), z(8, 32, dtype=I8), z(8, dtype=F32).requires_grad_()), {}),
+}
+
+
+def linear_args(**change):
+    a = dict(q=z(3, 4, 64), k=z(3, 2, 64), v=z(3, 2, 64), state=z(5, 2, 64, 64, dtype=F32), log_decay=z(2, dtype=F32),
+             read=z(3, dtype=I32))
+    a.update(change)
+    return a
+
+
+LINEARS = {
+    "type": lambda: linear_args(q=z(3, 4, 64, dtype=F32)),
+    "2^31 rows": lambda: linear_args(q=far_rows(1 << 31, 4, 64)),
+    "keys": lambda: linear_args(k=z(2, 2, 64)),
+    "values' heads": lambda: linear_args(v=z(3, 4, 64)),
+    "heads": lambda: linear_args(q=z(3, 3, 64)),
+    "dim": lambda: linear_args(q=z(3, 4, 32), k=z(3, 2, 32), v=z(3, 2, 32), state=z(5, 2, 32, 32, dtype=F32)),
+    "state's type": lambda: linear_args(state=z(5, 2, 64, 64)),
+    "state's heads": lambda: linear_args(state=z(5, 3, 64, 64, dtype=F32)),
+    "transposed states": lambda: linear_args(state=z(5, 2, 64, 64, dtype=F32).transpose(2, 3)),
+    "overlapping slots": lambda: linear_args(state=far_rows(5, 2, 64, 64, dtype=F32)),
+    "overlapping states": lambda: linear_args(
+        state=z(6, 64, 64, dtype=F32).as_strided((5, 2, 64, 64), (4096, 4096, 64, 1))),
+    "log_decay": lambda: linear_args(log_decay=z(4, dtype=F32)),
+    "read": lambda: linear_args(read=z(2, dtype=I32)),
+    "read's type": lambda: linear_args(read=z(3, dtype=torch.int64)),
+    "write": lambda: linear_args(write=z(2, dtype=I32)),
+    "row_start": lambda: linear_args(row_start=z(3, dtype=I32)),
+    "columns": lambda: linear_args(q=z(3, 64, 4).transpose(1, 2)),
+    "result": lambda: linear_args(out=z(3, 4, 64, dtype=FP16)),
+    "one head's result for all": lambda: linear_args(out=z(3, 1, 64).expand(3, 4, 64)),
+    "one token's result for all": lambda: linear_args(out=far_rows(3, 4, 64)),
+    "scale": lambda: linear_args(scale=INF),
+    "gradient": lambda: linear_args(state=z(5, 2, 64, 64, dtype=F32).requires_grad_()),
+}
+
+
+@pytest.mark.parametrize("what", NORMS)
+def test_norm_refuses(what):
+    kw = NORMS[what]()
+    with pytest.raises(K.KvrError):
+        K.block_norm(kw.pop("x"), **kw)
+
+
+@pytest.mark.parametrize("what", PRODUCTS)
+def test_product_refuses(what):
+    args, kw = PRODUCTS[what]()
+    with pytest.raises(K.KvrError):
+        K.integer_product(*args, **kw)
+
+
+@pytest.mark.parametrize("what", LINEARS)
+def test_linear_refuses(what):
+    with pytest.raises(K.KvrError):
+        K.linear_attention(**LINEARS[what]())
+
+
+def test_heads_first_results_and_states():
+    # (strides in the other order are no overlap)
+    p = R.Linear([70, 1], heads=4, kv_heads=2, dim=64)
+    args = list(p.args())
+    args[3] = args[3].transpose(0, 1).contiguous().transpose(0, 1)
+    out = torch.empty((4, 71, 64), dtype=BF16, device=DEV).transpose(0, 1)
+    K.linear_attention(*args, out=out)
+    R.check_linear(out, args[3], p)
+
+
+def test_two_streams_at_once():
+    p = [R.Linear([900, 3, 200], heads=4, kv_heads=2, dim=128, seed=i) for i in range(2)]
+    x, xs, w, ws, _ = product_problem(300, 512, 700)
+    args, sides = [q.args() for q in p], [torch.cuda.Stream() for _ in p]
+    data = [on(t) for t in (x, w, ws, xs)]
+    torch.cuda.synchronize()
+    got = []
+    for a, side in zip(args, sides):
+        with torch.cuda.stream(side):
+            product = [K.integer_product(*data[:3], x_scale=data[3]) for _ in range(3)]
+            got.append((K.linear_attention(*a), product))
+    torch.cuda.synchronize()
+    for q, a, (out, product) in zip(p, args, got):
+        R.check_linear(out, a[3], q)
+        for y in product:
+            R.check_product(y, *R.product(x.numpy(), xs.numpy(), w.numpy(), ws.numpy(), None), BF16)
+
+
 # ---------------------------------------------------------------- together
 
 

@@ -191,6 +191,22 @@ def test_null_structs_refused():
     assert lib.kvr_linear_workspace(linear(), None) == K.KVR_EINVAL
 
 
+def test_overlapping_pieces():
+    # a lattice of pieces of three elements; those that lie between each other without touching are refused too
+    def touch(n, step, m, each):
+        seen = [i * step + j * each + e for i in range(n) for j in range(m) for e in range(3)]
+        return len(seen) != len(set(seen))
+
+    for n in range(4):
+        for m in range(4):
+            for step in range(14):
+                for each in range(14):
+                    said = L._overlap(n, step, m, each, 3)
+                    assert said or not touch(n, step, m, each), (n, step, m, each)
+                    if n <= 1 or m <= 1 or step >= m * each or each >= n * step:
+                        assert said == touch(n, step, m, each), (n, step, m, each)
+
+
 def test_tensors_on_the_cpu_refused():
     x = torch.zeros((4, 64), dtype=torch.bfloat16)
     w = torch.zeros((8, 64), dtype=torch.int8)
