@@ -48,13 +48,14 @@ inline bool quantised_within(int tokens, int dim, int channels) {
 }
 
 // ---- linear attention ----
-// Requests of up to so many tokens take the recurrent form; where a request has
-// more than kManyTokens on average, all take the chunked one (for which a launch
-// less is done).
-constexpr int kFewTokens = 4;
-constexpr int kManyTokens = 32;
+// Requests of up to so many tokens take the recurrent form (256 requests, us,
+// recurrent and chunked: 32 heads of 64: 1 token 59 and 131, 4 tokens 85 and
+// 134, 8 tokens 121 and 136, 16 tokens 193 and 138; 8 heads of 128: 4 tokens 65
+// and 71, 8 tokens 79 and 74).
+inline int few_tokens(int dim) { return dim == 64 ? 8 : 4; }
 // So many requests of which none is cut are not planned for: every workgroup
-// checks row_start.
+// checks row_start, an entry a thread (one request of 100 tokens, 16 heads: 10.8
+// us, with a plan 13.9; 256 requests of 9 tokens: no difference).
 constexpr int kUnplanned = 256;
 // Workgroups of the chunked form that the device holds.
 constexpr int kLinearSlots = 2 * kComputeUnits;

@@ -283,10 +283,17 @@ kvr_status kvr_linear_attention(const kvr_linear* l, void* d_workspace, size_t b
   a.segment_cap = o.segment_cap;
   a.planned = o.planned;
   // a device that would be half empty takes the queries' heads side by side,
-  // though each keeps the state (33 requests of up to 77 tokens, 15 / 5 heads:
-  // 27.7 -> 22 us)
+  // though each keeps the state (16 requests of 200 tokens, 32 / 4 heads of 128:
+  // 41 instead of 112 us; one that is not, 64 requests, 32 / 8 heads: 153
+  // instead of 108 us)
   a.teams = 2ll * o.segment_cap * l->kv_heads <= kvr::kLinearSlots && a.share <= 65535 ? a.share : 1;
-  a.few = l->d_row_start && l->num_tokens > (int64_t)kvr::kManyTokens * l->num_requests ? -1 : kvr::kFewTokens;
+  // Requests that the device holds at once all take the chunked form, unless
+  // they have a token each: a launch less (16 requests, 32 heads of 64: of 2
+  // tokens 10.1 instead of 12.1 us, of 40 18.8 instead of 21.6).  Of more, those
+  // of few tokens are done sooner apart (100 requests of one token and 100 of 90:
+  // 117 instead of 135 us).
+  const bool at_once = (int64_t)l->num_requests * l->kv_heads <= kvr::kLinearSlots;
+  a.few = l->d_row_start && l->num_tokens > l->num_requests && at_once ? -1 : kvr::few_tokens(l->dim);
   a.scale = l->scale;
   const hipError_t e = kvr::launch_linear(a, l->dtype == KVR_FP16, static_cast<hipStream_t>(hip_stream));
   return e == hipSuccess ? KVR_OK : hip_failed(e, "linear attention kernels launch");

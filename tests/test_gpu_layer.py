@@ -329,6 +329,14 @@ def test_linear_many_requests(dtype):
 
 
 @TYPES
+@DIMS
+@pytest.mark.parametrize("requests", [30, 80])
+def test_linear_short_requests(dtype, dim, requests):
+    # 240 and 640 states: all that the device takes at once, and more; lengths on both sides of a few
+    check_linear(R.Linear([i % 11 for i in range(requests)], heads=8, kv_heads=8, dim=dim, dtype=dtype))
+
+
+@TYPES
 def test_linear_cut_requests_in_place(dtype):
     # cut ones whose last segment writes what the first begins with, teams of query heads beside each other
     check_linear(R.Linear([700, 300, 0, 5], heads=6, kv_heads=2, dtype=dtype, write=None))
