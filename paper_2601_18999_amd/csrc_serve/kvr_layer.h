@@ -68,7 +68,7 @@ struct alignas(32) Segment {
 };
 
 struct LinearHdr {
-  int32_t segments, followed;  // in all, and such that another one follows
+  int32_t segments, followed, cut;  // in all, such that another one follows, and the first ones of those
   int32_t rejected;
 };
 
