@@ -91,7 +91,7 @@ struct LinearLayout {
 };
 
 // Segments of equal length, as many as the device holds workgroups (one takes
-// a segment's key head), but not of fewer than 256 tokens.  Where there are
+// a segment's key head), but hardly of fewer than 256 tokens.  Where there are
 // that many requests, half as many: most are not cut then, which takes no
 // second pass (16 requests of 128 to 1,024 tokens, 32 heads: 136 -> 120 us;
 // one request of 9,216 tokens 132 -> 153 us).
@@ -99,7 +99,17 @@ kvr_status lay_out(const kvr_linear* l, LinearLayout* o) {
   const int64_t tokens = l->num_tokens;
   const int64_t slots = (int64_t)l->num_requests * l->kv_heads < kvr::kLinearSlots ? kvr::kLinearSlots : kvr::kLinearSlots / 2;
   const int64_t even = (tokens * l->kv_heads + slots - 1) / slots;
-  const int64_t segment = even > 256 ? (even + 63) / 64 * 64 : 256;
+  // Shorter ones where the device would be half empty all the same, and the
+  // requests are long enough to be cut; query heads that share a state make the
+  // most of it (us, with 256, 128 and 64 tokens a segment: one request of 200
+  // tokens, 32 / 8 heads of 128: 58, 27, 21.5; of 1,600: 40, 35, 40; of 3,200: 52,
+  // 58, 60; four of 100 tokens, 32 / 32 heads: 22, 22, 29).
+  int64_t least = 256;
+  for (int64_t n = 128; n >= 64; n /= 2)
+    if (tokens * (l->heads + l->kv_heads) <= n * kvr::kLinearSlots &&
+        tokens > (l->heads == l->kv_heads ? 2 * n : n) * l->num_requests)
+      least = n;
+  const int64_t segment = even > least ? (even + 63) / 64 * 64 : least;
   const bool cut = l->d_row_start && tokens > segment;  // whether there can be a request of several segments
   const int64_t cap = l->num_requests + (cut ? tokens / segment : 0);
   // (a launch has fewer than 2^32 threads)
