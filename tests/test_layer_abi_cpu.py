@@ -169,8 +169,9 @@ def test_small_or_missing_workspaces_refused():
     # few requests that are not cut take no workspace
     assert K.kvr_linear_workspace(linear()) == 0 and K.kvr_linear_workspace(linear(num_requests=256)) == 0
     assert K.kvr_linear_workspace(linear(num_requests=257)) > 0
-    assert K.kvr_linear_workspace(linear(num_tokens=256)) == 0
-    cut = dict(num_tokens=257)
+    # (three requests, two heads to a state: cut from 64 tokens each on, as the device would be half empty)
+    assert K.kvr_linear_workspace(linear(num_tokens=192)) == 0
+    cut = dict(num_tokens=193)
     assert K.kvr_linear_workspace(linear(**cut)) >= 2 * 2 * 64 * 64 * 4
     _refused(lambda: K.kvr_linear_attention(linear(**cut), 0, 1 << 40))
     _refused(lambda: K.kvr_linear_attention(linear(**cut), P + 16, 1 << 40))
