@@ -368,39 +368,38 @@ hipError_t launch_direct(const ProductArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-// Few tokens: twice 16 channels a workgroup where there are enough for the
-// device.
-template <class T, class X>
-hipError_t launch_few(const ProductArgs& a, hipStream_t st) {
-  if (a.channels > 32 * (kComputeUnits - 1)) return launch_direct<T, X, 2, 1, 16>(a, st);
-  return launch_direct<T, X, 1, 1, 8>(a, st);
-}
-
 // Which kernel, by what they take (8-bit tokens, bfloat16 results, weights that
 // no cache holds, us; direct kernels by tokens x channels of a workgroup, tiles
 // by channels x tokens and the groups of waves that have k in turn):
-//   tokens x k x channels    direct 16x16  16x32  64x16  64x32   tiles 64x64/2  128x64/2  128x128/1  /2  256x256
-//        8 x  4,096 x  4,096      8.0       8.2    7.9    9.8         12.3         18         25      22     57
-//        8 x  4,096 x 16,384     19.7      16.5   24.9   18.3         16.9         22         26      24     59
-//       16 x 16,384 x  8,192     40.1      35.4   48.1   37.6         41           66         90      77    212
-//       17 x  4,096 x  4,096     10.1       8.4    8.5   10.5         12.5         19         26      23     58
-//       33 x  4,096 x  8,192     23.8      22.1   18.2   12.2         13.6         22         26      24     59
-//      333 x  5,008 x  1,001     24.6      18.6   24.0   13.2         15.3         30         45      42     83
-//      128 x  4,096 x  8,192     62        50     44     25.1         14.8         22         29      28     62
-//      512 x  4,096 x  4,096    117        92     81     47           23.2         20.7       28      27     64
-//      256 x  4,096 x 16,384    243       197    163     92           45           44         31.0    31.1   68
-//    1,024 x  4,096 x  8,192    456       365    315    178           75           74         53.0    56.1   65
-//    2,048 x  4,096 x  8,192    904       727    625    354          143          145        100     109     80
+//   tokens x k x channels    direct 16x16  16x32  32x32  64x32   tiles 64x64/2  128x64/2  128x128/1  /2  256x256
+//        8 x  4,096 x  4,096      8.0       8.2    9.0    9.8         12.3         18         25      22     57
+//        8 x  4,096 x 16,384     19.7      16.5   19.0   18.3         16.9         22         26      24     59
+//       16 x 16,384 x  8,192     40.1      35.4   37.5   37.6         41           66         90      77    212
+//       64 x 16,384 x  1,024     17.8      25.2   33.6   45.4         43.2
+//      532 x  8,592 x    128     14.1      10.5   14.8   18.5         22.6
+//       64 x  4,096 x  2,048     10.0       8.5   10.9   14.3         14.4
+//      200 x  4,096 x  1,024     16.0      13.1    9.8   13.4         12.0
+//       33 x  4,096 x  8,192     23.8      22.1   17.3   12.2         13.6         22         26      24     59
+//      333 x  5,008 x  1,001     24.6      18.6   18.9   13.2         15.3         30         45      42     83
+//      128 x  4,096 x  8,192     62        50     35     25.1         14.8         22         29      28     62
+//      512 x  4,096 x  4,096    117        92     65     47           23.2         20.7       28      27     64
+//      256 x  4,096 x 16,384    243       197    133     92           45           44         31.0    31.1   68
+//    1,024 x  4,096 x  8,192    456       365    252    178           75           74         53.0    56.1   65
+//    2,048 x  4,096 x  8,192    904       727    500    354          143          145        100     109     80
 // The direct kernels are taken as long as one round of workgroups does it (up
-// to 16 tokens, which weights bound, always); of the tiles those that are done
-// first, by the time of a round of one workgroup a compute unit (0.1 us, k =
-// 4,096; those of 128 x 128 without groups are two a compute unit where there
-// are as many).  64 x 64 without groups took 18.7 instead of 14.8 us for 128
-// tokens x 8,192 channels, with four of them 15.8.
+// to 16 tokens, which weights bound, always), the smallest of those; of the
+// tiles those that are done first, by the time of a round of one workgroup a
+// compute unit (0.1 us, k = 4,096; those of 128 x 128 without groups are two a
+// compute unit where there are as many).  64 x 64 without groups took 18.7
+// instead of 14.8 us for 128 tokens x 8,192 channels, with four of them 15.8.
 template <class T, class X>
 hipError_t launch_one_round(const ProductArgs& a, hipStream_t st) {
-  if (a.tokens <= 16) return launch_few<T, X>(a, st);
-  if (product_tiles(a.tokens, a.channels, 64, 16) <= kComputeUnits) return launch_direct<T, X, 1, 4, 16>(a, st);
+  auto fits = [&](int tokens, int channels) {
+    return product_tiles(a.tokens, a.channels, tokens, channels) <= kComputeUnits;
+  };
+  if (fits(16, 16)) return launch_direct<T, X, 1, 1, 8>(a, st);
+  if (a.tokens <= 16 || fits(16, 32)) return launch_direct<T, X, 2, 1, 16>(a, st);
+  if (fits(32, 32)) return launch_direct<T, X, 2, 2, 16>(a, st);
   return launch_direct<T, X, 2, 4, 8>(a, st);
 }
 

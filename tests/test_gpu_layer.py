@@ -192,6 +192,15 @@ def test_product_types(dtype, out, tokens):
     check_product(product_problem(tokens, 336, 260, dtype, bias=tokens == 9), out)
 
 
+@pytest.mark.parametrize("dim", [80, 400])
+@pytest.mark.parametrize("tokens,channels", [
+    (532, 128), (1000, 60), (150, 1600), (200, 1001), (31, 8192), (100, 8190), (129, 8200), (700, 4000), (250, 16300),
+    (1000, 8200), (2040, 8100), (2049, 10000)])
+def test_product_by_results(tokens, channels, dim):
+    # from one round of the smallest workgroups to several of the largest tiles
+    check_product(product_problem(tokens, dim, channels))
+
+
 @pytest.mark.parametrize("tokens,dim", [(1, 16), (7, 65536), (1, 65536), (2, 32784), (16, 4096), (16, 4112), (17, 64),
                                         (15, 1040), (25, 128), (64, 1024), (65, 1008), (100, 640), (1000, 64)])
 @pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
