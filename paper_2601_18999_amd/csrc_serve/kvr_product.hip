@@ -7,6 +7,11 @@
 // split matters.  Everything is computed transposed (channels are the rows of
 // the matrix instructions' results, tokens the columns), so that a lane has
 // four neighbouring channels of one token at a time.
+//
+// Two kernels: tiles that pass through LDS, which the matrix units bound (9,216
+// tokens x 16,384 channels, k = 4,096: 645 us, 1.92 PFLOP/s; 8,192^3 at 2.05),
+// and a direct one for few results, which the weights' bytes bound (16 tokens x
+// 16,384 channels, k = 4,096: 16.5 us, 4.1 TB/s).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
