@@ -120,13 +120,13 @@ def block_norm(x: torch.Tensor, *, after: Optional[torch.Tensor] = None, gate: O
         _no_gradient(where)
     kind = torch.int8 if int8 else dtype
     if out is None:
-        out = torch.empty((tokens, dim), dtype=kind, device=device)
+        out = torch.empty_like(x, dtype=kind, memory_format=torch.contiguous_format)
         p_out, o0 = out.data_ptr(), dim
     else:
         p_out, o0 = _matrix(where, "out", out, (kind,), tokens, dim, device)
         _apart(where, "out", out)
     if int8:
-        scale = torch.empty(tokens, dtype=torch.float32, device=device)
+        scale = x.new_empty(tokens, dtype=torch.float32)
         p_scale = scale.data_ptr()
     if tokens and dim:
         kvr_block_norm(
@@ -182,7 +182,7 @@ def integer_product(x: torch.Tensor, weight: torch.Tensor, weight_scale: torch.T
     if to == 3:
         _refuse(where, f"a result of {dtype} is not supported (bfloat16, float16, float32)")
     if out is None:
-        out = torch.empty((tokens, channels), dtype=dtype, device=device)
+        out = x.new_empty((tokens, channels), dtype=dtype)
         p_out, o0 = out.data_ptr(), channels
     else:
         p_out, o0 = _matrix(where, "out", out, (dtype,), tokens, channels, device)
@@ -190,7 +190,7 @@ def integer_product(x: torch.Tensor, weight: torch.Tensor, weight_scale: torch.T
     nbytes = _product_bytes(code, to, tokens, dim, channels)
     p_work = 0
     if nbytes:
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        ws = x.new_empty(nbytes, dtype=torch.uint8)
         p_work = ws.data_ptr()
     if tokens:
         kvr_integer_product(
@@ -282,6 +282,6 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, state: t
             _refuse(where, "without row_start there is one token a request")
         return out
     nbytes = _linear_bytes(code, tokens, requests, heads, kv_heads, dim, bool(p_rows))
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    ws = q.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
     kvr_linear_attention(args, ws.data_ptr() if nbytes else 0, nbytes, _stream(device.index))
     return out
