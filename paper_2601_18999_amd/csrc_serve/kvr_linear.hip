@@ -42,9 +42,7 @@ constexpr int kThreads = 256;
 constexpr int kChunk = 64;  // tokens
 
 // Whether the request's slots are the pool's (else that is reported).
-__device__ __forceinline__ bool slots_fit(const LinearArgs& a, int request, int& read, int& write) {
-  read = a.read[request];
-  write = a.write[request];
+__device__ __forceinline__ bool slots_fit(const LinearArgs& a, int read, int write) {
   const bool fit = read >= -1 && read < a.slots && write >= -1 && write < a.slots;
   if (!fit && a.status && threadIdx.x == 0) atomicOr(a.status, (uint32_t)KVR_DEV_BAD_PAGE);
   return fit;
@@ -154,17 +152,18 @@ __global__ __launch_bounds__(kThreads) void linear_steps_kernel(LinearArgs a) {
   const uint32_t at = divide(blockIdx.x, a.kv_div);
   const int head = (int)(blockIdx.x - at * a.kv_div.d);
   int row0 = (int)at, rows = 1;
+  const int read = a.read[at], write = a.write[at];  // (on their way while row_start is checked)
+  const float log_decay = a.log_decay[head];
   if (a.row_start) {
+    row0 = a.row_start[at];
+    rows = a.row_start[at + 1] - row0;
     if (rejected(a)) {
       for (int t = (int)at; t < a.tokens; t += a.requests) fill_nan<T>(a, t, 1, head, D);
       return;
     }
-    row0 = a.row_start[at];
-    rows = a.row_start[at + 1] - row0;
     if (rows > a.few) return;
   }
-  int read, write;
-  if (!slots_fit(a, (int)at, read, write)) {
+  if (!slots_fit(a, read, write)) {
     fill_nan<T>(a, row0, rows, head, D);
     return;
   }
@@ -177,7 +176,7 @@ __global__ __launch_bounds__(kThreads) void linear_steps_kernel(LinearArgs a) {
 #pragma unroll
     for (int i = 0; i < kRows; ++i) state[i] = f32x4{0, 0, 0, 0};
   }
-  const float decay = expf(a.log_decay[head]);
+  const float decay = expf(log_decay);
   for (int t = row0; t < row0 + rows; ++t) {
     const T* k = reinterpret_cast<const T*>(a.k + t * a.k_tok + head * a.k_head);
     const T* v = reinterpret_cast<const T*>(a.v + t * a.v_tok + head * a.v_head) + 4 * col;
@@ -400,23 +399,30 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = wave % kGroups, rw = wave / kGroups;
   const uint32_t at = divide(blockIdx.x, a.kv_div);
   const int head = (int)(blockIdx.x - at * a.kv_div.d);
+  const float g = a.log_decay[head];
+  Segment seg;
+  int read = -1, write = -1;
+  if (OUT && !a.planned) {  // (on their way while row_start is checked)
+    const int row0 = a.row_start[at];
+    seg = {(int)at, row0, a.row_start[at + 1] - row0, 0, 1, 0};
+    read = a.read[at];
+    write = a.write[at];
+  }
   if (rejected(a)) {  // (with few >= 0 linear_steps_kernel writes the results)
     if (OUT && a.few < 0 && blockIdx.y == 0)
       for (int t = (int)at; t < a.tokens; t += a.segment_cap) fill_nan<typename T::Type>(a, t, 1, head, D);
     return;
   }
-  Segment seg;
   if (!OUT || a.planned) {
     if ((int)at >= (OUT ? a.hdr->segments : a.hdr->followed)) return;
     seg = a.segments[at];
-  } else {
-    const int row0 = a.row_start[at];
-    seg = {(int)at, row0, a.row_start[at + 1] - row0, 0, 1, 0};
-    if (a.few >= 0 && seg.rows <= a.few) return;
+    read = a.read[seg.request];
+    write = a.write[seg.request];
+  } else if (a.few >= 0 && seg.rows <= a.few) {
+    return;
   }
-  int read, write;
   const int team = OUT ? (int)blockIdx.y : 0;
-  if (!slots_fit(a, seg.request, read, write)) {
+  if (!slots_fit(a, read, write)) {
     if (OUT && team == 0) fill_nan<typename T::Type>(a, seg.row0, seg.rows, head, D);
     return;
   }
@@ -427,7 +433,6 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
   const int teams = seg.parts == 1 && read == write ? 1 : OUT ? a.teams : 1;
   if (team >= teams) return;
   const int s0 = a.share / teams * team, s1 = s0 + a.share / teams;
-  const float g = a.log_decay[head];
   // d^m; a decay of 0 has d^0 = 1
   auto decay_by = [&](int m) { return m ? expf(g * (float)m) : 1.0f; };
 
