@@ -414,8 +414,14 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
     return;
   }
   if (!OUT || a.planned) {
-    if ((int)at >= (OUT ? a.hdr->segments : a.hdr->followed)) return;
-    seg = a.segments[at];
+    const int all = OUT ? a.hdr->segments : a.hdr->followed;
+    int from = (int)at;
+    if (from >= all) return;
+    // The list is the longest first.  Where the device takes all at once, two a
+    // compute unit, the second ones are the shortest first.
+    const int alone = kComputeUnits / a.kv_heads;
+    if (OUT && from >= alone && all * a.kv_heads <= kLinearSlots) from = all - 1 - (from - alone);
+    seg = a.segments[from];
     read = a.read[seg.request];
     write = a.write[seg.request];
   } else if (a.few >= 0 && seg.rows <= a.few) {
