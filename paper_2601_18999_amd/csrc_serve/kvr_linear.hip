@@ -324,22 +324,12 @@ struct Tile {
   static constexpr int kChunks = D / 8, kStepRows = kThreads / kChunks, kN = kChunk / kStepRows;
   s16x8 x[kN];
 
-  // `from`: the lane's chunk of its first row; rows behind `rows`: zeros
-  __device__ __forceinline__ void fetch(const char* from, int64_t stride, int rows, int thread) {
-    const int64_t next = kStepRows * stride;
-    if (rows >= kChunk) {
+  // `from`: the lane's chunk of row 0.  Rows behind `last` are that one again:
+  // nothing branches here, as the compiler waits for loads that a branch may
+  // have made before it goes on.
+  __device__ __forceinline__ void fetch(const char* from, int64_t stride, int row, int last) {
 #pragma unroll
-      for (int i = 0; i < kN; ++i, from += next) x[i] = *(const s16x8*)from;
-    } else {
-#pragma unroll
-      for (int i = 0; i < kN; ++i, from += next) {
-        x[i] = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
-        if (thread / kChunks + i * kStepRows < rows) x[i] = *(const s16x8*)from;
-      }
-    }
-  }
-  static __device__ __forceinline__ const char* lane(const char* from, int64_t stride, int thread) {
-    return from + thread / kChunks * stride + thread % kChunks * 16;
+    for (int i = 0; i < kN; ++i) x[i] = *(const s16x8*)(from + min(row + i * kStepRows, last) * stride);
   }
   // in as many parts as the products take (one tile behind the other)
   template <class T>
@@ -469,14 +459,18 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
   // the state is for results only, costs the others more than it saves.)
   const bool kept = !OUT || (team == 0 && seg.index == seg.parts - 1 && write >= 0);
   const int q_head0 = head * a.share + s0;
-  const char* k_from = Tile<D>::lane(a.k + seg.row0 * a.k_tok + head * a.k_head, a.k_tok, tid);
-  const char* v_from = Tile<D>::lane(a.v + seg.row0 * a.v_tok + head * a.v_head, a.v_tok, tid);
-  const char* q_from = Tile<D>::lane(a.q + seg.row0 * a.q_tok + q_head0 * a.q_head, a.q_tok, tid);
+  const int chunk16 = tid % Tile<D>::kChunks * 16, last = seg.rows - 1;
+  const char* k_from = a.k + seg.row0 * a.k_tok + head * a.k_head + chunk16;
+  const char* v_from = a.v + seg.row0 * a.v_tok + head * a.v_head + chunk16;
+  const char* q_from = a.q + seg.row0 * a.q_tok + q_head0 * a.q_head + chunk16;
 
   Tile<D> tk, tv, tq;
-  tk.fetch(k_from, a.k_tok, seg.rows, tid);
-  tv.fetch(v_from, a.v_tok, seg.rows, tid);
-  if (OUT) tq.fetch(q_from, a.q_tok, seg.rows, tid);
+  if (chunks) {
+    const int row = tid / Tile<D>::kChunks;
+    tk.fetch(k_from, a.k_tok, row, last);
+    tv.fetch(v_from, a.v_tok, row, last);
+    if (OUT) tq.fetch(q_from, a.q_tok, row, last);
+  }
   // scale * d^(i - j) of the scores that this lane computes: queries i = 16
   // wave + lane % 16, keys j = 16 t + 4 (lane / 16) + e, and of those which are
   // not later ones (bit 4 t + e)
@@ -493,42 +487,38 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
         earlier |= (m >= 0) << (4 * t + e);
       }
   }
-#pragma unroll 1
-  for (int chunk = 0; chunk < chunks; ++chunk) {
-    const int row0 = chunk * kChunk, rows = min(kChunk, seg.rows - row0);
-    // (places in LDS are computed where they are used: kept over the loop, they take more registers than there are)
-    asm volatile("" : "+v"(lane), "+v"(n), "+v"(h), "+v"(tid));
-    __syncthreads();  // the tiles of the chunk before are read
+  int chunk = 0, rows = min(kChunk, seg.rows);
+  auto to_lds = [&]() {
     tk.template store_parts<T>(keys, tid);
     tv.store(values, tid);
+    if (OUT) tq.template store_parts<T>(queries, tid);
     if (tid < kChunk && (chunk == 0 || rows < kChunk)) left[tid] = tid < rows ? decay_by(rows - 1 - tid) : 0.0f;
-    // the next chunk's; what is on its way is waited for as a whole, so nothing
-    // is fetched before all that is there is in LDS
-    auto fetch_next = [&]() {
-      if (chunk + 1 == chunks) return;
-      const int behind = seg.rows - row0 - kChunk;
-      k_from += kChunk * a.k_tok;
-      v_from += kChunk * a.v_tok;
-      q_from += kChunk * a.q_tok;
-      tk.fetch(k_from, a.k_tok, behind, tid);
-      tv.fetch(v_from, a.v_tok, behind, tid);
-      if (OUT) tq.fetch(q_from, a.q_tok, behind, tid);
+  };
+  if (chunks) to_lds();
+#pragma unroll 1
+  while (chunk < chunks) {
+    const int row0 = chunk * kChunk;
+    // (places in LDS are computed where they are used: kept over the loop, they take more registers than there are)
+    asm volatile("" : "+v"(lane), "+v"(n), "+v"(h), "+v"(tid));
+    // the next chunk's (behind the last one its last row), and the queries of
+    // the next head
+    const int row = row0 + tid / Tile<D>::kChunks;
+    tk.fetch(k_from, a.k_tok, row + kChunk, last);
+    tv.fetch(v_from, a.v_tok, row + kChunk, last);
+    auto fetch_queries = [&](int s) {
+      const bool here = s < s1 - s0;
+      tq.fetch(q_from + (here ? s * a.q_head : 0), a.q_tok, here ? row : row + kChunk, last);
     };
+    if (OUT) fetch_queries(1);
+    __syncthreads();
     const int v_place = column_place<D, false>(lane) + c * 64;
     if constexpr (OUT) {
 #pragma unroll 1
-      for (int s = 0; s < s1 - s0; ++s) {
-        if (s) __syncthreads();
+      for (int s = 0;; ++s) {
         // (nor are the state's parts kept over this loop)
 #pragma unroll
         for (int t = 0; t < kGroups; ++t) asm volatile("" : "+v"(state[t]));
         asm volatile("" : "+v"(lane), "+v"(n), "+v"(h), "+v"(tid));
-        tq.template store_parts<T>(queries, tid);
-        if (s + 1 < s1 - s0)
-          tq.fetch(q_from + (s + 1) * a.q_head, a.q_tok, rows, tid);
-        else
-          fetch_next();
-        __syncthreads();
         // scores, transposed: keys 16 t .. of the wave's 16 queries; those of later keys are 0, and of a later 32
         // queries' keys are not read
         const char* k_at = keys + Rows<D>::at(lane % 16) + lane / 16 * 16;
@@ -689,17 +679,23 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
           for (int i = 0; i < 4; ++i)
             *(s16x4*)(r_to + Rows<D>::of(32 * t) + i * 16) =
                 T::narrow(f32x4{o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]});
-        const char* r_from = queries + Rows<D>::at(lane / 4) + rw * kRowTiles * Rows<D>::of(32) + c * 64 + lane % 4 * 16;
-        char* to = a.out + (seg.row0 + row0 + first + lane / 4) * a.o_tok + (q_head0 + s) * a.o_head + c * 64 + lane % 4 * 16;
+        // (rows behind the end: the last one again)
+        const char* r_from = queries + c * 64 + lane % 4 * 16;
+        char* to = a.out + (seg.row0 + row0) * a.o_tok + (q_head0 + s) * a.o_head + c * 64 + lane % 4 * 16;
+        if (kRowWaves == 1 || first < rows) {
 #pragma unroll
-        for (int i = 0; i < 2 * kRowTiles; ++i, to += 16 * a.o_tok) {
-          const s16x8 x = *(const s16x8*)(r_from + Rows<D>::of(16 * i));
-          if (first + 16 * i + lane / 4 < rows) __builtin_memcpy(to, &x, sizeof(x));
+          for (int i = 0; i < 2 * kRowTiles; ++i) {
+            const int r = min(first + 16 * i + lane / 4, rows - 1);
+            const s16x8 x = *(const s16x8*)(r_from + Rows<D>::at(r));
+            __builtin_memcpy(to + r * a.o_tok, &x, sizeof(x));
+          }
         }
+        if (s + 1 == s1 - s0) break;
+        __syncthreads();
+        tq.template store_parts<T>(queries, tid);
+        fetch_queries(s + 2);
+        __syncthreads();
       }
-    } else {
-      fetch_next();
-      __syncthreads();
     }
     // the state behind the chunk
     if (!kept && chunk + 1 == chunks) break;
@@ -737,6 +733,10 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
           for (int p = 0; p < P; ++p)
             if (r + p < 3) state[t] = multiply(ks[k & 1][t][p], vp[r], state[t]);
     }
+    if (++chunk == chunks) break;
+    rows = min(kChunk, seg.rows - chunk * kChunk);
+    __syncthreads();  // the tiles are read
+    to_lds();
   }
 
   // (read again: kept over the loop, they are more than the scalar registers hold)
