@@ -171,6 +171,9 @@ def test_small_or_missing_workspaces_refused():
     assert K.kvr_linear_workspace(linear(num_requests=257)) > 0
     # (three requests, two heads to a state: cut from 64 tokens each on, as the device would be half empty)
     assert K.kvr_linear_workspace(linear(num_tokens=192)) == 0
+    # (short ones are not, while they are few tokens in all)
+    assert K.kvr_linear_workspace(linear(num_tokens=512, num_requests=32)) == 0
+    assert K.kvr_linear_workspace(linear(num_tokens=512, num_requests=31)) > 0
     cut = dict(num_tokens=193)
     assert K.kvr_linear_workspace(linear(**cut)) >= 2 * 2 * 64 * 64 * 4
     _refused(lambda: K.kvr_linear_attention(linear(**cut), 0, 1 << 40))
