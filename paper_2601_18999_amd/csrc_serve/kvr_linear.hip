@@ -13,8 +13,8 @@
 // fill the device: one pass adds up what each segment brings to the state, a
 // second one turns these into the states before the segments, and the third
 // one computes the results of all segments side by side.  One request of 9,216
-// tokens, 32 heads of 128: 38 + 12 + 91 us, where the bytes of the three take 30
-// + 13 + 60.  In the last one the matrix units are busy for 26% of the time and
+// tokens, 32 heads of 128: 38 + 12 + 84 us, where the bytes of the three take 30
+// + 13 + 60.  In the last one the matrix units are busy for 28% of the time and
 // the vector units, which split the state and weigh the scores, for 38%; two
 // waves a SIMD, which is what their registers allow, hide little of the one
 // behind the other, or of the loads.
