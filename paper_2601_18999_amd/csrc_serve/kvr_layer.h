@@ -49,10 +49,10 @@ inline bool quantised_within(int tokens, int dim, int channels) {
 
 // ---- linear attention ----
 // Requests of up to so many tokens take the recurrent form (256 requests, us,
-// recurrent and chunked: 32 heads of 64: 1 token 59 and 131, 4 tokens 85 and
-// 134, 8 tokens 121 and 136, 16 tokens 193 and 138; 8 heads of 128: 4 tokens 65
-// and 71, 8 tokens 79 and 74).
-inline int few_tokens(int dim) { return dim == 64 ? 8 : 4; }
+// recurrent and chunked: 32 heads of 64: 1 token 64 and 120, 4 tokens 77 and
+// 121, 8 tokens 103 and 121, 12 tokens 130 and 121; 8 heads of 128: 4 tokens 63
+// and 70, 8 tokens 74 and 73, 12 tokens 85 and 74).
+constexpr int kFewTokens = 8;
 // So many requests of which none is cut are not planned for: every workgroup
 // checks row_start, an entry a thread (one request of 100 tokens, 16 heads: 10.8
 // us, with a plan 13.9; 256 requests of 9 tokens: no difference).

@@ -307,7 +307,7 @@ kvr_status kvr_linear_attention(const kvr_linear* l, void* d_workspace, size_t b
   // of few tokens are done sooner apart (100 requests of one token and 100 of 90:
   // 117 instead of 135 us).
   const bool at_once = (int64_t)l->num_requests * l->kv_heads <= kvr::kLinearSlots;
-  a.few = l->d_row_start && l->num_tokens > l->num_requests && at_once ? -1 : kvr::few_tokens(l->dim);
+  a.few = l->d_row_start && l->num_tokens > l->num_requests && at_once ? -1 : kvr::kFewTokens;
   a.scale = l->scale;
   const hipError_t e = kvr::launch_linear(a, l->dtype == KVR_FP16, static_cast<hipStream_t>(hip_stream));
   return e == hipSuccess ? KVR_OK : hip_failed(e, "linear attention kernels launch");
