@@ -97,7 +97,8 @@ struct LinearLayout {
 // one request of 9,216 tokens 132 -> 153 us).
 kvr_status lay_out(const kvr_linear* l, LinearLayout* o) {
   const int64_t tokens = l->num_tokens;
-  const int64_t slots = (int64_t)l->num_requests * l->kv_heads < kvr::kLinearSlots ? kvr::kLinearSlots : kvr::kLinearSlots / 2;
+  const bool many = (int64_t)l->num_requests * l->kv_heads >= kvr::kLinearSlots;
+  const int64_t slots = many ? kvr::kLinearSlots / 2 : kvr::kLinearSlots;
   const int64_t even = (tokens * l->kv_heads + slots - 1) / slots;
   // Shorter ones where the device would be half empty all the same, and the
   // requests are long enough to be cut; query heads that share a state make the
@@ -249,7 +250,8 @@ kvr_status kvr_linear_attention(const kvr_linear* l, void* d_workspace, size_t b
   st = lay_out(l, &o);
   if (st != KVR_OK) return st;
   if (!l->d_state || !l->d_log_decay || !l->d_read) return invalid("d_state, d_log_decay and d_read are required");
-  if (l->num_tokens && (!l->d_q || !l->d_k || !l->d_v || !l->d_out)) return invalid("d_q, d_k, d_v and d_out are required");
+  if (l->num_tokens && (!l->d_q || !l->d_k || !l->d_v || !l->d_out))
+    return invalid("d_q, d_k, d_v and d_out are required");
   kvr::LinearArgs a;
   a.q_tok = step(l->q_token, l->num_tokens, 2);
   a.q_head = step(l->q_head, l->heads, 2);

@@ -74,8 +74,9 @@ __device__ __forceinline__ bool rejected(const LinearArgs& a) {
 }
 
 // Checks row_start and lists the segments: those that others follow, which are
-// full (the requests' first ones before the others), then the last ones, the longest first (the workgroups that start last
-// then have little to do).  One workgroup.
+// full (the requests' first ones before the others), then the last ones, the
+// longest first (the workgroups that start last then have little to do).  One
+// workgroup.
 __global__ __launch_bounds__(kThreads) void linear_plan_kernel(LinearArgs a) {
   constexpr int kKinds = 64;  // by chunks, the last one all longer ones
   __shared__ int place[kKinds], followed, cut, slots;
@@ -274,10 +275,12 @@ __device__ __forceinline__ void split(f32x8 x, s16x8 (&part)[N]) {
   }
 }
 __device__ __forceinline__ f32x16 multiply(s16x8 a, s16x8 b, f32x16 c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0,
+                                                 0);
 }
 __device__ __forceinline__ f32x4 multiply(s16x8 a, s16x8 b, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0,
+                                                 0);
 }
 
 // Tokens as the matrix units take them: bfloat16 as they are, halves as two
@@ -773,7 +776,8 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
     to = z.added + ((int64_t)(seg.slot + seg.index + 1) * z.kv_heads + head) * D * D;
   } else if (team == 0 && seg.index == seg.parts - 1) {
     const int into = z.write[seg.request];
-    if (into >= 0 && (seg.rows || into != z.read[seg.request])) to = z.state + into * z.state_slot + head * z.state_head;
+    if (into >= 0 && (seg.rows || into != z.read[seg.request]))
+      to = z.state + into * z.state_slot + head * z.state_head;
   }
   if (to && rw == 0) {
 #pragma unroll

@@ -348,8 +348,9 @@ def test_linear_short_requests(dtype, dim, requests):
 @TYPES
 @pytest.mark.parametrize("in_place", [False, True], ids=["apart", "in place"])
 @pytest.mark.parametrize("new, heads, kv, dim", [
-    ([65], 8, 2, 128), ([64], 8, 2, 128), ([200], 8, 2, 64), ([129], 4, 4, 64), ([577], 4, 4, 128), ([1153], 16, 4, 128),
-    ([70] * 19, 4, 1, 64), ([129, 0, 300], 6, 2, 128), ([1] * 30 + [300] + [2, 0] * 15, 4, 2, 128), ([1, 640, 64, 128], 6, 3, 64)])
+    ([65], 8, 2, 128), ([64], 8, 2, 128), ([200], 8, 2, 64), ([129], 4, 4, 64), ([577], 4, 4, 128),
+    ([1153], 16, 4, 128), ([70] * 19, 4, 1, 64), ([129, 0, 300], 6, 2, 128),
+    ([1] * 30 + [300] + [2, 0] * 15, 4, 2, 128), ([1, 640, 64, 128], 6, 3, 64)])
 def test_linear_a_few_longer_requests(new, heads, kv, dim, in_place, dtype):
     # that are cut finely, as the device would be half empty
     n = len(new)
