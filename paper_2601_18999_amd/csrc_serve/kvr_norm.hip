@@ -36,21 +36,23 @@ __device__ __forceinline__ u32x4 load16(const char* p) {
 }
 
 // Eight elements of a row of n from `at` on, as they stand in memory; 0 behind
-// its end.
-template <class T>
+// its end.  EVEN: n is a multiple of 8; no branch stands around its loads, as
+// the compiler waits for one that a branch may have made before it goes on.
+template <class T, bool EVEN>
 struct Raw {
   static constexpr int kLoads = sizeof(T) / 2, kEach = 16 / sizeof(T);  // elements of a load
   u32x4 x[kLoads];
 
   __device__ __forceinline__ void load(const char* row, int at, int n) {
+    if constexpr (EVEN) {
+      const int from = min(at, n - 8);
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) x[i] = load16(row + (from + i * kEach) * (int)sizeof(T));
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) x[i] = u32x4{0, 0, 0, 0};
-    if (n % 8 == 0) {
-      if (at < n) {
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) x[i] = load16(row + (at + i * kEach) * (int)sizeof(T));
-      }
-    } else if (n >= 8) {
+    if (n >= 8) {
       // those that would end behind the row end with it, and are shifted
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
@@ -71,11 +73,11 @@ struct Raw {
     }
   }
 
-  __device__ __forceinline__ void widen(float (&f)[8]) const {
+  __device__ __forceinline__ void widen(float (&f)[8], int at, int n) const {
     Eight<T> y;
     __builtin_memcpy(&y, x, sizeof(y));
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = (float)y.e[i];
+    for (int i = 0; i < 8; ++i) f[i] = !EVEN || at < n ? (float)y.e[i] : 0.0f;
   }
 };
 
@@ -98,7 +100,7 @@ __device__ __forceinline__ void store8(char* row, int at, int n, const float (&f
 // T: the type of x, R: of the residual.  Several rows a compute unit are on
 // their way at once, which takes few registers for each: with 180 instead of
 // 64 (eight waves of a row of 4,096, V = 1) 9,216 rows took 144 us.
-template <class T, class R, bool SINGLE, int V>
+template <class T, class R, bool SINGLE, int V, bool EVEN>
 __global__ __launch_bounds__(SINGLE ? 256 : 64 * kMostWaves, V == 1 ? 8 : 4) void norm_kernel(NormArgs a) {
   __shared__ float sums[2][kMostWaves];
   __shared__ uint32_t tops[kMostWaves];
@@ -124,14 +126,14 @@ __global__ __launch_bounds__(SINGLE ? 256 : 64 * kMostWaves, V == 1 ? 8 : 4) voi
     return s * a.inv_dim;
   };
   auto weigh = [&](float(&f)[V][8], const char* weight, int which) {
-    Raw<T> raw[V];
+    Raw<T, EVEN> raw[V];
     if (V == 1) raw[0].load(weight, at0, a.dim);
     const float by = __builtin_amdgcn_rsqf(mean_square(f, which) + a.eps);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       if (V > 1) raw[v].load(weight, at0 + v * next, a.dim);
       float w[8];
-      raw[v].widen(w);
+      raw[v].widen(w, at0 + v * next, a.dim);
 #pragma unroll
       for (int i = 0; i < 8; ++i) f[v][i] = f[v][i] * by * w[i];
     }
@@ -140,8 +142,8 @@ __global__ __launch_bounds__(SINGLE ? 256 : 64 * kMostWaves, V == 1 ? 8 : 4) voi
 #pragma unroll 1
   for (int64_t row = first; row < a.tokens; row += step) {
     // what comes from far is on its way before the first sum is waited for
-    Raw<T> raw_x[V], raw_gate[V];
-    Raw<R> raw_res[V];
+    Raw<T, EVEN> raw_x[V], raw_gate[V];
+    Raw<R, EVEN> raw_res[V];
     const char *gate = a.gate + row * a.gate_tok, *res = a.residual + row * a.res_tok;
 #pragma unroll
     for (int v = 0; v < V; ++v) raw_x[v].load(a.x + row * a.x_tok, at0 + v * next, a.dim);
@@ -149,14 +151,14 @@ __global__ __launch_bounds__(SINGLE ? 256 : 64 * kMostWaves, V == 1 ? 8 : 4) voi
     if (V == 1 && a.residual) raw_res[0].load(res, at0, a.dim);
     float f[V][8];
 #pragma unroll
-    for (int v = 0; v < V; ++v) raw_x[v].widen(f[v]);
+    for (int v = 0; v < V; ++v) raw_x[v].widen(f[v], at0 + v * next, a.dim);
     if (a.after) weigh(f, a.after, 0);
     if (a.gate) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         if (V > 1) raw_gate[v].load(gate, at0 + v * next, a.dim);
         float g[8];
-        raw_gate[v].widen(g);
+        raw_gate[v].widen(g, at0 + v * next, a.dim);
         if (a.activation != KVR_ACT_NONE) {
           // (an error of the exponent's product is one of |g| half steps)
 #pragma unroll
@@ -174,7 +176,7 @@ __global__ __launch_bounds__(SINGLE ? 256 : 64 * kMostWaves, V == 1 ? 8 : 4) voi
         const int at = at0 + v * next;
         if (V > 1) raw_res[v].load(res, at, a.dim);
         float r[8];
-        raw_res[v].widen(r);
+        raw_res[v].widen(r, at, a.dim);
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[v][i] = __builtin_fmaf(a.residual_scale, f[v][i], r[i]);
         store8<R>(a.residual_out + row * a.res_out_tok, at, a.dim, f[v]);
@@ -222,7 +224,11 @@ template <class T, class R, bool SINGLE, int V>
 void launch(const NormArgs& a, hipStream_t st) {
   const int64_t rows = SINGLE ? ((int64_t)a.tokens + 3) / 4 : a.tokens;
   const int threads = SINGLE ? 256 : (a.dim + 512 * V - 1) / (512 * V) * 64;
-  norm_kernel<T, R, SINGLE, V><<<(uint32_t)(rows < kMostBlocks ? rows : kMostBlocks), threads, 0, st>>>(a);
+  const uint32_t blocks = (uint32_t)(rows < kMostBlocks ? rows : kMostBlocks);
+  if (a.dim % 8 == 0)
+    norm_kernel<T, R, SINGLE, V, true><<<blocks, threads, 0, st>>>(a);
+  else
+    norm_kernel<T, R, SINGLE, V, false><<<blocks, threads, 0, st>>>(a);
 }
 
 // Values of a lane: 16, which have more of a row on its way for each of its
