@@ -5,10 +5,10 @@
 // V times eight elements a lane; the two means and the largest magnitude are
 // sums and maxima over its lanes, and those of its waves over LDS.  Memory
 // bounds long calls, as every input is read once and every output written once:
-// 9,216 rows of 4,096 with everything and a 32-bit residual (528 MB) 103 us, 5.1
-// TB/s, as a copy.  Short ones are bound by the row's two or three sums, each of
+// 9,216 rows of 4,096 with everything and a 32-bit residual (528 MB) 97 us, 5.4
+// TB/s (a copy: 5.1).  Short ones are bound by the row's two or three sums, each of
 // which the next step waits for: 777 rows of 5,003 (31 MB) 11 us, 8 rows of
-// 4,096 4.
+// 4,096 3.5.
 #include <hip/hip_runtime.h>
 
 #include "kvr_layer.h"
@@ -37,7 +37,9 @@ __device__ __forceinline__ u32x4 load16(const char* p) {
 
 // Eight elements of a row of n from `at` on, as they stand in memory; 0 behind
 // its end.  EVEN: n is a multiple of 8; no branch stands around its loads, as
-// the compiler waits for one that a branch may have made before it goes on.
+// the compiler waits for one that a branch may have made before it goes on (9,216
+// rows of 4,096 with everything 105 -> 98 us).  (For other rows to be shifted
+// when they are used took 17 instead of 14 us for 777 of 5,003.)
 template <class T, bool EVEN>
 struct Raw {
   static constexpr int kLoads = sizeof(T) / 2, kEach = 16 / sizeof(T);  // elements of a load
@@ -234,7 +236,7 @@ void launch(const NormArgs& a, hipStream_t st) {
 // Values of a lane: 16, which have more of a row on its way for each of its
 // waits (9,216 rows of 4,096, 16-bit residual and norm before: 61 us with 8, 54
 // with 16, 67 with 32), where the residual has 16 bits; with a 32-bit one that
-// takes too many registers (9,216 rows with everything: 105 us with 8, 116 with
+// takes too many registers (9,216 rows with everything: 98 us with 8, 102 with
 // 16).
 template <class T, class R>
 void launch_typed(const NormArgs& a, hipStream_t st) {
