@@ -39,6 +39,30 @@ inline int64_t product_tiles(int64_t tokens, int64_t channels, int tile_tokens, 
   return (tokens + tile_tokens - 1) / tile_tokens * ((channels + tile_channels - 1) / tile_channels);
 }
 
+// Tiles that pass through LDS, and the groups of waves that have k in turn.
+struct ProductTile {
+  int channels, tokens, groups, threads;
+};
+
+// Those that are done first, by the time of a round of one workgroup a compute
+// unit (0.1 us, k = 4,096; those of 128 x 128 without groups are two a compute
+// unit where there are as many; kvr_product.hip has the table).  Tiles 64 wide
+// are left to others where they are more than a launch holds (it has fewer than
+// 2^32 threads): up to 64 channels of 2^29 tokens.
+inline ProductTile product_tile(int64_t tokens, int64_t channels) {
+  auto rounds = [&](int c, int t) { return (product_tiles(tokens, channels, t, c) + kComputeUnits - 1) / kComputeUnits; };
+  auto time = [&](int64_t round, int c, int t) {
+    return product_tiles(tokens, channels, t, c) < 1 << 23 ? round * rounds(c, t) : INT64_MAX;
+  };
+  const int64_t r128 = rounds(128, 128);
+  const int64_t t64 = time(115, 64, 64), t12864 = time(175, 128, 64), t128 = r128 == 1 ? 270 : 245 * r128,
+                t256 = 620 * rounds(256, 256);
+  if (t64 <= t12864 && t64 <= t128 && t64 <= t256) return {64, 64, 2, 512};
+  if (t12864 <= t128 && t12864 <= t256) return {128, 64, 2, 512};
+  if (t256 < t128) return {256, 256, 1, 512};
+  return r128 == 1 ? ProductTile{128, 128, 2, 512} : ProductTile{128, 128, 1, 256};
+}
+
 // Whether tokens of 16 bits are brought to integers by every workgroup of the
 // product for itself: where they are few elements, and the product is of one
 // round of workgroups or of up to 16 tokens (25 tokens x 128 x 1,408: 12.8 us

@@ -50,7 +50,7 @@ kvr_status check(const kvr_product* p) {
   // (sums of 65,536 products of 8-bit integers are below 2^31)
   if (p->dim < 16 || p->dim > 65536 || p->dim % 16) return invalid("dim must be a multiple of 16 in 16..65536");
   if (p->channels < 1 || p->channels > (1 << 24)) return invalid("channels must be in 1..2^24");
-  // (a launch has fewer than 2^32 threads, a tile up to 512)
+  // (a launch has fewer than 2^32 threads, a tile up to 512; product_tile takes none of which there are more)
   if ((int64_t)(p->num_tokens / 128 + 1) * (p->channels / 128 + 1) >= 1 << 23)
     return invalid("too many tokens and channels for one call: (num_tokens / 128 + 1) * (channels / 128 + 1) must be "
                    "below 2^23");

@@ -393,10 +393,8 @@ hipError_t launch_direct(const ProductArgs& a, hipStream_t st) {
 //    2,048 x  4,096 x  8,192    904       727    500    354          143          145        100     109     80
 // The direct kernels are taken as long as one round of workgroups does it (up
 // to 16 tokens, which weights bound, always), the smallest of those; of the
-// tiles those that are done first, by the time of a round of one workgroup a
-// compute unit (0.1 us, k = 4,096; those of 128 x 128 without groups are two a
-// compute unit where there are as many).  64 x 64 without groups took 18.7
-// instead of 14.8 us for 128 tokens x 8,192 channels, with four of them 15.8.
+// tiles product_tile's.  64 x 64 without groups took 18.7 instead of 14.8 us for
+// 128 tokens x 8,192 channels, with four of them 15.8.
 template <class T, class X>
 hipError_t launch_one_round(const ProductArgs& a, hipStream_t st) {
   auto fits = [&](int tokens, int channels) {
@@ -414,16 +412,11 @@ hipError_t launch(const ProductArgs& a, hipStream_t st) {
   if (a.dtype == KVR_FP16) return launch_one_round<T, _Float16>(a, st);
   if (a.tokens <= 16 || product_tiles(a.tokens, a.channels, 64, 32) <= kComputeUnits)
     return launch_one_round<T, int8_t>(a, st);
-  auto rounds = [&](int channels, int tokens) {
-    return (product_tiles(a.tokens, a.channels, tokens, channels) + kComputeUnits - 1) / kComputeUnits;
-  };
-  const int64_t r128 = rounds(128, 128);
-  const int64_t t64 = 115 * rounds(64, 64), t12864 = 175 * rounds(128, 64), t128 = r128 == 1 ? 270 : 245 * r128,
-                t256 = 620 * rounds(256, 256);
-  if (t64 <= t12864 && t64 <= t128 && t64 <= t256) return launch_tiles<T, 2, 2, 1, 1, 4, 2>(a, st);
-  if (t12864 <= t128 && t12864 <= t256) return launch_tiles<T, 2, 2, 2, 1, 4, 2>(a, st);
-  if (t256 < t128) return launch_tiles<T, 4, 2, 2, 4, 4, 1>(a, st);
-  return r128 == 1 ? launch_tiles<T, 2, 2, 2, 2, 4, 2>(a, st) : launch_tiles<T, 2, 2, 2, 2, 4, 1>(a, st);
+  const ProductTile tile = product_tile(a.tokens, a.channels);
+  if (tile.channels == 64) return launch_tiles<T, 2, 2, 1, 1, 4, 2>(a, st);
+  if (tile.tokens == 64) return launch_tiles<T, 2, 2, 2, 1, 4, 2>(a, st);
+  if (tile.channels == 256) return launch_tiles<T, 4, 2, 2, 4, 4, 1>(a, st);
+  return tile.groups == 2 ? launch_tiles<T, 2, 2, 2, 2, 4, 2>(a, st) : launch_tiles<T, 2, 2, 2, 2, 4, 1>(a, st);
 }
 
 }  // namespace

@@ -1,0 +1,25 @@
+"""Edges of the norms, 8-bit products and linear attention on the GPU: sizes at a
+launch's limit, arguments at the ends of their ranges, what a call refuses."""
+import pytest
+import torch
+
+import paper_2601_18999_amd as K
+from gpu_helpers import note
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF16, FP16, F32 = torch.bfloat16, torch.float16, torch.float32
+
+
+def test_product_of_more_tokens_than_narrow_tiles_fit_a_launch():
+    # 2^29 tokens that are one in memory (tiles of 64 x 64 would be 2^32 threads), each with a scale of its own
+    tokens, channels, dim = 1 << 29, 3, 16
+    g = torch.Generator().manual_seed(0)
+    x, w = (torch.randint(-128, 128, (n, dim), generator=g, dtype=torch.int8).to(DEV) for n in (1, channels))
+    ws = (torch.rand(channels, generator=g) + 0.5).to(DEV)
+    xs = torch.arange(tokens, device=DEV, dtype=torch.int32).remainder_(509).add_(1).float()
+    note(f"product {tokens} x {dim} x {channels}")
+    got = K.integer_product(x.expand(tokens, dim), w, ws, x_scale=xs)
+    sums = (x.double() @ w.double().t()).float()
+    for c in range(channels):
+        assert torch.equal(got[:, c], (sums[0, c] * xs * ws[c]).bfloat16())
