@@ -130,7 +130,10 @@ __global__ __launch_bounds__(SINGLE ? 256 : 64 * kMostWaves, V == 1 ? 8 : 4) voi
   auto weigh = [&](float(&f)[V][8], const char* weight, int which) {
     Raw<T, EVEN> raw[V];
     if (V == 1) raw[0].load(weight, at0, a.dim);
-    const float by = __builtin_amdgcn_rsqf(mean_square(f, which) + a.eps);
+    // (the instruction takes a subnormal number for 0)
+    const float mean = mean_square(f, which) + a.eps;
+    const bool small = mean < 0x1p-126f;
+    const float by = __builtin_amdgcn_rsqf(small ? mean * 0x1p64f : mean) * (small ? 0x1p32f : 1.0f);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       if (V > 1) raw[v].load(weight, at0 + v * next, a.dim);
