@@ -126,7 +126,8 @@ def block_norm(x: torch.Tensor, *, after: Optional[torch.Tensor] = None, gate: O
         p_out, o0 = _matrix(where, "out", out, (kind,), tokens, dim, device)
         _apart(where, "out", out)
     if int8:
-        scale = x.new_empty(tokens, dtype=torch.float32)
+        # (no kernel runs for rows without an element)
+        scale = x.new_empty(tokens, dtype=torch.float32) if dim else x.new_zeros(tokens, dtype=torch.float32)
         p_scale = scale.data_ptr()
     if tokens and dim:
         kvr_block_norm(

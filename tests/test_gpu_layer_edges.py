@@ -44,3 +44,9 @@ def test_norm_with_the_smallest_eps(dim, eps):
         n, _, mn, _ = R.norm(x, **{which: w}, eps=eps)
         R.check_norm(got, n, mn, BF16)
         assert (got[0] == 0).all()
+
+
+def test_norm_of_no_column_has_the_scale_0():
+    torch.full((5,), float("nan"), device=DEV)  # what the allocator hands out next
+    got = K.block_norm(torch.empty((5, 0), dtype=BF16, device=DEV), int8=True)
+    assert got.out.shape == (5, 0) and (got.scale == 0).all()
