@@ -6,8 +6,8 @@ states (``kvr_block_norm``, ``kvr_integer_product`` and
 As in ``serve``: the functions check what the C side cannot see (types, shapes,
 devices), marshal the arguments and launch on torch's current stream of the
 tensors' device; they neither synchronise nor copy to the host; errors raise
-``KvrError``; there are no gradients, and a call whose result would need one is
-refused.
+``KvrError``; there are no gradients, and a call whose result would need one, or
+would have a tangent, is refused.
 """
 from __future__ import annotations
 
@@ -16,9 +16,10 @@ import struct
 from typing import NamedTuple, Optional
 
 import torch
+from torch.autograd import forward_ad
 
 from . import (kvr_block_norm, kvr_integer_product, kvr_linear_attention, kvr_linear_workspace, kvr_product_workspace)
-from .serve import _current, _gpu, _no_gradient, _refuse, _status, _stream, _vector
+from .serve import _current, _gpu, _no_gradient, _no_tangent, _refuse, _status, _stream, _vector
 
 DTYPE_CODES = {torch.bfloat16: 0, torch.float16: 1, torch.int8: 3, torch.float32: 4}
 ACTIVATIONS = {"none": 0, "sigmoid": 1, "silu": 2}
@@ -118,6 +119,8 @@ def block_norm(x: torch.Tensor, *, after: Optional[torch.Tensor] = None, gate: O
             (residual is not None and residual.requires_grad) or (before is not None and before.requires_grad) or \
             (out is not None and out.requires_grad):
         _no_gradient(where)
+    if forward_ad._current_level >= 0:
+        _no_tangent(where, x, after, gate, residual, before, out)
     kind = torch.int8 if int8 else dtype
     if out is None:
         out = torch.empty_like(x, dtype=kind, memory_format=torch.contiguous_format)
@@ -177,6 +180,8 @@ def integer_product(x: torch.Tensor, weight: torch.Tensor, weight_scale: torch.T
     if x.requires_grad or weight_scale.requires_grad or (int8 and x_scale.requires_grad) or \
             (bias is not None and bias.requires_grad) or (out is not None and out.requires_grad):
         _no_gradient(where)
+    if forward_ad._current_level >= 0:
+        _no_tangent(where, x, weight_scale, x_scale, bias, out)
     if dtype is None:
         dtype = out.dtype if out is not None else torch.bfloat16 if int8 else x.dtype
     code, to = DTYPE_CODES[x.dtype], DTYPE_CODES.get(dtype, 3)
@@ -235,6 +240,8 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, state: t
                                     status=status)
     if q.requires_grad or k.requires_grad or v.requires_grad or state.requires_grad or log_decay.requires_grad:
         _no_gradient(where)
+    if forward_ad._current_level >= 0:
+        _no_tangent(where, q, k, v, state, log_decay, out)
     if q.dtype not in HALVES or q.dim() != 3:
         _refuse(where, "q must be [tokens, heads, dim] of torch.bfloat16 or torch.float16")
     tokens, heads, dim = q.shape

@@ -7,7 +7,8 @@ marshal the arguments and launch on torch's current stream of the tensors'
 device.  They neither synchronise nor copy to the host; workspaces and outputs
 come from torch's allocator.  Errors raise ``KvrError``.  They have no
 gradients: a call whose result would need one is refused (call under
-``torch.no_grad`` or ``torch.inference_mode``).
+``torch.no_grad`` or ``torch.inference_mode``), and so is one whose result
+would have a tangent.
 """
 from __future__ import annotations
 
@@ -16,6 +17,7 @@ import struct
 from typing import NamedTuple, Optional
 
 import torch
+from torch.autograd import forward_ad
 
 from . import (KVR_EINVAL, KvrError, kvr_attention_workspace, kvr_block_tables, kvr_block_tables_workspace,
                kvr_cache_store, kvr_shared_attention)
@@ -80,6 +82,13 @@ def _no_gradient(where: str) -> None:
     """Called where an argument requires one."""
     if torch.is_grad_enabled():
         _refuse(where, "there is no gradient: call under torch.no_grad(), or with detached tensors")
+
+
+def _no_tangent(where: str, *tensors) -> None:
+    """Called where forward mode has a level (``forward_ad._current_level`` >= 0)."""
+    if torch._C._is_fwd_grad_enabled() and \
+            any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        _refuse(where, "there is no tangent: call with the primal tensors")
 
 
 # of a device's index; of the current device
@@ -205,6 +214,8 @@ def cache_store(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache
             return cache_store(k, v, k_cache, v_cache, slots, k_scale=k_scale, v_scale=v_scale, status=status)
     if k.requires_grad or v.requires_grad or k_cache.requires_grad or v_cache.requires_grad:
         _no_gradient(where)
+    if forward_ad._current_level >= 0:
+        _no_tangent(where, k, v, k_cache, v_cache, k_scale, v_scale)
     cache = _cache_args(where, k_cache, v_cache, k_scale, v_scale, device)
     shape = k.shape
     if k.dtype is not v.dtype or v.device != device or len(shape) != 3 or shape != v.shape or \
@@ -250,6 +261,8 @@ def shared_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
                                     status=status)
     if q.requires_grad or k_cache.requires_grad or v_cache.requires_grad:
         _no_gradient(where)
+    if forward_ad._current_level >= 0:
+        _no_tangent(where, q, k_cache, v_cache, k_scale, v_scale, out)
     cache = _cache_args(where, k_cache, v_cache, k_scale, v_scale, device)
     _, _, kv_heads, dim = k_cache.shape
     if q.dim() != 3 or q.shape[2] != dim:

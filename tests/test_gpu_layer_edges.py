@@ -50,3 +50,69 @@ def test_norm_of_no_column_has_the_scale_0():
     torch.full((5,), float("nan"), device=DEV)  # what the allocator hands out next
     got = K.block_norm(torch.empty((5, 0), dtype=BF16, device=DEV), int8=True)
     assert got.out.shape == (5, 0) and (got.scale == 0).all()
+
+
+def norm_args():
+    return dict(x=z(4, 8), after=z(8), gate=z(4, 8), residual=z(4, 8), before=z(8), out=z(4, 8))
+
+
+def product_args():
+    return dict(x=z(4, 32, dtype=torch.int8), weight=z(8, 32, dtype=torch.int8), weight_scale=z(8, dtype=F32),
+                x_scale=z(4, dtype=F32), bias=z(8, dtype=F32), out=z(4, 8))
+
+
+def linear_args():
+    return dict(q=z(3, 4, 64), k=z(3, 2, 64), v=z(3, 2, 64), state=z(5, 2, 64, 64, dtype=F32), log_decay=z(2, dtype=F32),
+                read=torch.full((3,), -1, dtype=torch.int32, device=DEV), out=z(3, 4, 64))
+
+
+def store_args():
+    return dict(k=z(3, 2, 64), v=z(3, 2, 64), k_cache=z(4, 16, 2, 64), v_cache=z(4, 16, 2, 64),
+                slots=z(3, dtype=torch.int32), k_scale=z(2, dtype=F32), v_scale=z(2, dtype=F32))
+
+
+def attention_args():
+    i32 = torch.int32
+    return dict(q=z(3, 4, 64), k_cache=z(4, 16, 2, 64), v_cache=z(4, 16, 2, 64), row_start=None,
+                table=z(3, 1, dtype=i32), length=torch.ones(3, dtype=i32, device=DEV), out=z(3, 4, 64),
+                k_scale=z(2, dtype=F32), v_scale=z(2, dtype=F32))
+
+
+CALLS = {"block_norm": norm_args, "integer_product": product_args, "linear_attention": linear_args,
+         "cache_store": store_args, "shared_attention": attention_args}
+FLOATS = {"block_norm": ["x", "after", "gate", "residual", "before", "out"],
+          "integer_product": ["x", "weight_scale", "x_scale", "bias", "out"],
+          "linear_attention": ["q", "k", "v", "state", "log_decay", "out"],
+          "cache_store": ["k", "v", "k_cache", "v_cache"], "shared_attention": ["q", "k_cache", "v_cache", "out"]}
+
+
+@pytest.mark.parametrize("what,name", [(c, n) for c in FLOATS for n in FLOATS[c]])
+def test_a_tangent_is_refused(what, name):
+    # in forward mode the result would need one
+    call, args = getattr(K, what), CALLS[what]()
+    if what == "integer_product" and name == "x":
+        args.update(x=z(4, 32), x_scale=None)
+    if what in ("cache_store", "shared_attention"):
+        args.update(k_scale=None, v_scale=None)
+    with torch.autograd.forward_ad.dual_level():
+        call(**args)
+        t = args[name]
+        dual = dict(args, **{name: torch.autograd.forward_ad.make_dual(t, torch.ones_like(t))})
+        with pytest.raises(K.KvrError):
+            call(**dual)
+        with torch.no_grad(), pytest.raises(K.KvrError):  # (which leaves forward mode on)
+            call(**dual)
+        with torch.inference_mode():
+            call(**args)
+    call(**args)
+
+
+def test_tangents_of_scales_are_refused():
+    for what, name in (("cache_store", "k_scale"), ("cache_store", "v_scale"), ("shared_attention", "k_scale"),
+                       ("shared_attention", "v_scale")):
+        args = CALLS[what]()
+        eight = {n: args[n].to(torch.float8_e4m3fn) for n in ("k_cache", "v_cache")}
+        with torch.autograd.forward_ad.dual_level():
+            dual = torch.autograd.forward_ad.make_dual(args[name], torch.ones_like(args[name]))
+            with pytest.raises(K.KvrError):
+                getattr(K, what)(**dict(args, **eight, **{name: dual}))
