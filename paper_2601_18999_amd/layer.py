@@ -19,7 +19,7 @@ import torch
 from torch.autograd import forward_ad
 
 from . import (kvr_block_norm, kvr_integer_product, kvr_linear_attention, kvr_linear_workspace, kvr_product_workspace)
-from .serve import _current, _gpu, _no_gradient, _no_tangent, _refuse, _status, _stream, _vector
+from .serve import _current, _gpu, _no_gradient, _no_tangent, _refuse, _single, _status, _stream, _vector
 
 DTYPE_CODES = {torch.bfloat16: 0, torch.float16: 1, torch.int8: 3, torch.float32: 4}
 ACTIVATIONS = {"none": 0, "sigmoid": 1, "silu": 2}
@@ -135,7 +135,8 @@ def block_norm(x: torch.Tensor, *, after: Optional[torch.Tensor] = None, gate: O
     if tokens and dim:
         kvr_block_norm(
             NORM_RECORD.pack(NORM_RECORD.size, code, res_code, 3 if int8 else code, tokens, dim,
-                             ACTIVATIONS[activation], eps, residual_scale, 0, p_x, p_after, p_gate, p_res, p_before,
+                             ACTIVATIONS[activation], _single(where, "eps", eps),
+                             _single(where, "residual_scale", residual_scale), 0, p_x, p_after, p_gate, p_res, p_before,
                              p_new, p_out, p_scale, x0, g0, r0, n0, o0),
             _stream(device.index))
     return BlockNorm(out, new, scale)
@@ -280,9 +281,9 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, state: t
         _refuse(where, "the elements of a head must be contiguous")
     code = DTYPE_CODES[q.dtype]
     args = LINEAR_RECORD.pack(LINEAR_RECORD.size, code, tokens, requests, heads, kv_heads, dim, slots,
-                              dim ** -0.5 if scale is None else scale, 0, q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                              out.data_ptr(), state.data_ptr(), q0, q1, k0, k1, v0, v1, o0, o1, s0, s1, p_decay,
-                              p_rows, p_read, p_write, _status(where, status, device))
+                              dim ** -0.5 if scale is None else _single(where, "scale", scale), 0, q.data_ptr(),
+                              k.data_ptr(), v.data_ptr(), out.data_ptr(), state.data_ptr(), q0, q1, k0, k1, v0, v1, o0,
+                              o1, s0, s1, p_decay, p_rows, p_read, p_write, _status(where, status, device))
     if not requests:
         # the C call takes no empty batch; what it would refuse for one request is refused here too
         _linear_bytes(code, tokens, 1, heads, kv_heads, dim, True)

@@ -91,6 +91,16 @@ def _no_tangent(where: str, *tensors) -> None:
         _refuse(where, "there is no tangent: call with the primal tensors")
 
 
+_BEYOND = 2.0 ** 128 - 2.0 ** 103  # the first number that rounds past 32 bits
+
+
+def _single(where: str, name: str, x) -> float:
+    """A number that 32 bits hold (struct packs no others)."""
+    if not -_BEYOND < x < _BEYOND:
+        _refuse(where, f"{name} must be finite in 32 bits")
+    return x
+
+
 # of a device's index; of the current device
 _stream, _current = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
@@ -299,9 +309,9 @@ def shared_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
         p_lse = lse.data_ptr()
     code = DTYPE_CODES.get(q.dtype, -1)
     args = ATTENTION_RECORD.pack(ATTENTION_RECORD.size, code, tokens, requests, groups, heads, width, pwidth,
-                                 dim ** -0.5 if scale is None else scale, 0, q.data_ptr(), out.data_ptr(), p_lse, q0,
-                                 q1, o0, o1, p_rows, p_length, p_table, p_start, p_prefix, p_plen, stride, pstride,
-                                 _status(where, status, device))
+                                 dim ** -0.5 if scale is None else _single(where, "scale", scale), 0, q.data_ptr(),
+                                 out.data_ptr(), p_lse, q0, q1, o0, o1, p_rows, p_length, p_table, p_start, p_prefix,
+                                 p_plen, stride, pstride, _status(where, status, device))
     # (the C call takes no batch without requests)
     nbytes = _attention_bytes(DTYPE_CODES[k_cache.dtype], kv_heads, dim, code, tokens, requests or 1, groups, heads)
     if not requests:

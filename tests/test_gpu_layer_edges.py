@@ -116,3 +116,13 @@ def test_tangents_of_scales_are_refused():
             dual = torch.autograd.forward_ad.make_dual(args[name], torch.ones_like(args[name]))
             with pytest.raises(K.KvrError):
                 getattr(K, what)(**dict(args, **eight, **{name: dual}))
+
+
+@pytest.mark.parametrize("what,name", [("block_norm", "eps"), ("block_norm", "residual_scale"),
+                                       ("linear_attention", "scale"), ("shared_attention", "scale")])
+@pytest.mark.parametrize("value", [1e39, -1e300, float("inf"), float("nan")])
+def test_numbers_that_32_bits_do_not_hold_are_refused(what, name, value):
+    args = CALLS[what]()
+    args.update({n: None for n in ("k_scale", "v_scale") if n in args})
+    with pytest.raises(K.KvrError):
+        getattr(K, what)(**args, **{name: value})
