@@ -453,7 +453,7 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunks_kernel(LinearArgs a
   // of them, and all keep the state.  (Where a request's state is read and
   // written in one place, one team has all heads: it could be written before
   // another has read it.)
-  const int teams = seg.parts == 1 && read == write ? 1 : OUT ? a.teams : 1;
+  const int teams = seg.parts == 1 && read == write && read >= 0 ? 1 : OUT ? a.teams : 1;
   if (team >= teams) return;
   const int s0 = a.share / teams * team, s1 = s0 + a.share / teams;
   // d^m; a decay of 0 has d^0 = 1

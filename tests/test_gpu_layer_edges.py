@@ -126,3 +126,18 @@ def test_numbers_that_32_bits_do_not_hold_are_refused(what, name, value):
     args.update({n: None for n in ("k_scale", "v_scale") if n in args})
     with pytest.raises(K.KvrError):
         getattr(K, what)(**args, **{name: value})
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("new,heads,kv,dim", [([200, 0, 9, 64] * 3, 32, 4, 128), ([40, 77] * 8, 15, 5, 64)])
+def test_linear_requests_that_begin_with_nothing_and_are_not_kept(new, heads, kv, dim, dtype):
+    # (their query heads are taken side by side, as no state is written)
+    none = [-1] * len(new)
+    p = R.Linear(new, heads=heads, kv_heads=kv, dim=dim, dtype=dtype, read=none, write=none, spare=1)
+    args = p.args()
+    note(f"linear unkept {heads}/{kv} {dim}")
+    out = K.linear_attention(*args)
+    R.check_linear(out, args[3], p)
+    assert torch.equal(args[3].cpu(), p.state)
+    in_place = K.linear_attention(*args[:6], None, args[7])
+    assert torch.equal(in_place, out)
