@@ -471,6 +471,8 @@ kvr_status kvr_shared_attention(const kvr_cache* c, const kvr_attention* a, void
  * rounded to nearest even.  A row whose largest magnitude is below 2^-100 has
  * zeros and the scale 0; one that holds an infinity or NaN has zeros and the
  * scale NaN.  (n is made of the r before it is rounded for d_residual_out.)
+ * Of 32 bits are the squares too: of a row whose sum of squares is beyond
+ * them the norm is 0.  A sigmoid below 2^-126 is 0.
  * d_out may be d_x where the types and strides are the same, else outputs do
  * not overlap inputs. */
 enum { KVR_ACT_NONE = 0, KVR_ACT_SIGMOID = 1, KVR_ACT_SILU = 2 }; /* z, 1 / (1 + e^-z), z / (1 + e^-z) */
@@ -536,8 +538,17 @@ kvr_status kvr_integer_product(const kvr_product* p, void* d_workspace, size_t b
  * What stands in a later token, or in another request, has no influence on a
  * row (infinities and NaN among it).  Where an infinity has an influence, the
  * value can be NaN in its place.  d_out does not overlap inputs.  Tokens behind
- * d_row_start's last are not written.  Where a call's tokens are split differently over calls, the
- * results differ by roundings; the same call gives the same bits.
+ * d_row_start's last are not written.
+ * Sums are of 32 bits, and what is added to a state is made of operands of 24.
+ * Calls of a token a request, and requests of up to 8 where the sizes of a call
+ * make it take their tokens one by one, are computed in 32 bits throughout.  Of
+ * other requests the scores q k^T and the states that queries meet are operands of 16
+ * bits, and of halves some products of what two numbers are beyond 8 bits are
+ * left out: results are off by up to 2^-16 (KVR_BF16) or 2^-13 + 2^-16 (KVR_FP16)
+ * of the sum of all terms' magnitudes before they are rounded, states of halves
+ * by 2^-22 of theirs, both beside the roundings of 32-bit sums.  Where a call's
+ * tokens are split differently over calls, the results differ by as much; the
+ * same call gives the same bits.
  * row_start that is not valid (negative, decreasing, more than num_tokens)
  * sets KVR_DEV_BAD_LENGTH in d_status (optional): every result is NaN, no
  * state is written.  A slot that the pool does not have sets KVR_DEV_BAD_PAGE:

@@ -111,8 +111,10 @@ kvr_status lay_out(const kvr_linear* l, LinearLayout* o) {
         tokens > (l->heads == l->kv_heads ? 2 * n : n) * l->num_requests)
       least = n;
   // A batch of short requests is not cut, though one could be long (100 requests
-  // of 4 tokens, 4 / 2 heads: 9.7 instead of 20 us; one of 448 and 63 of one, 32 /
-  // 8 heads of 128: 94 instead of 73, 32 / 32: 84 instead of 86).
+  // of 4 tokens, 4 / 2 heads: 9.7 instead of 20 us, and 100 of 6, which are more in
+  // all, 19; 64 of 8, 32 / 8 heads of 128: 29, with a token more 35).  One long one
+  // among single tokens pays for that (of 448 among 63, 32 / 8 heads: 94 instead of
+  // 73; of 449 106, of 450 75 again; 32 / 32: 84 instead of 86).
   if (tokens <= 512 && tokens <= 16 * (int64_t)l->num_requests) least = 512;
   const int64_t segment = even > least ? (even + 63) / 64 * 64 : least;
   const bool cut = l->d_row_start && tokens > segment;  // whether there can be a request of several segments

@@ -284,7 +284,9 @@ __device__ __forceinline__ f32x4 multiply(s16x8 a, s16x8 b, f32x4 c) {
 }
 
 // Tokens as the matrix units take them: bfloat16 as they are, halves as two
-// bfloat16 (exact but for the smallest).
+// bfloat16, exactly.  (Of the products of such pairs that of the two second parts
+// is left out, which is below 2^-14 of the whole; of what is added to a state,
+// where one factor has three parts, below 2^-22.)
 struct OfBf16 {
   typedef __bf16 Type;
   static constexpr int kParts = 1;

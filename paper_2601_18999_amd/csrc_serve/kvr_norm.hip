@@ -2,13 +2,14 @@
 // (kvr_block_norm; kvr.h has the formulas).
 //
 // A row is held in registers (32-bit) from its one reading to its one writing,
-// V times eight elements a lane; the two means and the largest magnitude are
+// V times eight elements a lane (rows above 32,768 partly in scratch memory: see
+// launch_typed); the two means and the largest magnitude are
 // sums and maxima over its lanes, and those of its waves over LDS.  Memory
 // bounds long calls, as every input is read once and every output written once:
 // 9,216 rows of 4,096 with everything and a 32-bit residual (528 MB) 97 us, 5.4
 // TB/s (a copy: 5.1).  Short ones are bound by the row's two or three sums, each of
-// which the next step waits for: 777 rows of 5,003 (31 MB) 11 us, 8 rows of
-// 4,096 3.5.
+// which the next step waits for: 777 rows of 5,003 (31 MB) 11.2 us, of 5,000
+// 10.5, 8 rows of 4,096 3.5.
 #include <hip/hip_runtime.h>
 
 #include "kvr_layer.h"
@@ -240,7 +241,10 @@ void launch(const NormArgs& a, hipStream_t st) {
 // waits (9,216 rows of 4,096, 16-bit residual and norm before: 61 us with 8, 54
 // with 16, 67 with 32), where the residual has 16 bits; with a 32-bit one that
 // takes too many registers (9,216 rows with everything: 98 us with 8, 102 with
-// 16).
+// 16).  64 values, of rows above 32,768, are more than 128 registers hold beside
+// what is on its way: 74 to 257 of them go to scratch memory (16-bit result, norm
+// before: 2,048 rows of 32,768 56 us, 4.8 TB/s; 1,024 of 65,536 117, 2.3 TB/s; of
+// 65,533 218).
 template <class T, class R>
 void launch_typed(const NormArgs& a, hipStream_t st) {
   constexpr bool kWide = sizeof(R) == 4;
