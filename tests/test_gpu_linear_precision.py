@@ -38,6 +38,15 @@ def test_precision(new, heads, kv, dim, make, dtype):
 
 
 @TYPES
+@pytest.mark.parametrize("new,heads,kv", [([300], 512, 512), ([70, 5], 1024, 1024), ([130, 1, 64], 300, 300),
+                                          ([90], 640, 1), ([1, 1], 257, 257)])
+def test_precision_of_many_heads(new, heads, kv, dtype):
+    # more key heads than compute units, and many query heads beside each other
+    p = P.problem(new, heads, kv, 64, dtype)
+    P.check(*run(p), p)
+
+
+@TYPES
 @pytest.mark.parametrize("dim", [64, 128])
 def test_precision_in_place_and_in_slices(dim, dtype):
     p = P.problem([5, 70, 1, 300], 6, 2, dim, dtype, read=[0, 1, -1, 3], write=[0, 1, 2, 3])
